@@ -395,6 +395,134 @@ craft_status craft_moe_rank_forward_tiles(const craft_plan_t *plan, int32_t laye
 craft_status craft_moe_rank_forward_result(const void *workspace, int64_t *rows,
                                            int32_t *overflow);
 
+/* ------------------------------------------------------------ paged key/value cache
+ * Not in the paper, whose memory budget is the part of HBM that replicas of experts do not take
+ * from the key/value cache (Sec. 4.2, Sec. 5): the cache of the attention in front of the MoE layer,
+ * what a serving step does to it, and the attention of one new token per request.
+ *
+ * The cache of one layer is a pool of pages of page_size tokens.  Token i of request r lives in
+ * page table[r][i / page_size] at place i % page_size; its "slot" is page * page_size + place.
+ *   format     of the stored elements.  CRAFT_KV_F32 and CRAFT_KV_BF16: queries, new rows and
+ *              outputs are of the same type.  CRAFT_KV_E4M3: OCP FP8 E4M3 codes with one fp32 scale
+ *              per token and head (as craft_quantize_e4m3: scale = max|x| / 448, 1 for a row of
+ *              zeros); queries, new rows and outputs are bf16
+ *   pages, page_size, heads   page_size a power of two up to 65536; pages * page_size < 2^31
+ *   dk, dv     elements of a key row and of a value row; multiples of 4 (F32), 8 (BF16), 16 (E4M3)
+ *   k          DEVICE [pages][heads][page_size][dk] by the strides below (in elements; the last
+ *              dimension is contiguous), 16-byte aligned, as every stride in bytes
+ *   v          DEVICE likewise [..][dv]; or NULL: latent rows, a token's value row is the first dv
+ *              elements of its key row (dv <= dk; the v strides and v_scale are ignored)
+ *   k_scale, v_scale   DEVICE [pages][heads][page_size] fp32, 16-byte aligned, CRAFT_KV_E4M3 only
+ * Limits: dk and dv <= 256 with rows of their own, dk <= 576 and dv <= 512 for latent rows; strides
+ * are positive, a token's below 2^26 bytes.
+ */
+enum { CRAFT_KV_F32 = 0, CRAFT_KV_BF16 = 1, CRAFT_KV_E4M3 = 2 };
+
+typedef struct {
+    int32_t format;
+    int32_t page_size;
+    int64_t pages;
+    int32_t heads, dk, dv;
+    void *k;
+    void *v;
+    float *k_scale;
+    float *v_scale;
+    int64_t k_page, k_head, k_token;
+    int64_t v_page, v_head, v_token;
+} craft_kv_cache;
+
+/* Block tables and slot map of one serving step, from the lengths of the requests.
+ * Request r has lens[r] tokens in the cache and gets add[r] more; add[r] < 0: it has ended and its
+ * pages go back to the pool, to be handed out by a later call.
+ *   add, lens    DEVICE [R] int32; a length outside [0, max_pages * page_size] counts as the nearer end
+ *   table        DEVICE [R][table_stride] int32, of which max_pages entries per request are used;
+ *                entries of new pages are written, others left alone
+ *   ring, pool   DEVICE [pages] int32 and [2] int64: the free pages are ring[i % pages] for pool[0] <= i
+ *                < pool[1], handed out from the front; pages given back are written behind pool[1]
+ *                (ended requests in ascending order, a request's pages in the order of its tokens)
+ *   lens_out     DEVICE [R] int32: lengths after the step (0 for ended requests)
+ *   pool_out     DEVICE [2] int64.  lens_out and pool_out may be lens and pool themselves
+ *   token_off    DEVICE [R+1] int32: the step's tokens, request by request, are numbered
+ *                token_off[r] .. token_off[r+1]
+ *   slots        DEVICE [max_new] int32: slot of each token, -1 behind the last one (and for a token
+ *                whose table entry, written by someone else, is no page)
+ *   positions    DEVICE [max_new] int32, optional: its place in its request, -1 behind the last one
+ * A request that would outgrow its table row gets nothing and is skipped.  The others are served in
+ * order; from the first one on for which the free pages or the max_new places do not suffice, no
+ * request gets any token (ended ones give their pages back all the same).  What request r got is
+ * token_off[r+1] - token_off[r].
+ *   workspace    DEVICE, 16-byte aligned, at least craft_kv_tables_workspace() bytes
+ * Limits: R, max_pages * page_size, max_new and pages * page_size < 2^31, page_size a power of two up
+ * to 65536.  R may be 0 (pool_out, token_off[0] and the -1s are still written).
+ */
+typedef struct {
+    int32_t R, max_pages, page_size, max_new;
+    int64_t pages;
+    int64_t table_stride;
+    const int32_t *add;
+    const int32_t *lens;
+    int32_t *table;
+    int32_t *ring;
+    const int64_t *pool;
+    int32_t *lens_out;
+    int64_t *pool_out;
+    int32_t *token_off;
+    int32_t *slots;
+    int32_t *positions;
+    void *workspace;
+    size_t workspace_bytes;
+} craft_kv_tables_args;
+
+craft_status craft_kv_tables_workspace(const craft_kv_tables_args *args, size_t *bytes);
+craft_status craft_kv_tables(const craft_kv_tables_args *args, void *stream);
+
+/* New tokens' keys and values into their slots.
+ *   k      DEVICE [T][heads][dk], a token every k_stride elements (heads of a token next to one another)
+ *   v      DEVICE [T][heads][dv], every v_stride elements; ignored for latent rows
+ *   slots  DEVICE [T] int32; a slot outside [0, pages * page_size) is skipped.  Slots must differ: of
+ *          rows for the same slot any may remain, or in 8 bits a mixture
+ * Rows 16-byte aligned.  T may be 0. */
+craft_status craft_kv_append(const craft_kv_cache *cache, int64_t T, const void *k, int64_t k_stride,
+                             const void *v, int64_t v_stride, const int32_t *slots, void *stream);
+
+/* Attention of one new token per request over the cache (which holds that token's row already):
+ *   s[i] = scale * q . K[i],  out = sum_i softmax(s)[i] V[i]   over the tokens i of the request,
+ * the last `window` of them if window > 0.  Query head h reads cache head h / (Hq / heads).
+ *   q       DEVICE [R][Hq][dk], a request every q_stride elements, a head every q_head_stride
+ *   lens    DEVICE [R] int32; 0 or less (a place of the batch that is not in use): out is zeros, lse
+ *           -infinity.  A length over max_pages * page_size counts as that
+ *   table   DEVICE [R][table_stride] int32.  Tokens whose page is outside [0, pages) are left out
+ *   out     DEVICE [R][Hq][dv] contiguous, of q's type, fully overwritten
+ *   lse     DEVICE [R][Hq] fp32, optional: log sum_i exp(s[i]), with which parts of a context that
+ *           lie elsewhere can be joined
+ *   workspace  DEVICE, 16-byte aligned, at least craft_decode_attention_workspace() bytes.  Calls
+ *           that share one must be ordered on one stream
+ * Scores, maxima, sums and the weighted sum are fp32; the weights exp(s - max) are rounded to bf16
+ * in front of the product with 16- and 8-bit values.  The result depends on the arguments only (the
+ * order of the sums: on the lengths and on the GPU's number of compute units), never on scheduling.
+ * Rows of the pages behind a request's last token may hold anything.
+ * Limits: Hq a multiple of heads; R * Hq < 2^31; max_pages * page_size < 2^31.  R may be 0.
+ */
+typedef struct {
+    int32_t R, Hq;
+    int32_t max_pages, window;
+    float scale;
+    const void *q;
+    int64_t q_stride, q_head_stride;
+    const int32_t *lens;
+    const int32_t *table;
+    int64_t table_stride;
+    void *out;
+    float *lse;
+    void *workspace;
+    size_t workspace_bytes;
+} craft_attention_args;
+
+craft_status craft_decode_attention_workspace(const craft_kv_cache *cache, const craft_attention_args *args,
+                                              size_t *bytes);
+craft_status craft_decode_attention(const craft_kv_cache *cache, const craft_attention_args *args,
+                                    void *stream);
+
 /* ------------------------------------------------------------ kernel timing
  * Optional HIP-event timing of the kernels inside craft_moe_rank_forward, recorded on the
  * stream the kernels run on.  level 0 = off, 1 = the grouped gate/up GEMM only, 2 = every

@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libcraft.so")
 
 CRAFT_F32, CRAFT_BF16 = 0, 1
 CRAFT_W_BF16, CRAFT_W_E4M3 = 0, 1
+CRAFT_KV_F32, CRAFT_KV_BF16, CRAFT_KV_E4M3 = 0, 1, 2
 KERNEL_NAMES = ["route", "scan", "dispatch", "gateup", "down", "combine", "gate"]
 
 c_i32, c_i64, c_vp, c_sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t
@@ -40,6 +41,25 @@ class FwdArgs(ctypes.Structure):
                 ("tile_rows_down", c_i32), ("riders_gateup", c_i32), ("riders_down", c_i32),
                 ("tables", c_vp), ("workspace", c_vp),
                 ("workspace_bytes", c_sz)]
+
+
+class KvCacheDesc(ctypes.Structure):
+    _fields_ = [("format", c_i32), ("page_size", c_i32), ("pages", c_i64), ("heads", c_i32), ("dk", c_i32), ("dv", c_i32),
+                ("k", c_vp), ("v", c_vp), ("k_scale", c_vp), ("v_scale", c_vp),
+                ("k_page", c_i64), ("k_head", c_i64), ("k_token", c_i64),
+                ("v_page", c_i64), ("v_head", c_i64), ("v_token", c_i64)]
+
+
+class KvTablesArgs(ctypes.Structure):
+    _fields_ = [("R", c_i32), ("max_pages", c_i32), ("page_size", c_i32), ("max_new", c_i32), ("pages", c_i64), ("table_stride", c_i64),
+                ("add", c_vp), ("lens", c_vp), ("table", c_vp), ("ring", c_vp), ("pool", c_vp), ("lens_out", c_vp), ("pool_out", c_vp),
+                ("token_off", c_vp), ("slots", c_vp), ("positions", c_vp), ("workspace", c_vp), ("workspace_bytes", c_sz)]
+
+
+class AttentionArgs(ctypes.Structure):
+    _fields_ = [("R", c_i32), ("Hq", c_i32), ("max_pages", c_i32), ("window", c_i32), ("scale", ctypes.c_float),
+                ("q", c_vp), ("q_stride", c_i64), ("q_head_stride", c_i64), ("lens", c_vp), ("table", c_vp), ("table_stride", c_i64),
+                ("out", c_vp), ("lse", c_vp), ("workspace", c_vp), ("workspace_bytes", c_sz)]
 
 
 EXPORTS = {
@@ -76,6 +96,11 @@ EXPORTS = {
     "craft_moe_rank_forward_tiles": (ctypes.c_int, [c_vp, c_i32, c_i32, P(FwdArgs), P(c_i32), P(c_i32),
                                                     P(c_i32), P(c_i32)]),
     "craft_moe_rank_forward_result": (ctypes.c_int, [c_vp, P(c_i64), P(c_i32)]),
+    "craft_kv_tables_workspace": (ctypes.c_int, [P(KvTablesArgs), P(c_sz)]),
+    "craft_kv_tables": (ctypes.c_int, [P(KvTablesArgs), c_vp]),
+    "craft_kv_append": (ctypes.c_int, [P(KvCacheDesc), c_i64, c_vp, c_i64, c_vp, c_i64, c_vp, c_vp]),
+    "craft_decode_attention_workspace": (ctypes.c_int, [P(KvCacheDesc), P(AttentionArgs), P(c_sz)]),
+    "craft_decode_attention": (ctypes.c_int, [P(KvCacheDesc), P(AttentionArgs), c_vp]),
     "craft_probe_copy": (ctypes.c_int, [c_vp, c_vp, c_i64, c_vp]),
     "craft_probe_read": (ctypes.c_int, [c_vp, c_i64, c_i32, c_i32, c_vp, P(ctypes.c_double), c_vp]),
     "craft_probe_mfma_bf16": (ctypes.c_int, [c_i32, c_i32, c_vp, P(ctypes.c_double), c_vp]),
@@ -454,6 +479,165 @@ class RankForward:
         _check(lib().craft_moe_rank_forward_result(_dev(self.workspace), rows, ovf),
                "craft_moe_rank_forward_result")
         return rows.value, ovf.value
+
+
+# ---------------------------------------------------------- paged key/value cache
+
+class KvCache:
+    """The paged cache of one layer over tensors that the caller made.
+
+    k, v: cuda [pages][heads][page_size][d], float32, bfloat16 or float8_e4m3fn; any strides with a contiguous last
+    dimension.  v=None: latent rows, a token's value row is the first `dv` elements of its key row.
+    k_scale, v_scale: cuda float32 [pages][heads][page_size], for float8_e4m3fn only."""
+
+    def __init__(self, k, v=None, k_scale=None, v_scale=None, dv: Optional[int] = None):
+        import torch
+        formats = {torch.float32: CRAFT_KV_F32, torch.bfloat16: CRAFT_KV_BF16, torch.float8_e4m3fn: CRAFT_KV_E4M3}
+        assert k.dtype in formats and k.dim() == 4 and k.stride(3) == 1 and k.is_cuda
+        pages, heads, page_size, dk = k.shape
+        if v is None:
+            assert dv is not None, "latent rows need the number of value elements"
+        else:
+            assert v.dtype == k.dtype and v.shape[:3] == k.shape[:3] and v.stride(3) == 1 and v.device == k.device
+            assert dv is None or dv == v.shape[3]
+            dv = v.shape[3]
+        eight = k.dtype == torch.float8_e4m3fn
+        assert (k_scale is not None) == eight and (v_scale is not None) == (eight and v is not None)
+        for sc in (k_scale, v_scale):
+            assert sc is None or (sc.dtype == torch.float32 and tuple(sc.shape) == (pages, heads, page_size) and sc.is_contiguous())
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.pages, self.heads, self.page_size, self.dk, self.dv = pages, heads, page_size, dk, dv
+        self.dtype = torch.bfloat16 if eight else k.dtype          # of queries, new rows and outputs
+        d = KvCacheDesc()
+        d.format, d.page_size, d.pages, d.heads, d.dk, d.dv = formats[k.dtype], page_size, pages, heads, dk, dv
+        d.k, (d.k_page, d.k_head, d.k_token) = k.data_ptr(), self._strides(k)
+        if v is not None:
+            d.v, (d.v_page, d.v_head, d.v_token) = v.data_ptr(), self._strides(v)
+        d.k_scale = k_scale.data_ptr() if k_scale is not None else None
+        d.v_scale = v_scale.data_ptr() if v_scale is not None else None
+        self.desc = d
+
+    @staticmethod
+    def _strides(t):
+        # a dimension of one element has no stride of its own: any that is allowed will do
+        return [st if n > 1 else t.shape[3] for n, st in zip(t.shape[:3], t.stride()[:3])]
+
+    @classmethod
+    def allocate(cls, pages: int, page_size: int, heads: int, dk: int, dv: Optional[int] = None, dtype: str = "bf16",
+                 latent: bool = False, device="cuda:0"):
+        """A zeroed cache; dtype "f32", "bf16" or "e4m3"; dv is dk unless given."""
+        import torch
+        td = {"f32": torch.float32, "bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}[dtype]
+        dv = dk if dv is None else dv
+        rows = lambda d: torch.zeros((pages, heads, page_size, d), dtype=td, device=device)
+        scales = lambda: torch.ones((pages, heads, page_size), dtype=torch.float32, device=device)
+        eight = dtype == "e4m3"
+        return cls(rows(dk), None if latent else rows(dv), scales() if eight else None,
+                   scales() if eight and not latent else None, dv)
+
+    def append(self, k, v, slots, stream=None):
+        """k: cuda [T][heads][dk], v: [T][heads][dv] (None for latent rows), of the cache's `dtype`, the heads of a
+        token contiguous; slots: cuda int32 [T], negative ones skipped."""
+        import torch
+        T = slots.shape[0]
+        assert slots.dtype == torch.int32 and slots.is_cuda and slots.is_contiguous()
+        row_k = self._rows(k, T, self.dk)
+        row_v = self._rows(v, T, self.dv) if self.v is not None else 0
+        assert self.v is not None or v is None
+        _check(lib().craft_kv_append(ctypes.byref(self.desc), T, c_vp(k.data_ptr()), row_k,
+                                     c_vp(v.data_ptr()) if v is not None else None, row_v, c_vp(slots.data_ptr()), _stream_ptr(stream)),
+               "craft_kv_append")
+
+    def _rows(self, t, T, d):
+        assert t.is_cuda and t.dtype == self.dtype and tuple(t.shape) == (T, self.heads, d)
+        assert (d == 1 or t.stride(2) == 1) and (self.heads == 1 or t.stride(1) == d)
+        return t.stride(0) if T > 1 else self.heads * d
+
+
+class KvTables:
+    """Block tables, lengths and free pages of up to `requests` requests, advanced on the GPU step by step.
+
+    After step(add): `slots` and `positions` (int32 [max_new], -1 behind the last token) and `token_off`
+    (int32 [requests + 1]) describe the step's tokens, `lens` and `table` the cache.  Tensors of an existing state can
+    be handed in; a new one has all pages free."""
+
+    def __init__(self, requests: int, max_pages: int, pages: int, page_size: int, max_new: int, lens=None, table=None, ring=None,
+                 pool=None, device="cuda:0"):
+        import torch
+        i32 = dict(dtype=torch.int32, device=device)
+        self.lens = torch.zeros(requests, **i32) if lens is None else lens
+        self.table = torch.full((requests, max_pages), -1, **i32) if table is None else table
+        self.ring = torch.arange(pages, **i32) if ring is None else ring
+        self.pool = torch.tensor([0, pages], dtype=torch.int64, device=device) if pool is None else pool
+        for t, shape, dtype in ((self.lens, (requests,), torch.int32), (self.ring, (pages,), torch.int32), (self.pool, (2,), torch.int64)):
+            assert t.is_cuda and t.dtype == dtype and tuple(t.shape) == shape and t.is_contiguous()
+        assert self.table.is_cuda and self.table.dtype == torch.int32 and tuple(self.table.shape) == (requests, max_pages)
+        assert max_pages == 1 or self.table.stride(1) == 1
+        dev = self.lens.device
+        self.slots = torch.full((max_new,), -1, dtype=torch.int32, device=dev)
+        self.positions = torch.full((max_new,), -1, dtype=torch.int32, device=dev)
+        self.token_off = torch.zeros(requests + 1, dtype=torch.int32, device=dev)
+        a = KvTablesArgs()
+        a.R, a.max_pages, a.page_size, a.max_new, a.pages = requests, max_pages, page_size, max_new, pages
+        a.table_stride = self.table.stride(0) if requests > 1 else max_pages
+        a.lens, a.table, a.ring, a.pool = (t.data_ptr() for t in (self.lens, self.table, self.ring, self.pool))
+        a.token_off, a.slots, a.positions = self.token_off.data_ptr(), self.slots.data_ptr(), self.positions.data_ptr()
+        n = c_sz()
+        _check(lib().craft_kv_tables_workspace(ctypes.byref(a), n), "craft_kv_tables_workspace")
+        self.workspace = torch.empty(n.value, dtype=torch.uint8, device=dev)
+        a.workspace, a.workspace_bytes = self.workspace.data_ptr(), n.value
+        self.args = a
+
+    def step(self, add, lens_out=None, pool_out=None, stream=None):
+        """add: cuda int32 [requests], new tokens per request, negative: it has ended.  The new lengths and pool
+        counters replace the old ones, or go to `lens_out` and `pool_out`.  Returns slots."""
+        import torch
+        lens_out, pool_out = self.lens if lens_out is None else lens_out, self.pool if pool_out is None else pool_out
+        assert add.is_cuda and add.dtype == torch.int32 and add.shape == self.lens.shape and add.is_contiguous()
+        assert lens_out.dtype == torch.int32 and lens_out.shape == self.lens.shape and lens_out.is_contiguous()
+        assert pool_out.dtype == torch.int64 and pool_out.shape == self.pool.shape and pool_out.is_contiguous()
+        a = self.args
+        a.add, a.lens_out, a.pool_out = add.data_ptr(), lens_out.data_ptr(), pool_out.data_ptr()
+        _check(lib().craft_kv_tables(ctypes.byref(a), _stream_ptr(stream)), "craft_kv_tables")
+        return self.slots
+
+
+class DecodeAttention:
+    """Output, workspace and argument block for repeated calls of one new token per request over a KvCache."""
+
+    def __init__(self, cache: KvCache, requests: int, query_heads: int, max_pages: int, scale: Optional[float] = None,
+                 window: int = 0, want_lse: bool = False):
+        import torch
+        self.cache, self.R, self.Hq, self.max_pages = cache, requests, query_heads, max_pages
+        dev = cache.k.device
+        self.out = torch.empty((requests, query_heads, cache.dv), dtype=cache.dtype, device=dev)
+        self.lse = torch.empty((requests, query_heads), dtype=torch.float32, device=dev) if want_lse else None
+        a = AttentionArgs()
+        a.R, a.Hq, a.max_pages, a.window = requests, query_heads, max_pages, window
+        a.scale = cache.dk ** -0.5 if scale is None else scale
+        a.out = self.out.data_ptr()
+        a.lse = self.lse.data_ptr() if want_lse else None
+        n = c_sz()
+        _check(lib().craft_decode_attention_workspace(ctypes.byref(cache.desc), ctypes.byref(a), n), "craft_decode_attention_workspace")
+        self.workspace = torch.empty(n.value, dtype=torch.uint8, device=dev)
+        a.workspace, a.workspace_bytes = self.workspace.data_ptr(), n.value
+        self.args = a
+
+    def __call__(self, q, lens, table, stream=None):
+        """q: cuda [requests][query_heads][dk]; lens: int32 [requests]; table: int32 [requests][max_pages].  Returns
+        the (reused) output tensor."""
+        import torch
+        assert q.is_cuda and q.dtype == self.cache.dtype and tuple(q.shape) == (self.R, self.Hq, self.cache.dk) and q.stride(2) == 1
+        assert lens.is_cuda and lens.dtype == torch.int32 and tuple(lens.shape) == (self.R,) and lens.is_contiguous()
+        assert table.is_cuda and table.dtype == torch.int32 and tuple(table.shape) == (self.R, self.max_pages)
+        assert self.max_pages == 1 or table.stride(1) == 1
+        a = self.args
+        a.q, a.lens, a.table = q.data_ptr(), lens.data_ptr(), table.data_ptr()
+        a.q_head_stride = q.stride(1) if self.Hq > 1 else self.cache.dk
+        a.q_stride = q.stride(0) if self.R > 1 else self.Hq * self.cache.dk
+        a.table_stride = table.stride(0) if self.R > 1 else self.max_pages
+        _check(lib().craft_decode_attention(ctypes.byref(self.cache.desc), ctypes.byref(a), _stream_ptr(stream)), "craft_decode_attention")
+        return self.out
 
 
 def probe_copy(src, dst, stream=None):

@@ -11,6 +11,18 @@
 
 #include "kernels.h"
 
+int craft::num_compute_units() {
+    static int n = 0;
+    if (n == 0) {
+        int dev = 0;
+        hipDeviceProp_t prop;
+        if (hipGetDevice(&dev) == hipSuccess && hipGetDeviceProperties(&prop, dev) == hipSuccess)
+            n = prop.multiProcessorCount;
+        if (n <= 0) n = 256;
+    }
+    return n;
+}
+
 namespace {
 
 using namespace craft;
@@ -25,7 +37,7 @@ struct Layout {
     int64_t max_rows, NB;
 };
 
-int cached_num_cu();
+int cached_num_cu() { return num_compute_units(); }
 
 size_t gate_workspace_bytes(int32_t dtype, int64_t T, int32_t H, int32_t E) {
     const int nparts = dtype == CRAFT_BF16 && T > 0 ? router_logits_parts(T, H, E, cached_num_cu()) : 1;
@@ -95,18 +107,6 @@ struct ScopedEvent {
         if (stop) (void)hipEventRecord(stop, s);
     }
 };
-
-int cached_num_cu() {
-    static int n = 0;
-    if (n == 0) {
-        int dev = 0;
-        hipDeviceProp_t prop;
-        if (hipGetDevice(&dev) == hipSuccess && hipGetDeviceProperties(&prop, dev) == hipSuccess)
-            n = prop.multiProcessorCount;
-        if (n <= 0) n = 256;
-    }
-    return n;
-}
 
 // ---- row-tile height of the packed FFN ---------------------------------------------------
 // A row-tile may have 4 to 8 fragments of 32 rows.  Taller tiles reuse a weight fragment more

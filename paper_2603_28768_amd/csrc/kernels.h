@@ -10,6 +10,9 @@
 
 namespace craft {
 
+// Compute units of the current device (256 where there is none), looked up once.
+int num_compute_units();
+
 // Tokens handled by one workgroup of the routing and dispatch kernels.  Ranks of
 // assignments inside a block are taken from a 32-bit token mask per expert.
 constexpr int kTokPerBlock = 32;
@@ -263,5 +266,60 @@ hipError_t launch_probe_mfma(int32_t blocks, int32_t iters, float *sink, hipStre
 hipError_t launch_probe_mfma_operands(int32_t shape, int32_t data, int32_t blocks, int32_t iters, float *sink,
                                       hipStream_t s);
 hipError_t launch_load_accumulate(const int32_t *counts, int64_t n, int64_t *window, hipStream_t s);
+
+// ---- paged key/value cache (kv_cache.hip, attention.hip) ------------------------------------
+struct KvTablesArgs {
+    int32_t R, max_pages, max_new;
+    int32_t shift;                 // log2 of the tokens of a page
+    int64_t pages, table_stride;
+    const int32_t *add, *lens;
+    int32_t *table, *ring;
+    const int64_t *pool;
+    int32_t *lens_out;
+    int64_t *pool_out;
+    int32_t *token_off, *slots, *positions;
+    int32_t *ws_ctrl, *ws_len, *ws_page, *ws_back;     // workspace of a step of two launches
+};
+hipError_t launch_kv_tables(const KvTablesArgs &a, hipStream_t s);
+
+struct KvAppendArgs {
+    int64_t T;
+    int32_t heads;
+    int32_t k_row, v_row;          // 16-byte pieces of a new row
+    const unsigned char *k, *v;    // new rows; v null: latent
+    int64_t k_stride, v_stride;    // bytes between tokens
+    const int32_t *slots;
+    int64_t slots_total;
+    int32_t shift;
+    unsigned char *ck, *cv;        // the cache, strides in bytes
+    int64_t ck_page, ck_head, ck_token, cv_page, cv_head, cv_token;
+    float *k_scale, *v_scale;
+};
+hipError_t launch_kv_append(const KvAppendArgs &a, bool e4m3, hipStream_t s);
+
+struct AttentionArgs {
+    int32_t format;                // CRAFT_KV_*
+    int32_t R, Hq, heads, group;   // group = Hq / heads
+    int32_t dk, dv;
+    const void *q;
+    int64_t q_stride, q_head;      // elements
+    const int32_t *lens, *table;
+    int64_t table_stride;
+    int32_t max_pages, window, shift;
+    float scale_log2;              // scale * log2(e)
+    const unsigned char *k, *v;    // strides in bytes
+    int64_t k_page, k_head, k_token, v_page, v_head, v_token;
+    const float *k_scale, *v_scale;
+    int64_t pages;
+    void *out;
+    float *lse;
+    float *part;                   // workspace
+    int32_t *desc;
+    int32_t workers;
+};
+// Workgroups a launch may have, whatever the lengths; the workspace is sized for them.
+int32_t attention_workers(const AttentionArgs &a, int32_t num_cu);
+size_t attention_workspace(const AttentionArgs &a, int32_t num_cu);
+hipError_t launch_decode_attention(const AttentionArgs &a, hipStream_t s);
 
 }  // namespace craft
