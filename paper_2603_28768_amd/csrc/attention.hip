@@ -21,11 +21,12 @@
 // A wave has the keys of the next unit in flight while it works on the weights and values of this one, and the
 // other way round.
 //
-// Work: the units of all (request, head) items, laid end to end, are cut into equal runs, one per workgroup, by
-// prefix sums over the lengths that every workgroup does for itself: the launch does not depend on the lengths
-// (which the host does not know), and long and short requests take equal parts of the GPU.  The four waves of a
-// workgroup share its run of an item and meet in LDS at its end.  An item cut between workgroups leaves partial
-// sums, which a second launch joins in the order of the workgroups.
+// Work: the (request, head) items, each its units and a few more for what an item costs by itself, are laid end
+// to end and cut into equal runs, one per wave, by prefix sums over the lengths that every workgroup does for
+// itself: the launch does not depend on the lengths (which the host does not know), and long and short requests
+// take equal parts of the GPU.  A wave walks its run alone; what it begins and does not end, or ends and did not
+// begin, meets the neighbouring waves' sums in LDS at the end of the workgroup.  An item cut between workgroups
+// leaves partial sums, which a second launch joins in the order of the workgroups.
 #include <algorithm>
 
 #include "ffn_common.h"
@@ -38,7 +39,8 @@ typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kUnit = 32;                          // tokens
-constexpr int kMinUnits = 8;                       // of a workgroup's run, where there are few
+constexpr int kItemCost = 2;                       // what an item costs beside its units
+constexpr int kMinRun = 4;                         // of a wave, where there is little to do
 constexpr uint32_t kFar = 0x80000000u;             // an offset behind the end of every page: reads as zeros
 
 // Elements of 16 bytes, of the widest value load of a lane, and what the products take.
@@ -75,6 +77,12 @@ template <> struct Words<1> {
 template <int W> __device__ __forceinline__ uint32_t word(const typename Words<W>::type &x, int i) { return x[i]; }
 template <> __device__ __forceinline__ uint32_t word<1>(const uint32_t &x, int) { return x; }
 
+// The same in every lane of the wave: kept in scalar registers.
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+    return (int64_t)((uint64_t)(uint32_t)uniform((int32_t)(x >> 32)) << 32 | (uint32_t)uniform((int32_t)x));
+}
+
 // Reductions over the four lanes that hold a head (lane & 15): lanes 16 and 32 apart change places.
 __device__ __forceinline__ float other16(float x) {
     return __shfl_xor(x, 16, 64);
@@ -102,30 +110,43 @@ __device__ __forceinline__ int32_t units_of(const AttentionArgs &a, int32_t r, i
     return max(1, (int32_t)(((int64_t)n + kUnit - 1) / kUnit) - lo / kUnit);
 }
 
-// Where a run starts: request, units of the list in front of it, and the length of the list.
-struct Start {
-    int64_t before, total;
-    int32_t request;
+// The list of items cut into n runs.  Lengths in units, an item's own cost included.
+struct Runs {
+    int64_t total, each;   // the first `more` runs are one longer than `each`
+    int32_t n, more;
+    __device__ __forceinline__ void cut(int64_t t, int32_t most) {
+        total = t;
+        n = (int32_t)min((int64_t)most, (t + kMinRun - 1) / kMinRun);
+        if (t >> 32) {
+            each = t / n;
+        } else {
+            each = (uint32_t)t / (uint32_t)n;
+        }
+        more = (int32_t)(t - each * n);
+    }
+    __device__ __forceinline__ int64_t start(int32_t w) const { return each * w + min(w, more); }
+    __device__ __forceinline__ int32_t of(int64_t at) const {      // the run that holds place `at`
+        const int64_t longer = (each + 1) * more;
+        return at < longer ? (int32_t)(at / (each + 1)) : more + (int32_t)((at - longer) / each);
+    }
 };
 
-// The request that holds unit `rank * total / n` of the list; every thread of the workgroup gets it.
-// items: heads x blocks of 16 query heads.
-struct Runs {
-    int64_t total;
-    int32_t n;             // workgroups with a run
-    __device__ __forceinline__ int64_t start(int32_t w) const { return total * w / n; }
-    __device__ __forceinline__ int32_t of(int64_t unit) const { return (int32_t)(((unit + 1) * n - 1) / total); }
+// The request in which each wave's run starts, and the cost in front of it.
+struct Start {
+    int64_t before;
+    int32_t request;
 };
-__device__ __forceinline__ Start find_start(const AttentionArgs &a, int32_t items, int32_t rank, Runs *runs) {
+// per_request: items of a request (heads x blocks of 16 query heads).
+__device__ __forceinline__ Start find_start(const AttentionArgs &a, int32_t per_request, Runs &runs) {
     __shared__ int64_t wave_sum[kWaves];
-    __shared__ Start found;
+    __shared__ Start found[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int32_t per = (a.R + kThreads - 1) / kThreads;
     const int64_t r0 = min((int64_t)a.R, (int64_t)tid * per), r1 = min((int64_t)a.R, r0 + per);
     int64_t sum = 0;
     int32_t lo, len;
-    for (int64_t r = r0; r < r1; ++r) sum += units_of(a, (int32_t)r, &lo, &len);
-    sum *= items;
+    for (int64_t r = r0; r < r1; ++r) sum += units_of(a, (int32_t)r, &lo, &len) + kItemCost;
+    sum *= per_request;
     int64_t incl = sum;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -140,24 +161,103 @@ __device__ __forceinline__ Start find_start(const AttentionArgs &a, int32_t item
         if (w < wave) before += wave_sum[w];
         total += wave_sum[w];
     }
-    runs->total = total;
-    runs->n = (int32_t)min((int64_t)a.workers, (total + kMinUnits - 1) / kMinUnits);
-    const int64_t unit = rank < runs->n ? runs->start(rank) : total;
-    if (unit >= before && unit < before + sum) {
-        int32_t r = (int32_t)r0;
-        for (;; ++r) {
-            const int64_t u = (int64_t)units_of(a, r, &lo, &len) * items;
-            if (unit < before + u) break;
-            before += u;
+    runs.cut(uniform(total), a.workers * kWaves);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const int32_t rank = blockIdx.x * kWaves + w;
+        const int64_t at = runs.start(rank);
+        if (rank < runs.n && at >= before && at < before + sum) {
+            int64_t b = before;
+            int32_t r = (int32_t)r0;
+            for (;; ++r) {
+                const int64_t u = (int64_t)(units_of(a, r, &lo, &len) + kItemCost) * per_request;
+                if (at < b + u) break;
+                b += u;
+            }
+            found[w] = {b, r};
         }
-        found = {before, total, r};
     }
     __syncthreads();
-    return found;
+    return {uniform(found[wave].before), uniform(found[wave].request)};
 }
 
-// Partial sums of a run of an item: acc [16][DV], then m and l of 16 heads.
-template <int DV> constexpr int kPartFloats = 16 * DV + 32;
+// Running maximum, sum of weights and weighted sum of some tokens of an item, as a wave holds them: lane (head, g)
+// has the sum of the weights of its own tokens only, the rest is whole.
+template <int NV, int CE> struct Sums {
+    f32x4_t acc[NV][CE];
+    float m, l;
+    __device__ __forceinline__ void clear() {
+        m = -INFINITY;
+        l = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int e = 0; e < CE; ++e) acc[c][e] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    __device__ __forceinline__ void scale(float f) {
+        l *= f;
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int e = 0; e < CE; ++e) acc[c][e] *= f;
+    }
+    // Sums in memory: the accumulators, then m, then l, lane by lane.
+    static constexpr int kFloats = (NV * CE * 4 + 2) * 64;
+    __device__ __forceinline__ void put(float *to, int lane) const {
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int e = 0; e < CE; ++e) *reinterpret_cast<f32x4_t *>(to + ((c * CE + e) * 64 + lane) * 4) = acc[c][e];
+        to[NV * CE * 256 + lane] = m;
+        to[NV * CE * 256 + 64 + lane] = l;
+    }
+    __device__ __forceinline__ void add(const float *from, int lane) {
+        const float om = from[NV * CE * 256 + lane], ol = from[NV * CE * 256 + 64 + lane];
+        const float up = fmaxf(m, om);
+        const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - up), of = om == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(om - up);
+        m = up;
+        l = l * f + ol * of;
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int e = 0; e < CE; ++e) {
+                const f32x4_t x = *reinterpret_cast<const f32x4_t *>(from + ((c * CE + e) * 64 + lane) * 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[c][e][i] = acc[c][e][i] * f + x[i] * of;
+            }
+    }
+    // Row i of tile (c, e) is column (c 16 + 4 g + i) CE + e: CE neighbouring columns of the output per (c, i).
+    template <bool F32> __device__ __forceinline__ void write(const AttentionArgs &a, int32_t r, int32_t head0, int32_t n_heads, int lane) const {
+        const int col = lane & 15, g = lane >> 4;
+        const float sum = sum_of_head(l);
+        if (col >= n_heads) return;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        const int64_t head = (int64_t)r * a.Hq + head0 + col;
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int d = (c * 16 + 4 * g + i) * CE;
+                if (d >= a.dv) continue;
+                if constexpr (F32) {
+                    *reinterpret_cast<f32x4_t *>(static_cast<float *>(a.out) + head * a.dv + d) =
+                        (f32x4_t){acc[c][0][i] * inv, acc[c][1][i] * inv, acc[c][2][i] * inv, acc[c][3][i] * inv};
+                } else {
+                    uint32_t w[CE / 2];
+#pragma unroll
+                    for (int e = 0; e < CE / 2; ++e) w[e] = bf16_pair(acc[c][2 * e][i] * inv, acc[c][2 * e + 1][i] * inv);
+                    unsigned char *to = static_cast<unsigned char *>(a.out) + (head * a.dv + d) * 2;
+                    if constexpr (CE == 4) {
+                        *reinterpret_cast<u32x2_t *>(to) = (u32x2_t){w[0], w[1]};
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < CE / 8; ++e) *reinterpret_cast<u32x4_t *>(to + 16 * e) = (u32x4_t){w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]};
+                    }
+                }
+            }
+        if (g == 0 && a.lse) a.lse[head] = sum == 0.0f ? -INFINITY : (m + __log2f(sum)) * 0.6931471805599453f;
+    }
+};
 
 // Pages of the tokens that a lane reads of a unit.  Pages of 16 tokens and more: one for either tile, the same in
 // every lane.  SMALL pages: of the lane's key row in either tile, and of the tokens whose values it reads, which
@@ -171,29 +271,46 @@ template <int FMT, int DK, int DV, bool SMALL, bool AHEAD, int WPS>
 __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, int32_t blocks) {
     typedef Shape<FMT, DK, DV> S;
     typedef Words<S::VW> VWords;
-    constexpr int kPad = 4;                        // heads of the sums in LDS start in different banks
-    __shared__ float s_acc[kWaves][16][DV + kPad];
-    __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+    typedef Sums<S::NV, S::CE> State;
+    __shared__ float s_sums[kWaves][State::kFloats];   // of the item that a wave's run found begun
+    __shared__ int32_t s_found[kWaves];                // whether there is one, and whether it ends in the run
+    enum { kNone = 0, kOpen = 1, kEnded = 2 };
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
-    const int32_t items = a.heads * blocks, rank = blockIdx.x;
+    const int32_t per_request = a.heads * blocks, rank = blockIdx.x * kWaves + wave;
     Runs runs;
-    const Start st = find_start(a, items, rank, &runs);
-    if (tid == 0) a.desc[4 * rank] = -1;
-    if (rank >= runs.n) return;
-    const int64_t begin = runs.start(rank), end = runs.start(rank + 1);
-    int64_t at = begin, before = st.before;
+    const Start st = find_start(a, per_request, runs);
+    if (tid == 0) a.desc[4 * blockIdx.x] = -1;
+    if ((int32_t)blockIdx.x * kWaves >= runs.n) return;
+    int64_t at = 0, end = 0, before = st.before;
+    if (rank < runs.n) {
+        at = runs.start(rank);
+        end = runs.start(rank + 1);
+    }
     int32_t r = st.request;
+    if (lane == 0) s_found[wave] = kNone;
+    State z;
+    bool open = false;                             // the run ends inside an item that starts in it
+    int32_t open_item = 0, open_head0 = 0, open_heads = 0;
+    int64_t open_end = 0;
 
     while (at < end) {
         int32_t first, len;
-        const int32_t n_units = units_of(a, r, &first, &len);
+        const int32_t n_units = uniform(units_of(a, r, &first, &len));
+        first = uniform(first);
+        len = uniform(len);
+        const int32_t cost = n_units + kItemCost;
         const int64_t in_request = at - before;
-        const int32_t item = (int32_t)(in_request / n_units);
-        const int64_t item_begin = before + (int64_t)item * n_units, item_end = item_begin + n_units;
+        const int32_t item = in_request >> 32 ? (int32_t)(in_request / cost) : (int32_t)((uint32_t)in_request / (uint32_t)cost);
+        const int64_t item_begin = before + (int64_t)item * cost, item_end = item_begin + cost;
         const int64_t stop = min(end, item_end);
-        const int32_t u_lo = (int32_t)(at - item_begin), u_n = (int32_t)(stop - at);
-        const int32_t u0 = u_lo + (int32_t)((int64_t)u_n * wave / kWaves), u1 = u_lo + (int32_t)((int64_t)u_n * (wave + 1) / kWaves);
+        // an item's own cost comes first
+        const int32_t u0 = max(0, (int32_t)(at - item_begin) - kItemCost), u1 = max(0, (int32_t)(stop - item_begin) - kItemCost);
+        at = stop;
+        const int64_t item_before = before;
+        const int32_t item_r = r;
+        if (at == item_before + (int64_t)cost * per_request) { before = at; ++r; }
+        if (u0 == u1) continue;
         const int32_t h = item / blocks, block = item - h * blocks;
         const int32_t head0 = h * a.group + block * 16, n_heads = min(16, a.group - block * 16);
         const int32_t unit_base = first / kUnit;   // of the request's visible tokens
@@ -203,7 +320,7 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
         {
             const bool live = col < n_heads;
             constexpr int QB = FMT == CRAFT_KV_F32 ? 4 : 2, QE = 16 / QB;     // bytes of an element, elements of a piece
-            const unsigned char *qr = static_cast<const unsigned char *>(a.q) + ((int64_t)r * a.q_stride + (int64_t)(head0 + (live ? col : 0)) * a.q_head) * QB;
+            const unsigned char *qr = static_cast<const unsigned char *>(a.q) + ((int64_t)item_r * a.q_stride + (int64_t)(head0 + (live ? col : 0)) * a.q_head) * QB;
             const u32x4_t none = {0u, 0u, 0u, 0u};
 #pragma unroll
             for (int i = 0; i < S::QN; ++i) {
@@ -213,16 +330,11 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
         }
 
         const unsigned char *kh = a.k + h * a.k_head, *vh = a.v + h * a.v_head;
-        const int32_t *table = a.table + (int64_t)r * a.table_stride;
+        const int32_t *table = a.table + (int64_t)item_r * a.table_stride;
         const uint32_t k_span = 16u * (uint32_t)a.k_token, v_span = 16u * (uint32_t)a.v_token;
         const uint32_t k_off = (uint32_t)col * (uint32_t)a.k_token + g * 16;
 
-        f32x4_t acc[S::NV][S::CE];
-#pragma unroll
-        for (int c = 0; c < S::NV; ++c)
-#pragma unroll
-            for (int j = 0; j < S::CE; ++j) acc[c][j] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
-        float m = -INFINITY, l = 0.0f;             // l: of this lane's tokens only
+        z.clear();
 
         u32x4_t kr[2][AHEAD ? S::NK : 1];
         typename VWords::type vr[8][AHEAD ? S::NV : 1];
@@ -384,24 +496,19 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
             }
             float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
             top = max_of_head(top);
-            if (__any(top > m)) {
-                const float up = fmaxf(m, top);
-                const float f = up == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - up);
-                m = up;
-                l *= f;
-#pragma unroll
-                for (int c = 0; c < S::NV; ++c)
-#pragma unroll
-                    for (int j = 0; j < S::CE; ++j) acc[c][j] *= f;
+            if (__any(top > z.m)) {
+                const float up = fmaxf(z.m, top);
+                z.scale(up == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(z.m - up));
+                z.m = up;
             }
-            const float base = m == -INFINITY ? 0.0f : m;
+            const float base = z.m == -INFINITY ? 0.0f : z.m;
             float p[2][4];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     p[t][j] = __builtin_amdgcn_exp2f(x[t][j] - base);
-                    l += p[t][j];
+                    z.l += p[t][j];
                     if (FMT == CRAFT_KV_E4M3) p[t][j] *= vs[t][j];
                 }
             // ---- values
@@ -416,7 +523,7 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
                             const typename VWords::type vc = AHEAD ? vr[4 * t + j][AHEAD ? c : 0] : load_value(u, pages, seen, t, j, c);
 #pragma unroll
                             for (int e = 0; e < S::CE; ++e)
-                                acc[c][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word<S::VW>(vc, e)), p[t][j], acc[c][e], 0, 0, 0);
+                                z.acc[c][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word<S::VW>(vc, e)), p[t][j], z.acc[c][e], 0, 0, 0);
                         }
             } else {
                 const wide_t pw = {bf16_pair(p[0][0], p[0][1]), bf16_pair(p[0][2], p[0][3]), bf16_pair(p[1][0], p[1][1]), bf16_pair(p[1][2], p[1][3])};
@@ -436,8 +543,8 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
                                    : (e & 1) ? widen_pair<true>(word<S::VW>(vc[j], e >> 1)) : widen_pair<false>(word<S::VW>(vc[j], e >> 1));
                         const wide_t even = {perm(w[1], w[0], 0x05040100u), perm(w[3], w[2], 0x05040100u), perm(w[5], w[4], 0x05040100u), perm(w[7], w[6], 0x05040100u)};
                         const wide_t odd = {perm(w[1], w[0], 0x07060302u), perm(w[3], w[2], 0x07060302u), perm(w[5], w[4], 0x07060302u), perm(w[7], w[6], 0x07060302u)};
-                        acc[c][2 * e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, even), pf, acc[c][2 * e], 0, 0, 0);
-                        acc[c][2 * e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, odd), pf, acc[c][2 * e + 1], 0, 0, 0);
+                        z.acc[c][2 * e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, even), pf, z.acc[c][2 * e], 0, 0, 0);
+                        z.acc[c][2 * e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, odd), pf, z.acc[c][2 * e + 1], 0, 0, 0);
                     }
                 }
             }
@@ -445,94 +552,73 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
             pages = next;
         }
 
-        // ---- the four waves meet
-        l = sum_of_head(l);
-        __syncthreads();                           // the sums of the item before have been read
-        if (g == 0) { s_m[wave][col] = m; s_l[wave][col] = l; }
-#pragma unroll
-        for (int c = 0; c < S::NV; ++c)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int e = 0; e < S::CE; ++e) s_acc[wave][col][c * 16 * S::CE + (4 * g + j) * S::CE + e] = acc[c][e][j];
-        __syncthreads();
-        const bool starts = at == item_begin, ends = stop == item_end;
-        float *part = a.part + ((int64_t)2 * rank + (starts ? 1 : 0)) * kPartFloats<DV>;
-        for (int i = tid; i < n_heads * (DV / 4); i += kThreads) {
-            const int n = i / (DV / 4), d = (i - n * (DV / 4)) * 4;
-            float top = s_m[0][n];
-#pragma unroll
-            for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_m[w][n]);
-            float sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const float f = s_m[w][n] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(s_m[w][n] - top);
-                sum += f * s_l[w][n];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += f * s_acc[w][n][d + e];
-            }
-            if (starts && ends) {
-                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                const int64_t head = (int64_t)r * a.Hq + head0 + n;
-                if (d < a.dv) {
-                    if (FMT == CRAFT_KV_F32) {
-                        *reinterpret_cast<f32x4_t *>(static_cast<float *>(a.out) + head * a.dv + d) = (f32x4_t){v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
-                    } else {
-                        const u32x2_t w = {bf16_pair(v[0] * inv, v[1] * inv), bf16_pair(v[2] * inv, v[3] * inv)};
-                        *reinterpret_cast<u32x2_t *>(static_cast<unsigned char *>(a.out) + (head * a.dv + d) * 2) = w;
-                    }
-                }
-                if (d == 0 && a.lse) a.lse[head] = sum == 0.0f ? -INFINITY : (top + __log2f(sum)) * 0.6931471805599453f;
-            } else {
-                *reinterpret_cast<f32x4_t *>(part + n * DV + d) = (f32x4_t){v[0], v[1], v[2], v[3]};
-                if (d == 0) { part[16 * DV + n] = top; part[16 * DV + 16 + n] = sum; }
+        if (u0 > 0) {
+            z.put(s_sums[wave], lane);
+            if (lane == 0) s_found[wave] = u1 == n_units ? kEnded : kOpen;
+        } else if (u1 == n_units) {
+            z.template write<FMT == CRAFT_KV_F32>(a, item_r, head0, n_heads, lane);
+        } else {
+            open = true;
+            open_item = item;
+            open_head0 = head0;
+            open_heads = n_heads;
+            open_end = item_end;
+            r = item_r;
+        }
+    }
+
+    // ---- the waves meet: whoever began an item adds what the following waves found of it
+    __syncthreads();
+    float *part = a.part + (int64_t)2 * blockIdx.x * State::kFloats;
+    if (open) {
+        bool ended = false;
+        for (int w = wave + 1; w < kWaves && !ended; ++w) {
+            z.add(s_sums[w], lane);
+            ended = s_found[w] == kEnded;
+        }
+        if (ended) {
+            z.template write<FMT == CRAFT_KV_F32>(a, r, open_head0, open_heads, lane);
+        } else {
+            z.put(part + State::kFloats, lane);
+            if (lane == 0) {
+                // joined by the workgroup of the same number in the second launch
+                a.desc[4 * blockIdx.x] = r;
+                a.desc[4 * blockIdx.x + 1] = open_item;
+                a.desc[4 * blockIdx.x + 2] = runs.of(open_end - 1) / kWaves;
             }
         }
-        if (starts && !ends && tid == 0) {
-            // the item is joined by the workgroup of the same number in the second launch
-            a.desc[4 * rank] = r;
-            a.desc[4 * rank + 1] = item;
-            a.desc[4 * rank + 2] = runs.of(item_end - 1);
+    }
+    // the item that an earlier workgroup began
+    if (wave == 0 && s_found[0] != kNone) {
+        z.clear();
+        for (int w = 0; w < kWaves; ++w) {
+            z.add(s_sums[w], lane);
+            if (s_found[w] == kEnded) break;
         }
-        at = stop;
-        if (at == before + (int64_t)n_units * items) { before = at; ++r; }
+        z.put(part, lane);
     }
 }
 
-// Joins the parts of an item that starts in workgroup `rank`'s run and ends in a later one's.
-template <int FMT, int DV>
+// Joins the parts of an item that starts in workgroup blockIdx.x of the first launch and ends in a later one: that
+// one's last sums and the first ones of those that follow.
+template <int FMT, int DK, int DV>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttentionArgs a, int32_t blocks) {
-    const int32_t rank = blockIdx.x, r = a.desc[4 * rank];
+    typedef Shape<FMT, DK, DV> S;
+    typedef Sums<S::NV, S::CE> State;
+    __shared__ float s_sums[kWaves][State::kFloats];
+    const int32_t group = blockIdx.x, r = a.desc[4 * group];
     if (r < 0) return;
-    const int32_t item = a.desc[4 * rank + 1], h = item / blocks, block = item - h * blocks;
-    const int32_t head0 = h * a.group + block * 16, n_heads = min(16, a.group - block * 16);
-    // the parts: this workgroup's last run, then whole runs of the following ones, then the start of one
-    const int32_t last = a.desc[4 * rank + 2];
-    for (int i = threadIdx.x; i < n_heads * (DV / 4); i += kThreads) {
-        const int n = i / (DV / 4), d = (i - n * (DV / 4)) * 4;
-        float top = -INFINITY, sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int32_t w = rank; w <= last; ++w) {
-            const float *part = a.part + ((int64_t)2 * w + (w == rank ? 1 : 0)) * kPartFloats<DV>;
-            const float m = part[16 * DV + n], up = fmaxf(top, m);
-            const f32x4_t x = *reinterpret_cast<const f32x4_t *>(part + n * DV + d);
-            const float f = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - up), g = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - up);
-            sum = sum * f + part[16 * DV + 16 + n] * g;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = v[e] * f + x[e] * g;
-            top = up;
-        }
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        const int64_t head = (int64_t)r * a.Hq + head0 + n;
-        if (d < a.dv) {
-            if (FMT == CRAFT_KV_F32) {
-                *reinterpret_cast<f32x4_t *>(static_cast<float *>(a.out) + head * a.dv + d) = (f32x4_t){v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
-            } else {
-                const u32x2_t w = {bf16_pair(v[0] * inv, v[1] * inv), bf16_pair(v[2] * inv, v[3] * inv)};
-                *reinterpret_cast<u32x2_t *>(static_cast<unsigned char *>(a.out) + (head * a.dv + d) * 2) = w;
-            }
-        }
-        if (d == 0 && a.lse) a.lse[head] = sum == 0.0f ? -INFINITY : (top + __log2f(sum)) * 0.6931471805599453f;
-    }
+    const int32_t item = a.desc[4 * group + 1], last = a.desc[4 * group + 2];
+    const int32_t h = item / blocks, block = item - h * blocks;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    State z;
+    z.clear();
+    for (int32_t w = group + wave; w <= last; w += kWaves) z.add(a.part + (int64_t)(2 * w + (w == group ? 1 : 0)) * State::kFloats, lane);
+    if (wave > 0) z.put(s_sums[wave], lane);
+    __syncthreads();
+    if (wave > 0) return;
+    for (int w = 1; w < kWaves && group + w <= last; ++w) z.add(s_sums[w], lane);
+    z.template write<FMT == CRAFT_KV_F32>(a, r, h * a.group + block * 16, min(16, a.group - block * 16), lane);
 }
 
 template <int FMT, int DK, int DV, bool AHEAD, int WPS>
@@ -540,7 +626,7 @@ void launch(const AttentionArgs &a, int32_t blocks, hipStream_t s) {
     const dim3 grid((unsigned)a.workers), block(kThreads);
     if (a.shift < 4) hipLaunchKernelGGL((decode_kernel<FMT, DK, DV, true, AHEAD, WPS>), grid, block, 0, s, a, blocks);
     else hipLaunchKernelGGL((decode_kernel<FMT, DK, DV, false, AHEAD, WPS>), grid, block, 0, s, a, blocks);
-    hipLaunchKernelGGL((join_kernel<FMT, DV>), grid, block, 0, s, a, blocks);
+    hipLaunchKernelGGL((join_kernel<FMT, DK, DV>), grid, block, 0, s, a, blocks);
 }
 
 int padded_dim(const AttentionArgs &a) {
@@ -567,7 +653,7 @@ int32_t attention_workers(const AttentionArgs &a, int32_t num_cu) {
 size_t attention_workspace(const AttentionArgs &a, int32_t num_cu) {
     const int dv = padded_dim(a) == 576 ? 512 : padded_dim(a);
     const size_t w = (size_t)attention_workers(a, num_cu);
-    return w * 4 * sizeof(int32_t) + w * 2 * (size_t)(16 * dv + 32) * sizeof(float);
+    return w * 4 * sizeof(int32_t) + w * 2 * (size_t)(16 * dv + 128) * sizeof(float);
 }
 
 hipError_t launch_decode_attention(const AttentionArgs &a, hipStream_t s) {
