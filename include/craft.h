@@ -495,14 +495,18 @@ craft_status craft_kv_append(const craft_kv_cache *cache, int64_t T, const void 
  *   out     DEVICE [R][Hq][dv] contiguous, of q's type, fully overwritten
  *   lse     DEVICE [R][Hq] fp32, optional: log sum_i exp(s[i]), with which parts of a context that
  *           lie elsewhere can be joined
- *   workspace  DEVICE, 16-byte aligned, at least craft_decode_attention_workspace() bytes.  Calls
- *           that share one must be ordered on one stream
+ *   workspace  DEVICE, 16-byte aligned, at least craft_decode_attention_workspace() bytes.  Its first
+ *           CRAFT_ATTENTION_COUNTER_BYTES have to be zero before the first call that uses it; every
+ *           call leaves them at zero.  Calls that share a workspace (of any shapes) must be ordered
+ *           on one stream
  * Scores, maxima, sums and the weighted sum are fp32; the weights exp(s - max) are rounded to bf16
  * in front of the product with 16- and 8-bit values.  The result depends on the arguments only (the
  * order of the sums: on the lengths and on the GPU's number of compute units), never on scheduling.
  * Rows of the pages behind a request's last token may hold anything.
- * Limits: Hq a multiple of heads; R * Hq < 2^31; max_pages * page_size < 2^31.  R may be 0.
+ * Limits: Hq a multiple of heads; R * Hq < 2^31; max_pages * page_size <= 2^30.  R may be 0.
  */
+#define CRAFT_ATTENTION_COUNTER_BYTES (48u << 10)
+
 typedef struct {
     int32_t R, Hq;
     int32_t max_pages, window;

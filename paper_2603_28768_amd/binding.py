@@ -619,7 +619,7 @@ class DecodeAttention:
         a.lse = self.lse.data_ptr() if want_lse else None
         n = c_sz()
         _check(lib().craft_decode_attention_workspace(ctypes.byref(cache.desc), ctypes.byref(a), n), "craft_decode_attention_workspace")
-        self.workspace = torch.empty(n.value, dtype=torch.uint8, device=dev)
+        self.workspace = torch.zeros(n.value, dtype=torch.uint8, device=dev)       # the counters in it start at zero
         a.workspace, a.workspace_bytes = self.workspace.data_ptr(), n.value
         self.args = a
 

@@ -26,7 +26,9 @@
 // itself: the launch does not depend on the lengths (which the host does not know), and long and short requests
 // take equal parts of the GPU.  A wave walks its run alone; what it begins and does not end, or ends and did not
 // begin, meets the neighbouring waves' sums in LDS at the end of the workgroup.  An item cut between workgroups
-// leaves partial sums, which a second launch joins in the order of the workgroups.
+// leaves partial sums in the workspace, and the workgroup that finds by a counter that it is the last of its
+// item's joins them, in the order of the runs whoever it is: a second launch would take longer than a whole call
+// on a few short requests.  Of an item cut into many parts, 16 at a time are joined first.
 #include <algorithm>
 
 #include "ffn_common.h"
@@ -100,14 +102,13 @@ __device__ __forceinline__ float sum_of_head(float x) {
 }
 __device__ __forceinline__ uint32_t perm(uint32_t hi, uint32_t lo, uint32_t sel) { return __builtin_amdgcn_perm(hi, lo, sel); }
 
-__device__ __forceinline__ int32_t units_of(const AttentionArgs &a, int32_t r, int32_t *first, int32_t *len) {
-    const int64_t cap = (int64_t)a.max_pages << a.shift;
-    const int32_t n = (int32_t)min((int64_t)max(a.lens[r], 0), cap);
-    const int32_t lo = a.window > 0 && n > a.window ? n - a.window : 0;
-    *first = lo;
-    *len = n;
+__device__ __forceinline__ int32_t length_of(const AttentionArgs &a, int32_t r) {
+    return min(max(a.lens[r], 0), a.max_pages << a.shift);
+}
+__device__ __forceinline__ int32_t first_of(const AttentionArgs &a, int32_t len) { return a.window > 0 ? max(len - a.window, 0) : 0; }
+__device__ __forceinline__ int32_t units_of(const AttentionArgs &a, int32_t len) {
     // an empty request is one unit without tokens, so that somebody writes its zeros
-    return max(1, (int32_t)(((int64_t)n + kUnit - 1) / kUnit) - lo / kUnit);
+    return max(1, (len + kUnit - 1) / kUnit - first_of(a, len) / kUnit);
 }
 
 // The list of items cut into n runs.  Lengths in units, an item's own cost included.
@@ -126,15 +127,15 @@ struct Runs {
     }
     __device__ __forceinline__ int64_t start(int32_t w) const { return each * w + min(w, more); }
     __device__ __forceinline__ int32_t of(int64_t at) const {      // the run that holds place `at`
-        const int64_t longer = (each + 1) * more;
-        return at < longer ? (int32_t)(at / (each + 1)) : more + (int32_t)((at - longer) / each);
+        const int64_t longer = (each + 1) * more, in = at < longer ? at : at - longer, of = at < longer ? each + 1 : each;
+        return (at < longer ? 0 : more) + (total >> 32 ? (int32_t)(in / of) : (int32_t)((uint32_t)in / (uint32_t)of));
     }
 };
 
 // The request in which each wave's run starts, and the cost in front of it.
 struct Start {
     int64_t before;
-    int32_t request;
+    int32_t request, len;
 };
 // per_request: items of a request (heads x blocks of 16 query heads).
 __device__ __forceinline__ Start find_start(const AttentionArgs &a, int32_t per_request, Runs &runs) {
@@ -144,8 +145,11 @@ __device__ __forceinline__ Start find_start(const AttentionArgs &a, int32_t per_
     const int32_t per = (a.R + kThreads - 1) / kThreads;
     const int64_t r0 = min((int64_t)a.R, (int64_t)tid * per), r1 = min((int64_t)a.R, r0 + per);
     int64_t sum = 0;
-    int32_t lo, len;
-    for (int64_t r = r0; r < r1; ++r) sum += units_of(a, (int32_t)r, &lo, &len) + kItemCost;
+    int32_t len = 0;                               // of the last request: of the only one, up to kThreads requests
+    for (int64_t r = r0; r < r1; ++r) {
+        len = length_of(a, (int32_t)r);
+        sum += units_of(a, len) + kItemCost;
+    }
     sum *= per_request;
     int64_t incl = sum;
 #pragma unroll
@@ -170,20 +174,21 @@ __device__ __forceinline__ Start find_start(const AttentionArgs &a, int32_t per_
             int64_t b = before;
             int32_t r = (int32_t)r0;
             for (;; ++r) {
-                const int64_t u = (int64_t)(units_of(a, r, &lo, &len) + kItemCost) * per_request;
+                if (per > 1) len = length_of(a, r);
+                const int64_t u = (int64_t)(units_of(a, len) + kItemCost) * per_request;
                 if (at < b + u) break;
                 b += u;
             }
-            found[w] = {b, r};
+            found[w] = {b, r, len};
         }
     }
     __syncthreads();
-    return {uniform(found[wave].before), uniform(found[wave].request)};
+    return {uniform(found[wave].before), uniform(found[wave].request), uniform(found[wave].len)};
 }
 
 // Running maximum, sum of weights and weighted sum of some tokens of an item, as a wave holds them: lane (head, g)
 // has the sum of the weights of its own tokens only, the rest is whole.
-template <int NV, int CE> struct Sums {
+template <int NV, int CE, bool F32> struct Sums {
     f32x4_t acc[NV][CE];
     float m, l;
     __device__ __forceinline__ void clear() {
@@ -211,8 +216,33 @@ template <int NV, int CE> struct Sums {
         to[NV * CE * 256 + lane] = m;
         to[NV * CE * 256 + 64 + lane] = l;
     }
+    // The same for other workgroups, which may run on another XCD: stores that go through this one's L2 and loads
+    // that go past theirs (device scope), 16 bytes at a time.  With fences instead, which write back or invalidate
+    // the whole L2 of an XCD, 64 requests of 1 to 16384 tokens took 298 us, not 92.
+    static constexpr int kDevice = 16;
+    static __device__ __forceinline__ __amdgpu_buffer_rsrc_t sums_at(const float *p) { return rows_of(reinterpret_cast<const unsigned char *>(p), kFloats * 4); }
+    __device__ __forceinline__ void put_out(float *to, int lane) const {
+        const __amdgpu_buffer_rsrc_t rs = sums_at(to);
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int e = 0; e < CE; ++e) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, acc[c][e]), rs, (uint32_t)((c * CE + e) * 64 + lane) * 16, 0, kDevice);
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(m), rs, (uint32_t)(NV * CE * 256 + lane) * 4, 0, kDevice);
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(l), rs, (uint32_t)(NV * CE * 256 + 64 + lane) * 4, 0, kDevice);
+    }
+    __device__ __forceinline__ void add_from(const float *from, int lane) {
+        const __amdgpu_buffer_rsrc_t rs = sums_at(from);
+        const float om = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, (uint32_t)(NV * CE * 256 + lane) * 4, 0, kDevice));
+        const float ol = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, (uint32_t)(NV * CE * 256 + 64 + lane) * 4, 0, kDevice));
+        join(om, ol, [&](int c, int e) {
+            return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, (uint32_t)((c * CE + e) * 64 + lane) * 16, 0, kDevice));
+        });
+    }
     __device__ __forceinline__ void add(const float *from, int lane) {
-        const float om = from[NV * CE * 256 + lane], ol = from[NV * CE * 256 + 64 + lane];
+        join(from[NV * CE * 256 + lane], from[NV * CE * 256 + 64 + lane],
+             [&](int c, int e) { return *reinterpret_cast<const f32x4_t *>(from + ((c * CE + e) * 64 + lane) * 4); });
+    }
+    template <typename F> __device__ __forceinline__ void join(float om, float ol, F acc_of) {
         const float up = fmaxf(m, om);
         const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - up), of = om == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(om - up);
         m = up;
@@ -221,13 +251,13 @@ template <int NV, int CE> struct Sums {
         for (int c = 0; c < NV; ++c)
 #pragma unroll
             for (int e = 0; e < CE; ++e) {
-                const f32x4_t x = *reinterpret_cast<const f32x4_t *>(from + ((c * CE + e) * 64 + lane) * 4);
+                const f32x4_t x = acc_of(c, e);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[c][e][i] = acc[c][e][i] * f + x[i] * of;
             }
     }
     // Row i of tile (c, e) is column (c 16 + 4 g + i) CE + e: CE neighbouring columns of the output per (c, i).
-    template <bool F32> __device__ __forceinline__ void write(const AttentionArgs &a, int32_t r, int32_t head0, int32_t n_heads, int lane) const {
+    __device__ __forceinline__ void write(const AttentionArgs &a, int32_t r, int32_t head0, int32_t n_heads, int lane) const {
         const int col = lane & 15, g = lane >> 4;
         const float sum = sum_of_head(l);
         if (col >= n_heads) return;
@@ -239,7 +269,7 @@ template <int NV, int CE> struct Sums {
             for (int i = 0; i < 4; ++i) {
                 const int d = (c * 16 + 4 * g + i) * CE;
                 if (d >= a.dv) continue;
-                if constexpr (F32) {
+                if (F32) {
                     *reinterpret_cast<f32x4_t *>(static_cast<float *>(a.out) + head * a.dv + d) =
                         (f32x4_t){acc[c][0][i] * inv, acc[c][1][i] * inv, acc[c][2][i] * inv, acc[c][3][i] * inv};
                 } else {
@@ -259,47 +289,63 @@ template <int NV, int CE> struct Sums {
     }
 };
 
+// An item in the list, and its request and number there.
+struct Place {
+    int64_t begin, end;
+    int32_t request, item;
+};
+template <int NV, int CE, bool F32>
+__device__ __forceinline__ void write_item(const Sums<NV, CE, F32> &z, const AttentionArgs &a, const Place &p, int32_t blocks, int lane) {
+    const int32_t h = p.item / blocks, block = p.item - h * blocks;
+    z.write(a, p.request, h * a.group + block * 16, min(16, a.group - block * 16), lane);
+}
+
+// An item that several workgroups have parts of, the first of them with its first unit.
+struct Cut {
+    Place item;
+    int32_t mine;
+};
+constexpr int kJoin = 16;                          // parts joined by one workgroup
+constexpr int kCounters = 4096;                    // of a kind: most workgroups of a launch
+
 // Pages of the tokens that a lane reads of a unit.  Pages of 16 tokens and more: one for either tile, the same in
 // every lane.  SMALL pages: of the lane's key row in either tile, and of the tokens whose values it reads, which
 // are those whose scores it holds.  -1: no such token, or no page.
 template <bool SMALL> struct Pages { int32_t tile[2]; };
 template <> struct Pages<true> { int32_t key[2], value[8]; };
 
+// EXACT: rows of DK and DV elements; otherwise of fewer, and what lies behind a row is zeros.
 // WPS: workgroups of a CU that the registers must do for.  AHEAD: the next unit's rows are requested while this
 // one's are worked on (registers for a whole unit); otherwise a piece is requested where it is used.
-template <int FMT, int DK, int DV, bool SMALL, bool AHEAD, int WPS>
+template <int FMT, int DK, int DV, bool SMALL, bool EXACT, bool AHEAD, int WPS>
 __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, int32_t blocks) {
     typedef Shape<FMT, DK, DV> S;
     typedef Words<S::VW> VWords;
-    typedef Sums<S::NV, S::CE> State;
+    typedef Sums<S::NV, S::CE, FMT == CRAFT_KV_F32> State;
     __shared__ float s_sums[kWaves][State::kFloats];   // of the item that a wave's run found begun
     __shared__ int32_t s_found[kWaves];                // whether there is one, and whether it ends in the run
+    __shared__ Cut s_cut[2];
     enum { kNone = 0, kOpen = 1, kEnded = 2 };
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int32_t per_request = a.heads * blocks, rank = blockIdx.x * kWaves + wave;
     Runs runs;
     const Start st = find_start(a, per_request, runs);
-    if (tid == 0) a.desc[4 * blockIdx.x] = -1;
     if ((int32_t)blockIdx.x * kWaves >= runs.n) return;
     int64_t at = 0, end = 0, before = st.before;
     if (rank < runs.n) {
         at = runs.start(rank);
         end = runs.start(rank + 1);
     }
-    int32_t r = st.request;
+    int32_t r = st.request, len = st.len;
     if (lane == 0) s_found[wave] = kNone;
+    if (tid < 2) s_cut[tid].mine = 0;
     State z;
     bool open = false;                             // the run ends inside an item that starts in it
-    int32_t open_item = 0, open_head0 = 0, open_heads = 0;
-    int64_t open_end = 0;
+    Place began = {}, opened = {};                 // the item a run finds begun, the one it leaves open
 
     while (at < end) {
-        int32_t first, len;
-        const int32_t n_units = uniform(units_of(a, r, &first, &len));
-        first = uniform(first);
-        len = uniform(len);
-        const int32_t cost = n_units + kItemCost;
+        const int32_t first = first_of(a, len), n_units = units_of(a, len), cost = n_units + kItemCost;
         const int64_t in_request = at - before;
         const int32_t item = in_request >> 32 ? (int32_t)(in_request / cost) : (int32_t)((uint32_t)in_request / (uint32_t)cost);
         const int64_t item_begin = before + (int64_t)item * cost, item_end = item_begin + cost;
@@ -307,9 +353,14 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
         // an item's own cost comes first
         const int32_t u0 = max(0, (int32_t)(at - item_begin) - kItemCost), u1 = max(0, (int32_t)(stop - item_begin) - kItemCost);
         at = stop;
-        const int64_t item_before = before;
-        const int32_t item_r = r;
-        if (at == item_before + (int64_t)cost * per_request) { before = at; ++r; }
+        const Place here = {item_begin, item_end, r, item};
+        const int32_t n = len;
+        // the next run of items' length travels meanwhile
+        if (at == before + (int64_t)cost * per_request && at < end) {
+            before = at;
+            ++r;
+            len = uniform(length_of(a, r));
+        }
         if (u0 == u1) continue;
         const int32_t h = item / blocks, block = item - h * blocks;
         const int32_t head0 = h * a.group + block * 16, n_heads = min(16, a.group - block * 16);
@@ -320,7 +371,7 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
         {
             const bool live = col < n_heads;
             constexpr int QB = FMT == CRAFT_KV_F32 ? 4 : 2, QE = 16 / QB;     // bytes of an element, elements of a piece
-            const unsigned char *qr = static_cast<const unsigned char *>(a.q) + ((int64_t)item_r * a.q_stride + (int64_t)(head0 + (live ? col : 0)) * a.q_head) * QB;
+            const unsigned char *qr = static_cast<const unsigned char *>(a.q) + ((int64_t)here.request * a.q_stride + (int64_t)(head0 + (live ? col : 0)) * a.q_head) * QB;
             const u32x4_t none = {0u, 0u, 0u, 0u};
 #pragma unroll
             for (int i = 0; i < S::QN; ++i) {
@@ -330,7 +381,7 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
         }
 
         const unsigned char *kh = a.k + h * a.k_head, *vh = a.v + h * a.v_head;
-        const int32_t *table = a.table + (int64_t)item_r * a.table_stride;
+        const int32_t *table = a.table + (int64_t)here.request * a.table_stride;
         const uint32_t k_span = 16u * (uint32_t)a.k_token, v_span = 16u * (uint32_t)a.v_token;
         const uint32_t k_off = (uint32_t)col * (uint32_t)a.k_token + g * 16;
 
@@ -340,41 +391,58 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
         typename VWords::type vr[8][AHEAD ? S::NV : 1];
         f32x4_t ks[2], vs[2], vs_next[2];
 
-        auto page_of = [&](int32_t token) -> int32_t {
-            const int32_t page = token < len ? table[min(token >> a.shift, a.max_pages - 1)] : -1;
-            return (uint32_t)page < (uint64_t)a.pages ? page : -1;
-        };
+        auto checked = [&](int32_t page) -> int32_t { return (uint32_t)page < (uint64_t)a.pages ? page : -1; };
+        auto entry = [&](int32_t i) -> int32_t { return table[min(i, a.max_pages - 1)]; };
+        // a wave holds the next 64 entries of the table, and the 64 behind them
+        int32_t held0 = ((unit_base + u0) * kUnit) >> a.shift;
+        int32_t held = SMALL ? 0 : entry(held0 + lane), behind = SMALL ? 0 : entry(held0 + 64 + lane);
         auto pages_of = [&](int32_t u, bool live) -> Pages<SMALL> {
             Pages<SMALL> pg;
             if constexpr (SMALL) {
 #pragma unroll
-                for (int t = 0; t < 2; ++t) pg.key[t] = live ? page_of(u * kUnit + t * 16 + col) : -1;
+                for (int t = 0; t < 2; ++t) {
+                    const int32_t token = u * kUnit + t * 16 + col;
+                    pg.key[t] = live && token < n ? checked(entry(token >> a.shift)) : -1;
+                }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) pg.value[j] = live ? page_of(u * kUnit + (j >> 2) * 16 + 4 * g + (j & 3)) : -1;
+                for (int j = 0; j < 8; ++j) {
+                    const int32_t token = u * kUnit + (j >> 2) * 16 + 4 * g + (j & 3);
+                    pg.value[j] = live && token < n ? checked(entry(token >> a.shift)) : -1;
+                }
             } else {
 #pragma unroll
-                for (int t = 0; t < 2; ++t) pg.tile[t] = live ? __builtin_amdgcn_readfirstlane(page_of(u * kUnit + t * 16)) : -1;
+                for (int t = 0; t < 2; ++t) {
+                    const int32_t token = u * kUnit + t * 16;
+                    int32_t i = (token >> a.shift) - held0;
+                    if (i >= 64) {
+                        held0 += 64;
+                        i -= 64;
+                        held = behind;
+                        behind = entry(held0 + 64 + lane);
+                    }
+                    const int32_t page = checked(__builtin_amdgcn_readlane(held, i & 63));
+                    pg.tile[t] = live && token < n ? page : -1;
+                }
             }
             return pg;
         };
         const int32_t in_page = (1 << a.shift) - 1;
         auto load_key = [&](int32_t u, const Pages<SMALL> &pg, int t, int i) __attribute__((always_inline)) -> u32x4_t {
             const int32_t token = u * kUnit + t * 16;
-            const bool inside = (i * 4 + g) * Format<FMT>::kPiece < a.dk;
+            const bool inside = EXACT || (i * 4 + g) * Format<FMT>::kPiece < a.dk;
             if constexpr (SMALL) {
                 const u32x4_t none = {0u, 0u, 0u, 0u};
                 const unsigned char *row = kh + pg.key[t] * a.k_page + ((token + col) & in_page) * a.k_token;
                 return inside && pg.key[t] >= 0 ? *reinterpret_cast<const u32x4_t *>(row + i * 64 + g * 16) : none;
             } else {
-                const bool good = pg.tile[t] >= 0;
-                const __amdgpu_buffer_rsrc_t rs = rows_of(kh + (good ? pg.tile[t] * a.k_page + (token & in_page) * a.k_token : 0), good ? k_span : 0u);
+                const __amdgpu_buffer_rsrc_t rs = rows_of(kh + max(pg.tile[t], 0) * a.k_page + (token & in_page) * a.k_token, pg.tile[t] >= 0 ? k_span : 0u);
                 return __builtin_amdgcn_raw_buffer_load_b128(rs, (inside ? k_off : kFar) + i * 64, 0, 0);
             }
         };
         // rows behind the last token (and in front of the window) may hold anything: read as zeros
         auto load_value = [&](int32_t u, const Pages<SMALL> &pg, bool whole, int t, int j, int c) __attribute__((always_inline)) -> typename VWords::type {
             const int32_t token = u * kUnit + t * 16, row = 4 * g + j;
-            const bool inside = (whole || (token + row >= first && token + row < len)) && (c * 16 + col) * S::CE < a.dv;
+            const bool inside = (whole || (token + row >= first && token + row < n)) && (EXACT || (c * 16 + col) * S::CE < a.dv);
             if constexpr (SMALL) {
                 const int32_t page = pg.value[4 * t + j];
                 typename VWords::type x = {};
@@ -382,8 +450,7 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
                     x = *reinterpret_cast<const typename VWords::type *>(vh + page * a.v_page + ((token + row) & in_page) * a.v_token + (c * 16 + col) * (S::CE * S::B));
                 return x;
             } else {
-                const bool good = pg.tile[t] >= 0;
-                const __amdgpu_buffer_rsrc_t rs = rows_of(vh + (good ? pg.tile[t] * a.v_page + (token & in_page) * a.v_token : 0), good ? v_span : 0u);
+                const __amdgpu_buffer_rsrc_t rs = rows_of(vh + max(pg.tile[t], 0) * a.v_page + (token & in_page) * a.v_token, pg.tile[t] >= 0 ? v_span : 0u);
                 return VWords::load(rs, inside ? (uint32_t)row * (uint32_t)a.v_token + (c * 16 + col) * (S::CE * S::B) : kFar);
             }
         };
@@ -400,12 +467,12 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
                         vs_next[t][j] = page >= 0 ? a.v_scale[so] : 0.0f;
                     }
                 } else {
-                    const bool good = pg.tile[t] >= 0;
-                    const int64_t so = good ? (((int64_t)pg.tile[t] * a.heads + h) << a.shift) + (token & in_page) : 0;
+                    const uint32_t span = pg.tile[t] >= 0 ? 64u : 0u;
+                    const int64_t so = (((int64_t)max(pg.tile[t], 0) * a.heads + h) << a.shift) + (token & in_page);
                     ks[t] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
-                        rows_of(reinterpret_cast<const unsigned char *>(a.k_scale + so), good ? 64u : 0u), g * 16, 0, 0));
+                        rows_of(reinterpret_cast<const unsigned char *>(a.k_scale + so), span), g * 16, 0, 0));
                     vs_next[t] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
-                        rows_of(reinterpret_cast<const unsigned char *>(a.v_scale + so), good ? 64u : 0u), g * 16, 0, 0));
+                        rows_of(reinterpret_cast<const unsigned char *>(a.v_scale + so), span), g * 16, 0, 0));
                 }
             }
         };
@@ -418,25 +485,25 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
             }
             if (FMT == CRAFT_KV_E4M3) load_scales(u, pg);
         };
-        auto all_seen = [&](int32_t u) { return u * kUnit >= first && u * kUnit + kUnit <= len; };
+        auto all_seen = [&](int32_t u) { return u * kUnit >= first && u * kUnit + kUnit <= n; };
         auto load_values = [&](int32_t u, const Pages<SMALL> &pg) __attribute__((always_inline)) {
             if constexpr (AHEAD) {
-                const bool whole = all_seen(u);
+                auto load = [&](bool whole) __attribute__((always_inline)) {
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                    for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                        for (int j = 0; j < 4; ++j)
 #pragma unroll
-                        for (int c = 0; c < S::NV; ++c) vr[4 * t + j][c] = load_value(u, pg, whole, t, j, c);
+                            for (int c = 0; c < S::NV; ++c) vr[4 * t + j][c] = load_value(u, pg, whole, t, j, c);
+                };
+                if (all_seen(u)) load(true);
+                else load(false);
             }
         };
 
-        Pages<SMALL> pages = {};
-        if (u0 < u1) {
-            pages = pages_of(unit_base + u0, true);
-            load_keys(unit_base + u0, pages);
-            load_values(unit_base + u0, pages);
-        }
+        Pages<SMALL> pages = pages_of(unit_base + u0, true);
+        load_keys(unit_base + u0, pages);
+        load_values(unit_base + u0, pages);
         for (int32_t i = u0; i < u1; ++i) {
             const int32_t u = unit_base + i;
             const bool more = i + 1 < u1;
@@ -488,7 +555,7 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int32_t token = u * kUnit + t * 16 + 4 * g + j;
-                        if (token < first || token >= len || !there[4 * t + j]) {
+                        if (token < first || token >= n || !there[4 * t + j]) {
                             x[t][j] = -INFINITY;
                             if (FMT == CRAFT_KV_E4M3) vs[t][j] = 0.0f;      // the scale of a row never written
                         }
@@ -554,22 +621,19 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
 
         if (u0 > 0) {
             z.put(s_sums[wave], lane);
+            began = here;
             if (lane == 0) s_found[wave] = u1 == n_units ? kEnded : kOpen;
         } else if (u1 == n_units) {
-            z.template write<FMT == CRAFT_KV_F32>(a, item_r, head0, n_heads, lane);
+            write_item(z, a, here, blocks, lane);
         } else {
             open = true;
-            open_item = item;
-            open_head0 = head0;
-            open_heads = n_heads;
-            open_end = item_end;
-            r = item_r;
+            opened = here;
         }
     }
 
     // ---- the waves meet: whoever began an item adds what the following waves found of it
     __syncthreads();
-    float *part = a.part + (int64_t)2 * blockIdx.x * State::kFloats;
+    auto part_of = [&](int32_t group, bool begins) { return a.part + (int64_t)(2 * group + (begins ? 1 : 0)) * State::kFloats; };
     if (open) {
         bool ended = false;
         for (int w = wave + 1; w < kWaves && !ended; ++w) {
@@ -577,15 +641,10 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
             ended = s_found[w] == kEnded;
         }
         if (ended) {
-            z.template write<FMT == CRAFT_KV_F32>(a, r, open_head0, open_heads, lane);
+            write_item(z, a, opened, blocks, lane);
         } else {
-            z.put(part + State::kFloats, lane);
-            if (lane == 0) {
-                // joined by the workgroup of the same number in the second launch
-                a.desc[4 * blockIdx.x] = r;
-                a.desc[4 * blockIdx.x + 1] = open_item;
-                a.desc[4 * blockIdx.x + 2] = runs.of(open_end - 1) / kWaves;
-            }
+            z.put_out(part_of(blockIdx.x, true), lane);
+            if (lane == 0) s_cut[0] = {opened, 1};
         }
     }
     // the item that an earlier workgroup began
@@ -595,38 +654,60 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
             z.add(s_sums[w], lane);
             if (s_found[w] == kEnded) break;
         }
-        z.put(part, lane);
+        z.put_out(part_of(blockIdx.x, false), lane);
+        if (lane == 0) s_cut[1] = {began, 1};
     }
-}
-
-// Joins the parts of an item that starts in workgroup blockIdx.x of the first launch and ends in a later one: that
-// one's last sums and the first ones of those that follow.
-template <int FMT, int DK, int DV>
-__global__ __launch_bounds__(kThreads) void join_kernel(AttentionArgs a, int32_t blocks) {
-    typedef Shape<FMT, DK, DV> S;
-    typedef Sums<S::NV, S::CE> State;
-    __shared__ float s_sums[kWaves][State::kFloats];
-    const int32_t group = blockIdx.x, r = a.desc[4 * group];
-    if (r < 0) return;
-    const int32_t item = a.desc[4 * group + 1], last = a.desc[4 * group + 2];
-    const int32_t h = item / blocks, block = item - h * blocks;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    State z;
-    z.clear();
-    for (int32_t w = group + wave; w <= last; w += kWaves) z.add(a.part + (int64_t)(2 * w + (w == group ? 1 : 0)) * State::kFloats, lane);
-    if (wave > 0) z.put(s_sums[wave], lane);
     __syncthreads();
-    if (wave > 0) return;
-    for (int w = 1; w < kWaves && group + w <= last; ++w) z.add(s_sums[w], lane);
-    z.template write<FMT == CRAFT_KV_F32>(a, r, h * a.group + block * 16, min(16, a.group - block * 16), lane);
+    if (!s_cut[0].mine && !s_cut[1].mine) return;
+
+    // ---- joins of items cut between workgroups.  Counters: parts of a group of 16 that have arrived, by the
+    // number of the group's first workgroup (as the item's first one, or as a later one), and groups, by that of
+    // the item's first.  The last to arrive leaves a counter as it was found, at zero.
+    __shared__ int32_t s_last;
+    for (int i = 0; i < 2; ++i) {
+        if (!s_cut[i].mine) continue;
+        const Place cut = s_cut[i].item;
+        const int32_t first = runs.of(uniform(cut.begin) + kItemCost) / kWaves, last = runs.of(uniform(cut.end) - 1) / kWaves;
+        const int32_t number = ((int32_t)blockIdx.x - first) / kJoin, lead = first + number * kJoin;
+        const int32_t stop = min(lead + kJoin, last + 1), groups = (last - first) / kJoin + 1;
+        // one lane arrives for the workgroup, when the stores of all of it have been made
+        auto last_of = [&](int32_t *counter, int32_t of) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (tid == 0) {
+                s_last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == of - 1;
+                if (s_last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            __syncthreads();
+            return s_last != 0;
+        };
+        // the sums of parts lo, lo + step, .. below hi, in the first wave
+        auto join = [&](int32_t lo, int32_t hi, int32_t step) {
+            z.clear();
+            for (int32_t w = lo + wave * step; w < hi; w += kWaves * step) z.add_from(part_of(w, w == first), lane);
+            if (wave > 0) z.put(s_sums[wave], lane);
+            __syncthreads();
+            if (wave == 0)
+                for (int w = 1; w < kWaves && lo + w * step < hi; ++w) z.add(s_sums[w], lane);
+            __syncthreads();
+        };
+        if (!last_of(a.counters + (number ? kCounters : 0) + lead, stop - lead)) continue;
+        join(lead, stop, 1);
+        if (groups > 1) {
+            if (wave == 0) z.put_out(part_of(lead, number == 0), lane);
+            if (!last_of(a.counters + 2 * kCounters + first, groups)) continue;
+            join(first, last + 1, kJoin);
+        }
+        if (wave == 0) write_item(z, a, cut, blocks, lane);
+    }
 }
 
 template <int FMT, int DK, int DV, bool AHEAD, int WPS>
 void launch(const AttentionArgs &a, int32_t blocks, hipStream_t s) {
     const dim3 grid((unsigned)a.workers), block(kThreads);
-    if (a.shift < 4) hipLaunchKernelGGL((decode_kernel<FMT, DK, DV, true, AHEAD, WPS>), grid, block, 0, s, a, blocks);
-    else hipLaunchKernelGGL((decode_kernel<FMT, DK, DV, false, AHEAD, WPS>), grid, block, 0, s, a, blocks);
-    hipLaunchKernelGGL((join_kernel<FMT, DK, DV>), grid, block, 0, s, a, blocks);
+    if (a.shift < 4) hipLaunchKernelGGL((decode_kernel<FMT, DK, DV, true, false, AHEAD, WPS>), grid, block, 0, s, a, blocks);
+    else if (a.dk == DK && a.dv == DV) hipLaunchKernelGGL((decode_kernel<FMT, DK, DV, false, true, AHEAD, WPS>), grid, block, 0, s, a, blocks);
+    else hipLaunchKernelGGL((decode_kernel<FMT, DK, DV, false, false, AHEAD, WPS>), grid, block, 0, s, a, blocks);
 }
 
 int padded_dim(const AttentionArgs &a) {
@@ -647,13 +728,14 @@ void launch_format(const AttentionArgs &a, int32_t blocks, hipStream_t s) {
 }  // namespace
 
 int32_t attention_workers(const AttentionArgs &a, int32_t num_cu) {
-    return (padded_dim(a) == 576 ? 1 : 2) * num_cu;
+    return std::min(kCounters, (padded_dim(a) == 576 ? 1 : 2) * num_cu);
 }
+
+size_t attention_counters_bytes() { return 3 * kCounters * sizeof(int32_t); }
 
 size_t attention_workspace(const AttentionArgs &a, int32_t num_cu) {
     const int dv = padded_dim(a) == 576 ? 512 : padded_dim(a);
-    const size_t w = (size_t)attention_workers(a, num_cu);
-    return w * 4 * sizeof(int32_t) + w * 2 * (size_t)(16 * dv + 128) * sizeof(float);
+    return attention_counters_bytes() + (size_t)attention_workers(a, num_cu) * 2 * (size_t)(16 * dv + 128) * sizeof(float);
 }
 
 hipError_t launch_decode_attention(const AttentionArgs &a, hipStream_t s) {

@@ -313,12 +313,13 @@ struct AttentionArgs {
     int64_t pages;
     void *out;
     float *lse;
-    float *part;                   // workspace
-    int32_t *desc;
+    int32_t *counters;             // workspace: zero between calls
+    float *part;                   // behind them
     int32_t workers;
 };
 // Workgroups a launch may have, whatever the lengths; the workspace is sized for them.
 int32_t attention_workers(const AttentionArgs &a, int32_t num_cu);
+size_t attention_counters_bytes();
 size_t attention_workspace(const AttentionArgs &a, int32_t num_cu);
 hipError_t launch_decode_attention(const AttentionArgs &a, hipStream_t s);
 

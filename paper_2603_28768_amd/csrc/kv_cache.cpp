@@ -74,7 +74,8 @@ craft_status attention_args(const craft_kv_cache *c, const craft_attention_args 
     const craft_status st = view_of(c, &w);
     if (st != CRAFT_OK) return st;
     if (!a || a->R < 0 || a->Hq <= 0 || a->Hq % c->heads || (int64_t)a->R * a->Hq >= kInts) return CRAFT_EINVAL;
-    if (a->max_pages <= 0 || (int64_t)a->max_pages * c->page_size >= kInts || a->window < 0) return CRAFT_EINVAL;
+    // twice the longest request is still a 32-bit number
+    if (a->max_pages <= 0 || (int64_t)a->max_pages * c->page_size > kInts / 2 || a->window < 0) return CRAFT_EINVAL;
     AttentionArgs o{};
     o.format = c->format;
     o.R = a->R;
@@ -215,8 +216,8 @@ craft_status craft_decode_attention(const craft_kv_cache *cache, const craft_att
     a.out = args->out;
     a.lse = args->lse;
     a.workers = attention_workers(a, cus);
-    a.desc = static_cast<int32_t *>(args->workspace);
-    a.part = reinterpret_cast<float *>(a.desc + 4 * (size_t)a.workers);
+    a.counters = static_cast<int32_t *>(args->workspace);
+    a.part = reinterpret_cast<float *>(static_cast<unsigned char *>(args->workspace) + attention_counters_bytes());
     return launch_decode_attention(a, static_cast<hipStream_t>(stream)) == hipSuccess ? CRAFT_OK : CRAFT_EHIP;
 }
 

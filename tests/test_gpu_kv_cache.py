@@ -11,6 +11,7 @@ import kv_reference as ref
 pytestmark = pytest.mark.gpu
 
 DEV = "cuda:0"
+COUNTERS = 48 << 10         # bytes of an attention workspace that are zero between calls
 
 
 # ------------------------------------------------------------------------ tables
@@ -224,7 +225,7 @@ class Setup:
         c = self.cache
         q = self.q if q is None else q
         self.attn = binding.DecodeAttention(c, q.shape[0], q.shape[1], self.table.shape[1], scale=self.scale, window=window, want_lse=want_lse)
-        self.attn.workspace.fill_(0xff)                 # whatever was left there
+        self.attn.workspace[COUNTERS:] = 0xff           # whatever was left there
         self.attn.out.fill_(float("nan"))
         return self.attn(q, self.d_lens, self.d_table)
 
@@ -236,6 +237,7 @@ class Setup:
 def _check(torch, s, window=0):
     out = s.call(window)
     torch.cuda.synchronize()
+    assert not bool(s.attn.workspace[:COUNTERS].any())
     want, lse, bound, lse_bound = s.want(window)
     err = (out.double().cpu() - want).abs()
     assert torch.isfinite(out.float()).all()
