@@ -31,282 +31,21 @@
 // on a few short requests.  Of an item cut into many parts, 16 at a time are joined first.
 #include <algorithm>
 
-#include "ffn_common.h"
+#include "attention_common.h"
 
 namespace craft {
 namespace {
 
-typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
-
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
-constexpr int kUnit = 32;                          // tokens
 constexpr int kItemCost = 2;                       // what an item costs beside its units
-constexpr int kMinRun = 4;                         // of a wave, where there is little to do
-constexpr uint32_t kFar = 0x80000000u;             // an offset behind the end of every page: reads as zeros
+constexpr int kMinRun = 2;                         // of a wave, where there is little to do
 
-// Elements of 16 bytes, of the widest value load of a lane, and what the products take.
-template <int FMT> struct Format;
-template <> struct Format<CRAFT_KV_F32> { static constexpr int kBytes = 4, kPiece = 4; };
-template <> struct Format<CRAFT_KV_BF16> { static constexpr int kBytes = 2, kPiece = 8; };
-template <> struct Format<CRAFT_KV_E4M3> { static constexpr int kBytes = 1, kPiece = 16; };
-
-template <int FMT, int DK, int DV> struct Shape {
-    static constexpr int B = Format<FMT>::kBytes;
-    static constexpr int NK = DK * B / 64;                          // 16-byte key pieces of a lane per tile
-    static constexpr int CE = DV / 16 < Format<FMT>::kPiece ? DV / 16 : Format<FMT>::kPiece;   // elements of a value load
-    static constexpr int NV = DV / 16 / CE;                         // value loads of a lane per token
-    static constexpr int VW = CE * B / 4;                           // words of one
-    static constexpr int QN = FMT == CRAFT_KV_E4M3 ? 2 * NK : NK;   // 16-byte pieces of the queries
-};
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const unsigned char *p, uint32_t bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(p), 0, bytes, 0x00027000);
-}
-template <int W> struct Words;
-template <> struct Words<4> {
-    typedef u32x4_t type;
-    static __device__ __forceinline__ type load(__amdgpu_buffer_rsrc_t r, uint32_t off) { return __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0); }
-};
-template <> struct Words<2> {
-    typedef u32x2_t type;
-    static __device__ __forceinline__ type load(__amdgpu_buffer_rsrc_t r, uint32_t off) { return __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0); }
-};
-template <> struct Words<1> {
-    typedef uint32_t type;
-    static __device__ __forceinline__ type load(__amdgpu_buffer_rsrc_t r, uint32_t off) { return __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0); }
-};
-template <int W> __device__ __forceinline__ uint32_t word(const typename Words<W>::type &x, int i) { return x[i]; }
-template <> __device__ __forceinline__ uint32_t word<1>(const uint32_t &x, int) { return x; }
-
-// The same in every lane of the wave: kept in scalar registers.
-__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-    return (int64_t)((uint64_t)(uint32_t)uniform((int32_t)(x >> 32)) << 32 | (uint32_t)uniform((int32_t)x));
-}
-
-// Reductions over the four lanes that hold a head (lane & 15): lanes 16 and 32 apart change places.
-__device__ __forceinline__ float other16(float x) {
-    return __shfl_xor(x, 16, 64);
-}
-__device__ __forceinline__ float other32(float x) {
-    return __shfl_xor(x, 32, 64);
-}
-__device__ __forceinline__ float max_of_head(float x) {
-    x = fmaxf(x, other16(x));
-    return fmaxf(x, other32(x));
-}
-__device__ __forceinline__ float sum_of_head(float x) {
-    x += other16(x);
-    return x + other32(x);
-}
-__device__ __forceinline__ uint32_t perm(uint32_t hi, uint32_t lo, uint32_t sel) { return __builtin_amdgcn_perm(hi, lo, sel); }
-
-__device__ __forceinline__ int32_t length_of(const AttentionArgs &a, int32_t r) {
-    return min(max(a.lens[r], 0), a.max_pages << a.shift);
-}
-__device__ __forceinline__ int32_t first_of(const AttentionArgs &a, int32_t len) { return a.window > 0 ? max(len - a.window, 0) : 0; }
-__device__ __forceinline__ int32_t units_of(const AttentionArgs &a, int32_t len) {
-    // an empty request is one unit without tokens, so that somebody writes its zeros
-    return max(1, (len + kUnit - 1) / kUnit - first_of(a, len) / kUnit);
-}
-
-// The list of items cut into n runs.  Lengths in units, an item's own cost included.
-struct Runs {
-    int64_t total, each;   // the first `more` runs are one longer than `each`
-    int32_t n, more;
-    __device__ __forceinline__ void cut(int64_t t, int32_t most) {
-        total = t;
-        n = (int32_t)min((int64_t)most, (t + kMinRun - 1) / kMinRun);
-        if (t >> 32) {
-            each = t / n;
-        } else {
-            each = (uint32_t)t / (uint32_t)n;
-        }
-        more = (int32_t)(t - each * n);
-    }
-    __device__ __forceinline__ int64_t start(int32_t w) const { return each * w + min(w, more); }
-    __device__ __forceinline__ int32_t of(int64_t at) const {      // the run that holds place `at`
-        const int64_t longer = (each + 1) * more, in = at < longer ? at : at - longer, of = at < longer ? each + 1 : each;
-        return (at < longer ? 0 : more) + (total >> 32 ? (int32_t)(in / of) : (int32_t)((uint32_t)in / (uint32_t)of));
-    }
-};
-
-// The request in which each wave's run starts, and the cost in front of it.
-struct Start {
-    int64_t before;
-    int32_t request, len;
-};
-// per_request: items of a request (heads x blocks of 16 query heads).
-__device__ __forceinline__ Start find_start(const AttentionArgs &a, int32_t per_request, Runs &runs) {
-    __shared__ int64_t wave_sum[kWaves];
-    __shared__ Start found[kWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int32_t per = (a.R + kThreads - 1) / kThreads;
-    const int64_t r0 = min((int64_t)a.R, (int64_t)tid * per), r1 = min((int64_t)a.R, r0 + per);
-    int64_t sum = 0;
-    int32_t len = 0;                               // of the last request: of the only one, up to kThreads requests
-    for (int64_t r = r0; r < r1; ++r) {
-        len = length_of(a, (int32_t)r);
-        sum += units_of(a, len) + kItemCost;
-    }
-    sum *= per_request;
-    int64_t incl = sum;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t up = __shfl_up(incl, d, 64);
-        if (lane >= d) incl += up;
-    }
-    if (lane == 63) wave_sum[wave] = incl;
-    __syncthreads();
-    int64_t before = incl - sum, total = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) before += wave_sum[w];
-        total += wave_sum[w];
-    }
-    runs.cut(uniform(total), a.workers * kWaves);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        const int32_t rank = blockIdx.x * kWaves + w;
-        const int64_t at = runs.start(rank);
-        if (rank < runs.n && at >= before && at < before + sum) {
-            int64_t b = before;
-            int32_t r = (int32_t)r0;
-            for (;; ++r) {
-                if (per > 1) len = length_of(a, r);
-                const int64_t u = (int64_t)(units_of(a, len) + kItemCost) * per_request;
-                if (at < b + u) break;
-                b += u;
-            }
-            found[w] = {b, r, len};
-        }
-    }
-    __syncthreads();
-    return {uniform(found[wave].before), uniform(found[wave].request), uniform(found[wave].len)};
-}
-
-// Running maximum, sum of weights and weighted sum of some tokens of an item, as a wave holds them: lane (head, g)
-// has the sum of the weights of its own tokens only, the rest is whole.
-template <int NV, int CE, bool F32> struct Sums {
-    f32x4_t acc[NV][CE];
-    float m, l;
-    __device__ __forceinline__ void clear() {
-        m = -INFINITY;
-        l = 0.0f;
-#pragma unroll
-        for (int c = 0; c < NV; ++c)
-#pragma unroll
-            for (int e = 0; e < CE; ++e) acc[c][e] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    __device__ __forceinline__ void scale(float f) {
-        l *= f;
-#pragma unroll
-        for (int c = 0; c < NV; ++c)
-#pragma unroll
-            for (int e = 0; e < CE; ++e) acc[c][e] *= f;
-    }
-    // Sums in memory: the accumulators, then m, then l, lane by lane.
-    static constexpr int kFloats = (NV * CE * 4 + 2) * 64;
-    __device__ __forceinline__ void put(float *to, int lane) const {
-#pragma unroll
-        for (int c = 0; c < NV; ++c)
-#pragma unroll
-            for (int e = 0; e < CE; ++e) *reinterpret_cast<f32x4_t *>(to + ((c * CE + e) * 64 + lane) * 4) = acc[c][e];
-        to[NV * CE * 256 + lane] = m;
-        to[NV * CE * 256 + 64 + lane] = l;
-    }
-    // The same for other workgroups, which may run on another XCD: stores that go through this one's L2 and loads
-    // that go past theirs (device scope), 16 bytes at a time.  With fences instead, which write back or invalidate
-    // the whole L2 of an XCD, 64 requests of 1 to 16384 tokens took 298 us, not 92.
-    static constexpr int kDevice = 16;
-    static __device__ __forceinline__ __amdgpu_buffer_rsrc_t sums_at(const float *p) { return rows_of(reinterpret_cast<const unsigned char *>(p), kFloats * 4); }
-    __device__ __forceinline__ void put_out(float *to, int lane) const {
-        const __amdgpu_buffer_rsrc_t rs = sums_at(to);
-#pragma unroll
-        for (int c = 0; c < NV; ++c)
-#pragma unroll
-            for (int e = 0; e < CE; ++e) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, acc[c][e]), rs, (uint32_t)((c * CE + e) * 64 + lane) * 16, 0, kDevice);
-        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(m), rs, (uint32_t)(NV * CE * 256 + lane) * 4, 0, kDevice);
-        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(l), rs, (uint32_t)(NV * CE * 256 + 64 + lane) * 4, 0, kDevice);
-    }
-    __device__ __forceinline__ void add_from(const float *from, int lane) {
-        const __amdgpu_buffer_rsrc_t rs = sums_at(from);
-        const float om = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, (uint32_t)(NV * CE * 256 + lane) * 4, 0, kDevice));
-        const float ol = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, (uint32_t)(NV * CE * 256 + 64 + lane) * 4, 0, kDevice));
-        join(om, ol, [&](int c, int e) {
-            return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, (uint32_t)((c * CE + e) * 64 + lane) * 16, 0, kDevice));
-        });
-    }
-    __device__ __forceinline__ void add(const float *from, int lane) {
-        join(from[NV * CE * 256 + lane], from[NV * CE * 256 + 64 + lane],
-             [&](int c, int e) { return *reinterpret_cast<const f32x4_t *>(from + ((c * CE + e) * 64 + lane) * 4); });
-    }
-    template <typename F> __device__ __forceinline__ void join(float om, float ol, F acc_of) {
-        const float up = fmaxf(m, om);
-        const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - up), of = om == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(om - up);
-        m = up;
-        l = l * f + ol * of;
-#pragma unroll
-        for (int c = 0; c < NV; ++c)
-#pragma unroll
-            for (int e = 0; e < CE; ++e) {
-                const f32x4_t x = acc_of(c, e);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[c][e][i] = acc[c][e][i] * f + x[i] * of;
-            }
-    }
-    // Row i of tile (c, e) is column (c 16 + 4 g + i) CE + e: CE neighbouring columns of the output per (c, i).
-    __device__ __forceinline__ void write(const AttentionArgs &a, int32_t r, int32_t head0, int32_t n_heads, int lane) const {
-        const int col = lane & 15, g = lane >> 4;
-        const float sum = sum_of_head(l);
-        if (col >= n_heads) return;
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        const int64_t head = (int64_t)r * a.Hq + head0 + col;
-#pragma unroll
-        for (int c = 0; c < NV; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int d = (c * 16 + 4 * g + i) * CE;
-                if (d >= a.dv) continue;
-                if (F32) {
-                    *reinterpret_cast<f32x4_t *>(static_cast<float *>(a.out) + head * a.dv + d) =
-                        (f32x4_t){acc[c][0][i] * inv, acc[c][1][i] * inv, acc[c][2][i] * inv, acc[c][3][i] * inv};
-                } else {
-                    uint32_t w[CE / 2];
-#pragma unroll
-                    for (int e = 0; e < CE / 2; ++e) w[e] = bf16_pair(acc[c][2 * e][i] * inv, acc[c][2 * e + 1][i] * inv);
-                    unsigned char *to = static_cast<unsigned char *>(a.out) + (head * a.dv + d) * 2;
-                    if constexpr (CE == 4) {
-                        *reinterpret_cast<u32x2_t *>(to) = (u32x2_t){w[0], w[1]};
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < CE / 8; ++e) *reinterpret_cast<u32x4_t *>(to + 16 * e) = (u32x4_t){w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]};
-                    }
-                }
-            }
-        if (g == 0 && a.lse) a.lse[head] = sum == 0.0f ? -INFINITY : (m + __log2f(sum)) * 0.6931471805599453f;
-    }
-};
-
-// An item in the list, and its request and number there.
-struct Place {
-    int64_t begin, end;
-    int32_t request, item;
-};
 template <int NV, int CE, bool F32>
 __device__ __forceinline__ void write_item(const Sums<NV, CE, F32> &z, const AttentionArgs &a, const Place &p, int32_t blocks, int lane) {
     const int32_t h = p.item / blocks, block = p.item - h * blocks;
     z.write(a, p.request, h * a.group + block * 16, min(16, a.group - block * 16), lane);
 }
-
-// An item that several workgroups have parts of, the first of them with its first unit.
-struct Cut {
-    Place item;
-    int32_t mine;
-};
-constexpr int kJoin = 16;                          // parts joined by one workgroup
-constexpr int kCounters = 4096;                    // of a kind: most workgroups of a launch
 
 // Pages of the tokens that a lane reads of a unit.  Pages of 16 tokens and more: one for either tile, the same in
 // every lane.  SMALL pages: of the lane's key row in either tile, and of the tokens whose values it reads, which
@@ -314,10 +53,9 @@ constexpr int kCounters = 4096;                    // of a kind: most workgroups
 template <bool SMALL> struct Pages { int32_t tile[2]; };
 template <> struct Pages<true> { int32_t key[2], value[8]; };
 
-// EXACT: rows of DK and DV elements; otherwise of fewer, and what lies behind a row is zeros.
 // WPS: workgroups of a CU that the registers must do for.  AHEAD: the next unit's rows are requested while this
 // one's are worked on (registers for a whole unit); otherwise a piece is requested where it is used.
-template <int FMT, int DK, int DV, bool SMALL, bool EXACT, bool AHEAD, int WPS>
+template <int FMT, int DK, int DV, bool SMALL, bool AHEAD, int WPS>
 __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, int32_t blocks) {
     typedef Shape<FMT, DK, DV> S;
     typedef Words<S::VW> VWords;
@@ -330,7 +68,7 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
     const int col = lane & 15, g = lane >> 4;
     const int32_t per_request = a.heads * blocks, rank = blockIdx.x * kWaves + wave;
     Runs runs;
-    const Start st = find_start(a, per_request, runs);
+    const Start st = find_start<kWaves, kWaves>(a, per_request, kItemCost, a.workers * kWaves, kMinRun, blockIdx.x * kWaves, runs);
     if ((int32_t)blockIdx.x * kWaves >= runs.n) return;
     int64_t at = 0, end = 0, before = st.before;
     if (rank < runs.n) {
@@ -429,7 +167,7 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
         const int32_t in_page = (1 << a.shift) - 1;
         auto load_key = [&](int32_t u, const Pages<SMALL> &pg, int t, int i) __attribute__((always_inline)) -> u32x4_t {
             const int32_t token = u * kUnit + t * 16;
-            const bool inside = EXACT || (i * 4 + g) * Format<FMT>::kPiece < a.dk;
+            const bool inside = (i * 4 + g) * Format<FMT>::kPiece < a.dk;
             if constexpr (SMALL) {
                 const u32x4_t none = {0u, 0u, 0u, 0u};
                 const unsigned char *row = kh + pg.key[t] * a.k_page + ((token + col) & in_page) * a.k_token;
@@ -442,7 +180,7 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
         // rows behind the last token (and in front of the window) may hold anything: read as zeros
         auto load_value = [&](int32_t u, const Pages<SMALL> &pg, bool whole, int t, int j, int c) __attribute__((always_inline)) -> typename VWords::type {
             const int32_t token = u * kUnit + t * 16, row = 4 * g + j;
-            const bool inside = (whole || (token + row >= first && token + row < n)) && (EXACT || (c * 16 + col) * S::CE < a.dv);
+            const bool inside = (whole || (token + row >= first && token + row < n)) && (c * 16 + col) * S::CE < a.dv;
             if constexpr (SMALL) {
                 const int32_t page = pg.value[4 * t + j];
                 typename VWords::type x = {};
@@ -563,12 +301,7 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
             }
             float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
             top = max_of_head(top);
-            if (__any(top > z.m)) {
-                const float up = fmaxf(z.m, top);
-                z.scale(up == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(z.m - up));
-                z.m = up;
-            }
-            const float base = z.m == -INFINITY ? 0.0f : z.m;
+            const float base = z.raise(top);
             float p[2][4];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -670,17 +403,6 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
         const int32_t first = runs.of(uniform(cut.begin) + kItemCost) / kWaves, last = runs.of(uniform(cut.end) - 1) / kWaves;
         const int32_t number = ((int32_t)blockIdx.x - first) / kJoin, lead = first + number * kJoin;
         const int32_t stop = min(lead + kJoin, last + 1), groups = (last - first) / kJoin + 1;
-        // one lane arrives for the workgroup, when the stores of all of it have been made
-        auto last_of = [&](int32_t *counter, int32_t of) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
-            if (tid == 0) {
-                s_last = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == of - 1;
-                if (s_last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
-            __syncthreads();
-            return s_last != 0;
-        };
         // the sums of parts lo, lo + step, .. below hi, in the first wave
         auto join = [&](int32_t lo, int32_t hi, int32_t step) {
             z.clear();
@@ -691,11 +413,11 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
                 for (int w = 1; w < kWaves && lo + w * step < hi; ++w) z.add(s_sums[w], lane);
             __syncthreads();
         };
-        if (!last_of(a.counters + (number ? kCounters : 0) + lead, stop - lead)) continue;
+        if (!last_to_arrive(a.counters + (number ? kCounters : 0) + lead, stop - lead, &s_last)) continue;
         join(lead, stop, 1);
         if (groups > 1) {
             if (wave == 0) z.put_out(part_of(lead, number == 0), lane);
-            if (!last_of(a.counters + 2 * kCounters + first, groups)) continue;
+            if (!last_to_arrive(a.counters + 2 * kCounters + first, groups, &s_last)) continue;
             join(first, last + 1, kJoin);
         }
         if (wave == 0) write_item(z, a, cut, blocks, lane);
@@ -705,9 +427,8 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
 template <int FMT, int DK, int DV, bool AHEAD, int WPS>
 void launch(const AttentionArgs &a, int32_t blocks, hipStream_t s) {
     const dim3 grid((unsigned)a.workers), block(kThreads);
-    if (a.shift < 4) hipLaunchKernelGGL((decode_kernel<FMT, DK, DV, true, false, AHEAD, WPS>), grid, block, 0, s, a, blocks);
-    else if (a.dk == DK && a.dv == DV) hipLaunchKernelGGL((decode_kernel<FMT, DK, DV, false, true, AHEAD, WPS>), grid, block, 0, s, a, blocks);
-    else hipLaunchKernelGGL((decode_kernel<FMT, DK, DV, false, false, AHEAD, WPS>), grid, block, 0, s, a, blocks);
+    if (a.shift < 4) hipLaunchKernelGGL((decode_kernel<FMT, DK, DV, true, AHEAD, WPS>), grid, block, 0, s, a, blocks);
+    else hipLaunchKernelGGL((decode_kernel<FMT, DK, DV, false, AHEAD, WPS>), grid, block, 0, s, a, blocks);
 }
 
 int padded_dim(const AttentionArgs &a) {
@@ -721,13 +442,20 @@ void launch_format(const AttentionArgs &a, int32_t blocks, hipStream_t s) {
     case 64: launch<FMT, 64, 64, true, 2>(a, blocks, s); break;
     case 128: launch<FMT, 128, 128, true, 2>(a, blocks, s); break;
     case 256: launch<FMT, 256, 256, FMT != CRAFT_KV_F32, 2>(a, blocks, s); break;
-    default: launch<FMT, 576, 512, false, 1>(a, blocks, s); break;
+    default:
+        if constexpr (FMT == CRAFT_KV_F32) launch<FMT, 576, 512, false, 1>(a, blocks, s);
+        break;
     }
 }
 
 }  // namespace
 
+// Latent rows in 16 or 8 bits have a kernel of their own; in fp32, which serves bring-up, they come through here,
+// every block of 16 heads by itself.
+bool wide_latent(const AttentionArgs &a) { return padded_dim(a) == 576 && a.format != CRAFT_KV_F32; }
+
 int32_t attention_workers(const AttentionArgs &a, int32_t num_cu) {
+    if (wide_latent(a)) return latent_workers(a, num_cu);
     return std::min(kCounters, (padded_dim(a) == 576 ? 1 : 2) * num_cu);
 }
 
@@ -735,10 +463,12 @@ size_t attention_counters_bytes() { return 3 * kCounters * sizeof(int32_t); }
 
 size_t attention_workspace(const AttentionArgs &a, int32_t num_cu) {
     const int dv = padded_dim(a) == 576 ? 512 : padded_dim(a);
+    if (wide_latent(a)) return attention_counters_bytes() + latent_workspace(a, num_cu);
     return attention_counters_bytes() + (size_t)attention_workers(a, num_cu) * 2 * (size_t)(16 * dv + 128) * sizeof(float);
 }
 
 hipError_t launch_decode_attention(const AttentionArgs &a, hipStream_t s) {
+    if (wide_latent(a)) return launch_latent_attention(a, a.part, s);
     const int32_t blocks = (a.group + 15) / 16;
     if (a.format == CRAFT_KV_F32) launch_format<CRAFT_KV_F32>(a, blocks, s);
     else if (a.format == CRAFT_KV_BF16) launch_format<CRAFT_KV_BF16>(a, blocks, s);

@@ -297,6 +297,10 @@ struct KvAppendArgs {
 };
 hipError_t launch_kv_append(const KvAppendArgs &a, bool e4m3, hipStream_t s);
 
+// An item that starts in a run of the latent kernel and ends in run `last`; request -1: none.
+struct LatentCut {
+    int32_t request, head, last, unused;
+};
 struct AttentionArgs {
     int32_t format;                // CRAFT_KV_*
     int32_t R, Hq, heads, group;   // group = Hq / heads
@@ -315,6 +319,7 @@ struct AttentionArgs {
     float *lse;
     int32_t *counters;             // workspace: zero between calls
     float *part;                   // behind them
+    LatentCut *cuts;               // latent kernel: [workers], in front of its parts
     int32_t workers;
 };
 // Workgroups a launch may have, whatever the lengths; the workspace is sized for them.
@@ -322,5 +327,9 @@ int32_t attention_workers(const AttentionArgs &a, int32_t num_cu);
 size_t attention_counters_bytes();
 size_t attention_workspace(const AttentionArgs &a, int32_t num_cu);
 hipError_t launch_decode_attention(const AttentionArgs &a, hipStream_t s);
+// attention_latent.hip
+int32_t latent_workers(const AttentionArgs &a, int32_t num_cu);
+size_t latent_workspace(const AttentionArgs &a, int32_t num_cu);
+hipError_t launch_latent_attention(const AttentionArgs &a, void *workspace, hipStream_t s);
 
 }  // namespace craft
