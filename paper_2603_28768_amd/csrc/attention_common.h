@@ -51,20 +51,21 @@ static __device__ __forceinline__ int64_t uniform(int64_t x) {
     return (int64_t)((uint64_t)(uint32_t)uniform((int32_t)(x >> 32)) << 32 | (uint32_t)uniform((int32_t)x));
 }
 
-// Reductions over the four lanes that hold a head (lane & 15): lanes 16 and 32 apart change places.
-static __device__ __forceinline__ float other16(float x) {
-    return __shfl_xor(x, 16, 64);
-}
-static __device__ __forceinline__ float other32(float x) {
-    return __shfl_xor(x, 32, 64);
-}
+// Reductions over the four lanes that hold a head (lane & 15): rows of 16 lanes change places, odd ones of the one
+// copy with even ones of the other, then halves of the wave.
 static __device__ __forceinline__ float max_of_head(float x) {
-    x = fmaxf(x, other16(x));
-    return fmaxf(x, other32(x));
+    const uint32_t u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const uint32_t v = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 static __device__ __forceinline__ float sum_of_head(float x) {
-    x += other16(x);
-    return x + other32(x);
+    const uint32_t u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const uint32_t v = __float_as_uint(__uint_as_float(a[0]) + __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 static __device__ __forceinline__ uint32_t perm(uint32_t hi, uint32_t lo, uint32_t sel) { return __builtin_amdgcn_perm(hi, lo, sel); }
 
@@ -156,6 +157,11 @@ static __device__ __forceinline__ Start find_start(const AttentionArgs &a, int32
     return {uniform(mine.before), uniform(mine.request), uniform(mine.len)};
 }
 
+// How far a running maximum may lag behind the scores, in powers of two: weights up to 256 are as exact as weights
+// up to 1, and the sums are multiplied only when the maximum has grown by that much, which after the first units it
+// hardly ever does.
+constexpr float kSlack = 8.0f;
+
 // Running maximum (or nearly), sum of weights and weighted sum of some tokens of an item, as a wave holds them: lane (head, g)
 // has the sum of the weights of its own tokens only, the rest is whole.
 template <int NV, int CE, bool F32> struct Sums {
@@ -176,11 +182,9 @@ template <int NV, int CE, bool F32> struct Sums {
 #pragma unroll
             for (int e = 0; e < CE; ++e) acc[c][e] *= f;
     }
-    // Scores up to `top` come next: returns what to take from them.  The sums are kept for exp2(score - m) with an m
-    // that lags behind the maximum by up to 8: weights up to 256 are as exact as weights up to 1, and the sums are
-    // multiplied only when the maximum has grown by that much, which after the first units it hardly ever does.
+    // Scores up to `top` come next: returns what to take from them.
     __device__ __forceinline__ float raise(float top) {
-        if (__any(top > m + 8.0f)) {
+        if (__any(top > m + kSlack)) {
             const float up = fmaxf(m, top);
             scale(up == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - up));
             m = up;
@@ -239,8 +243,8 @@ template <int NV, int CE, bool F32> struct Sums {
                 if ((c * CE + e) % 8 == 7) __builtin_amdgcn_sched_barrier(0);
             }
     }
-    // Row i of tile (c, e) is column (c 16 + 4 g + i) CE + e: CE neighbouring columns of the output per (c, i).
-    __device__ __forceinline__ void write(const AttentionArgs &a, int32_t r, int32_t head0, int32_t n_heads, int lane) const {
+    // Row i of tile (c, e) is column ((c0 + c) 16 + 4 g + i) CE + e: CE neighbouring columns of the output per (c, i).
+    __device__ __forceinline__ void write(const AttentionArgs &a, int32_t r, int32_t head0, int32_t n_heads, int lane, int c0 = 0) const {
         const int col = lane & 15, g = lane >> 4;
         const float sum = sum_of_head(l);
         if (col >= n_heads) return;
@@ -250,7 +254,7 @@ template <int NV, int CE, bool F32> struct Sums {
         for (int c = 0; c < NV; ++c)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int d = (c * 16 + 4 * g + i) * CE;
+                const int d = ((c0 + c) * 16 + 4 * g + i) * CE;
                 if (d >= a.dv) continue;
                 if constexpr (CE == 1) {           // rows, and columns of the output, 4 g .. 4 g + 3 together
                     if (i == 0) {
@@ -273,7 +277,7 @@ template <int NV, int CE, bool F32> struct Sums {
                     }
                 }
             }
-        if (g == 0 && a.lse) a.lse[head] = sum == 0.0f ? -INFINITY : (m + __log2f(sum)) * 0.6931471805599453f;
+        if (c0 == 0 && g == 0 && a.lse) a.lse[head] = sum == 0.0f ? -INFINITY : (m + __log2f(sum)) * 0.6931471805599453f;
     }
 };
 

@@ -5,11 +5,13 @@
 // used where the first product leaves them).  What is different is the ratio: 128 heads make 2 (576 + 512) 128
 // operations of 1152 bytes, more than the matrix units' share of what HBM delivers, so every row is fetched once
 // for many heads, into LDS.  From there K is read as rows and V by columns, by each of the waves that hold the
-// heads.  A wave holds 16 heads: Q (18 fragments) and the sums (512 columns) fill most of its registers.
+// heads.  
 //
-// A workgroup holds 16 WH heads; WK groups of WH waves take every WK-th unit of 32 tokens and are added at the
-// end of an item's run.  Rows travel straight into LDS, a tile ahead, 16-byte pieces in an order (exclusive or with
-// the row's number) in which neither way of reading meets a bank twice.  Rows that a tile lacks (behind the last
+// A workgroup holds 64 heads, 16 a wave, one wave per SIMD unit: Q, the sums of 512 columns and what is on its way
+// from LDS take more than half of a SIMD unit's registers.  The products of a tile's scores run before those of the
+// tile in front of it with its values, so that the softmax of the one hides behind the other.  Rows travel straight
+// into LDS, up to three tiles of 32 tokens ahead, 16-byte pieces in an order (exclusive or with the row's number) in
+// which neither way of reading meets a bank twice.  Rows that a tile lacks (behind the last
 // token, in front of the window, without a page) are fetched from a row of zeros and masked by -infinity.
 #include <algorithm>
 
@@ -23,15 +25,20 @@ constexpr int kMinRun = 8;                         // of a workgroup, where ther
 
 __device__ const uint4 zero_row[72] = {};          // 1152 bytes
 
+// four bytes per lane
+static __device__ __forceinline__ void dma_word_at(ubase_t p, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(lds), "v"(p) : "memory");
+}
 static __device__ __forceinline__ void dma_chunk_at(ubase_t p, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds), "v"(p) : "memory");
 }
 
 // Where a row's 16-byte pieces lie: piece p in place p ^ place_of(row), so that what LDS delivers in a clock, 256
-// bytes, lies in 64 banks: a read of keys takes the same piece of 16 rows, a transposed read of values two
-// neighbouring pieces of 8 rows, or (8 bits) one piece of 8 rows of either tile of a unit.
+// bytes, lies in 64 banks: a read of keys takes a piece of rows 0 to 3 and 12 to 15 and the next one of rows 4 to
+// 11, or the other way round; a transposed read of values two neighbouring pieces of rows 0 to 7 or 8 to 15, or (8
+// bits) one piece of these rows of either tile of a unit.
 template <int FMT> __device__ __forceinline__ int place_of(int row) {
-    return (row & 7) << 1 | ((row >> 3 ^ (FMT == CRAFT_KV_E4M3 ? row >> 4 : 0)) & 1);
+    return ((row ^ (row >> 1 & 4)) & 7) << 1 | ((row >> 3 ^ (FMT == CRAFT_KV_E4M3 ? row >> 4 : 0)) & 1);
 }
 // the same for what lies behind the value part: 128 bytes, or 64
 template <int FMT> __device__ __forceinline__ int rest_place_of(int row) { return FMT == CRAFT_KV_BF16 ? row >> 1 & 7 : row >> 2 & 3; }
@@ -46,34 +53,39 @@ typedef const u32x4_t __attribute__((address_space(3))) *lds_piece_t;
 typedef s16x4_t __attribute__((address_space(3))) *lds_s16x4_t;
 typedef i32x2_t __attribute__((address_space(3))) *lds_i32x2_t;
 
-constexpr int kAhead = 1;                          // steps that reads of LDS are ahead
+constexpr int kWaves = 4;                          // of a workgroup, 16 heads each
+constexpr int kBuffers = 4;                        // tiles in LDS, and on their way there
+constexpr int kAhead = 3;                          // steps that reads of LDS are ahead
 constexpr int kStep = 2;                           // tiles of 16 columns of a step
 typedef Sums<32, 1, false> State;                  // 32 tiles of 16 columns
 
 // FMT: CRAFT_KV_BF16 or CRAFT_KV_E4M3 (codes stay codes in LDS and are widened in front of the products).
-template <int FMT, int WH, int WK>
-__global__ __launch_bounds__(64 * WH * WK) void latent_kernel(AttentionArgs a, int32_t blocks) {
+template <int FMT>
+__global__ __launch_bounds__(64 * kWaves, 1) void latent_kernel(AttentionArgs a, int32_t blocks) {
     typedef Shape<FMT, 576, 512> S;
-    constexpr int W = WH * WK, T = kUnit * WK, RPW = T / W;          // waves, rows of a tile, rows a wave fetches
+    constexpr int T = kUnit, RPW = T / kWaves;                       // rows of a tile, rows a wave fetches
     constexpr int RB = 512 * S::B, TB = 64 * S::B;                   // bytes of a row's value part and of the rest
     constexpr int BUF = T * (RB + TB);
-    constexpr int kSumBytes = (WK - 1) * WH * State::kFloats * 4;
-    __shared__ __attribute__((aligned(1024))) unsigned char s_rows[2 * BUF > kSumBytes ? 2 * BUF : kSumBytes];
-    __shared__ __attribute__((aligned(16))) float s_mask[2][T], s_scale[2][FMT == CRAFT_KV_E4M3 ? T : 4];
-    static_assert(RPW % 8 == 0, "a wave fetches whole groups of eight rows");
+    constexpr int kRows = FMT == CRAFT_KV_BF16 ? 1 : 2, kLanes = 64 / kRows;        // rows of a request, lanes of a row
+    constexpr int kRequests = FMT == CRAFT_KV_BF16 ? RPW + 1 : RPW / 2 + 2;   // of a wave for a tile
+    __shared__ __attribute__((aligned(1024))) unsigned char s_rows[kBuffers * BUF];
+    __shared__ __attribute__((aligned(16))) float s_mask[kBuffers][T], s_scale[kBuffers][FMT == CRAFT_KV_E4M3 ? T : 4];
+    static_assert(RPW == 8, "a wave fetches eight rows");
+    static_assert(S::NK % kRequests == 0 || S::NK / kRequests * kRequests <= S::NK, "a request every few steps");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col = lane & 15, g = lane >> 4, wh = wave % WH, wk = wave / WH;
+    const int col = lane & 15, g = lane >> 4;
     const int32_t worker = blockIdx.x % a.workers, block = blockIdx.x / a.workers;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)s_rows;
+    const uint32_t scale0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)&s_scale[0][0];
     Runs runs;
-    const Start st = find_start<W, 1>(a, a.heads, kItemCost, a.workers, kMinRun, worker, runs);
+    const Start st = find_start<kWaves, 1>(a, a.heads, kItemCost, a.workers, kMinRun, worker, runs);
     if (tid == 0 && block == 0) a.cuts[worker].request = -1;
     if (worker >= runs.n) return;
     const int32_t pieces = a.dk / (16 / S::B);     // of a row, 16 bytes each
     int64_t at = runs.start(worker), before = st.before;
     const int64_t end = runs.start(worker + 1);
     int32_t r = st.request, len = st.len;
-    const int32_t head_in_group = (block * WH + wh) * 16, n_heads = min(16, a.group - head_in_group);
+    const int32_t head_in_group = (block * kWaves + wave) * 16, n_heads = min(16, a.group - head_in_group);
     State z;
     // where this lane reads: its first key piece in the value part of a unit's rows and behind it, and its first
     // value.  Pieces and tiles of columns are read in the order of their places, so that those 256 bytes apart follow
@@ -105,12 +117,16 @@ __global__ __launch_bounds__(64 * WH * WK) void latent_kernel(AttentionArgs a, i
         // ---- a tile into LDS: this wave's rows.  Lane i has the place of row i of them.
         const unsigned char *kh = a.k + h * a.k_head;
         const int32_t *table = a.table + (int64_t)request * a.table_stride;
-        const int32_t in_page = (1 << a.shift) - 1, my_row = wave * RPW + (lane & (RPW - 1));
+        const int32_t in_page = (1 << a.shift) - 1;
         auto entry = [&](int32_t i) -> int32_t { return table[min(i, a.max_pages - 1)]; };
         int32_t held0 = (token0 + wave * RPW) >> a.shift;
         int32_t held = entry(held0 + lane), behind = entry(held0 + 64 + lane);
-        float scale_next = 0.0f;
-        auto fetch = [&](int32_t tile, int b) __attribute__((always_inline)) {
+        // A tile's requests: where each starts for this lane.  They are issued one by one between the products, since a
+        // wave waits where it asks for more than the memory pipeline takes at once.  Tiles behind the last one are
+        // asked for like the others (as zeros): so many requests are on their way, always.
+        ubase_t from[kRequests];
+        uint32_t to_main = 0, to_rest = 0;
+        auto plan = [&](int32_t tile, int b) __attribute__((always_inline)) {
             const int lane = (int)anew(tid & 63), my_row = wave * RPW + (lane & (RPW - 1));
             const int32_t token = token0 + tile * T + my_row;
             if (((token0 + tile * T + wave * RPW + RPW - 1) >> a.shift) - held0 >= 64) {
@@ -124,36 +140,44 @@ __global__ __launch_bounds__(64 * WH * WK) void latent_kernel(AttentionArgs a, i
             const bool there = token >= first && token < token1 && (uint32_t)page < (uint64_t)a.pages;
             const unsigned char *row = there ? kh + page * a.k_page + (token & in_page) * a.k_token : reinterpret_cast<const unsigned char *>(zero_row);
             if (lane < RPW) s_mask[b][my_row] = there ? 0.0f : -INFINITY;
-            if (FMT == CRAFT_KV_E4M3) scale_next = there ? a.k_scale[(((int64_t)page * a.heads + h) << a.shift) + (token & in_page)] : 0.0f;
+            if (FMT == CRAFT_KV_E4M3)
+                from[kRequests - 1] = reinterpret_cast<ubase_t>(there ? a.k_scale + ((((int64_t)page * a.heads + h) << a.shift) + (token & in_page)) : reinterpret_cast<const float *>(zero_row));
             const uint32_t lo = (uint32_t)(uintptr_t)row, hi = (uint32_t)((uintptr_t)row >> 32);
-            auto row_of = [&](int from) { return reinterpret_cast<ubase_t>((uint64_t)(uint32_t)__shfl((int)hi, from, 64) << 32 | (uint32_t)__shfl((int)lo, from, 64)); };
-            // what lies behind a shorter row is zeros
-            auto piece_of = [&](ubase_t base, int piece) { return (piece < pieces ? base : reinterpret_cast<ubase_t>(zero_row)) + piece * 16; };
-            const uint32_t main0 = lds0 + b * BUF + wave * RPW * RB, rest0 = lds0 + b * BUF + T * RB + wave * RPW * TB;
-            if (FMT == CRAFT_KV_BF16) {
+            to_main = lds0 + b * BUF + wave * RPW * RB;
+            to_rest = lds0 + b * BUF + T * RB + wave * RPW * TB;
+            const int rest_row = FMT == CRAFT_KV_BF16 ? lane >> 3 : lane >> 2 & (RPW - 1);
+            const int rest_piece = kLanes + ((lane & (FMT == CRAFT_KV_BF16 ? 7 : 3)) ^ rest_place_of<FMT>(wave * RPW + rest_row));
+            if (a.shift >= 3 && pieces == 72 / kRows && __all(there)) {
+                // eight rows of a page: one address and the distance between rows
+                ubase_t base = reinterpret_cast<ubase_t>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)hi) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)lo));
+                const uint32_t step = (uint32_t)a.k_token;
+                from[0] = base + ((uint32_t)rest_row * step + rest_piece * 16);
 #pragma unroll
-                for (int i = 0; i < RPW; ++i) {
-                    const ubase_t base = reinterpret_cast<ubase_t>((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)lo, i));
-                    const int piece = lane ^ place_of<FMT>(wave * RPW + i);
-                    if (pieces >= 64) dma_chunk(base, piece * 16, main0 + i * RB);
-                    else dma_chunk_at(piece_of(base, piece), main0 + i * RB);
-                }
-#pragma unroll
-                for (int i = 0; i < RPW; i += 8) {
-                    const int piece = 64 + ((lane & 7) ^ rest_place_of<FMT>(wave * RPW + i + (lane >> 3)));
-                    const ubase_t base = row_of(i + (lane >> 3));
-                    dma_chunk_at(piece_of(base, piece), rest0 + i * TB);
+                for (int i = 0; i < RPW; i += kRows) {
+                    const int in = FMT == CRAFT_KV_BF16 ? 0 : lane >> 5;
+                    from[1 + i / kRows] = base + ((uint32_t)(i + in) * step + ((lane & (kLanes - 1)) ^ place_of<FMT>(wave * RPW + i + in)) * 16);
                 }
             } else {
+                // what a row lacks at its end is zeros
+                auto piece_at = [&](int from, int piece) {
+                    const ubase_t base = reinterpret_cast<ubase_t>((uint64_t)(uint32_t)__shfl((int)hi, from, 64) << 32 | (uint32_t)__shfl((int)lo, from, 64));
+                    return (piece < pieces ? base : reinterpret_cast<ubase_t>(zero_row)) + piece * 16;
+                };
+                from[0] = piece_at(rest_row, rest_piece);
 #pragma unroll
-                for (int i = 0; i < RPW; i += 2) {
-                    const int piece = (lane & 31) ^ place_of<FMT>(wave * RPW + i + (lane >> 5));
-                    const ubase_t base = row_of(i + (lane >> 5));
-                    dma_chunk_at(piece_of(base, piece), main0 + i * RB);
+                for (int i = 0; i < RPW; i += kRows) {
+                    const int in = FMT == CRAFT_KV_BF16 ? 0 : lane >> 5;
+                    from[1 + i / kRows] = piece_at(i + in, (lane & (kLanes - 1)) ^ place_of<FMT>(wave * RPW + i + in));
                 }
-                const int piece = 32 + ((lane & 3) ^ rest_place_of<FMT>(wave * RPW + (lane >> 2)));
-                const ubase_t base = row_of(lane >> 2 & (RPW - 1));
-                if (lane < 4 * RPW) dma_chunk_at(piece_of(base, piece), rest0);
+            }
+        };
+        auto ask = [&](int i, int b) __attribute__((always_inline)) {
+            if (i >= 1 && i <= RPW / kRows) {
+                dma_chunk_at(from[i], to_main + (i - 1) * kRows * RB);
+            } else if (i == 0) {
+                if (FMT == CRAFT_KV_BF16 || lane < 4 * RPW) dma_chunk_at(from[0], to_rest);
+            } else if (i < kRequests && lane < RPW) {
+                dma_word_at(from[kRequests - 1], scale0 + (b * T + wave * RPW) * 4);
             }
         };
 
@@ -170,118 +194,152 @@ __global__ __launch_bounds__(64 * WH * WK) void latent_kernel(AttentionArgs a, i
             }
         }
         z.clear();
+        // here, and not inside the loop, the compiler waits for them; it knows nothing of the rows on their way, and a
+        // wait of its own would wait for those too
+#pragma unroll
+        for (int i = 0; i < S::QN; ++i) asm volatile("" : "+v"(q[i]));
 
-        fetch(0, 0);
-        auto land = [&](int b) {                   // what was fetched into buffer b is there for everybody
-            dma_wait<0>();
-            if (FMT == CRAFT_KV_E4M3 && lane < RPW) s_scale[b][my_row] = scale_next;
-            __syncthreads();
-        };
-        land(0);
-        const int32_t tiles = (u1 - u0 + WK - 1) / WK;
-        for (int32_t tile = 0; tile < tiles; ++tile) {
-            const int b = tile & 1;
-            if (tile + 1 < tiles) fetch(tile + 1, b ^ 1);
-            if (u0 + tile * WK + wk < u1 && n_heads > 0) {
-                const uint32_t rows = lds0 + b * BUF + wk * kUnit * RB, rest = lds0 + b * BUF + T * RB + wk * kUnit * TB;
-                // ---- scores.  The next pieces travel behind the products of these.
-                f32x4_t s[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
-                u32x4_t kr[kAhead + 1][2];
-                // a piece's place in its 256 bytes is exclusive-or'ed into the address of the lane's first one
-                const uint32_t key0 = anew(rows + key_at), key1 = FMT == CRAFT_KV_E4M3 ? key0 ^ 16 : key0, rest0 = anew(rest + rest_at);
-                auto read_keys = [&](int i) __attribute__((always_inline)) {
-                    const int step = key_step(i);
-                    if (step < RB / 64) {
-                        kr[i % (kAhead + 1)][0] = *(lds_piece_t)(uintptr_t)((key0 ^ (step & 3) * 64) + (step >> 2) * 256);
-                        kr[i % (kAhead + 1)][1] = *(lds_piece_t)(uintptr_t)((key1 ^ (step & 3) * 64) + (step >> 2) * 256 + 16 * RB);
-                    } else {
-                        kr[i % (kAhead + 1)][0] = *(lds_piece_t)(uintptr_t)(rest0 ^ (step & 1 & TB / 128) * 64);
-                        kr[i % (kAhead + 1)][1] = *(lds_piece_t)(uintptr_t)((rest0 ^ (step & 1 & TB / 128) * 64) + 16 * TB);
-                    }
-                };
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) read_keys(i);
-#pragma unroll
-                for (int i = 0; i < S::NK; ++i) {
-                    if (i + kAhead < S::NK) read_keys(i + kAhead);
-#pragma unroll
-                    for (int e = 0; e < (FMT == CRAFT_KV_E4M3 ? 2 : 1); ++e)
-#pragma unroll
-                        for (int t = 0; t < 2; ++t) {
-                            const u32x4_t kc = kr[i % (kAhead + 1)][t];
-                            const bf16x8_t kf = FMT == CRAFT_KV_BF16 ? __builtin_bit_cast(bf16x8_t, kc) : widen((u32x2_t){kc[2 * e], kc[2 * e + 1]});
-                            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, __builtin_bit_cast(bf16x8_t, q[FMT == CRAFT_KV_E4M3 ? 2 * key_step(i) + e : key_step(i)]), s[t], 0, 0, 0);
-                        }
-                    __builtin_amdgcn_sched_barrier(0);
+        const int32_t tiles = u1 - u0;
+        const bool busy = n_heads > 0;
+        // every wave's part of a tile has landed, and everybody is done with the tile before the last one
+        auto meet = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+        f32x4_t s[2];
+        auto scores = [&](int b, bool more, int next) __attribute__((always_inline)) {
+            const uint32_t rows = lds0 + b * BUF, rest = rows + T * RB;
+            // a piece's place in its 256 bytes is exclusive-or'ed into the address of the lane's first one
+            const uint32_t key0 = anew(rows + key_at), key1 = FMT == CRAFT_KV_E4M3 ? key0 ^ 16 : key0, rest0 = anew(rest + rest_at);
+            u32x4_t kr[kAhead + 1][2];
+            auto read_keys = [&](int i) __attribute__((always_inline)) {
+                const int step = key_step(i);
+                if (step < RB / 64) {
+                    kr[i % (kAhead + 1)][0] = *(lds_piece_t)(uintptr_t)((key0 ^ (step & 3) * 64) + (step >> 2) * 256);
+                    kr[i % (kAhead + 1)][1] = *(lds_piece_t)(uintptr_t)((key1 ^ (step & 3) * 64) + (step >> 2) * 256 + 16 * RB);
+                } else {
+                    kr[i % (kAhead + 1)][0] = *(lds_piece_t)(uintptr_t)(rest0 ^ (step & 1 & TB / 128) * 64);
+                    kr[i % (kAhead + 1)][1] = *(lds_piece_t)(uintptr_t)((rest0 ^ (step & 1 & TB / 128) * 64) + 16 * TB);
                 }
-                // ---- weights
-                f32x4_t scale[2];
-                float x[2][4];
+            };
+            s[0] = s[1] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const f32x4_t mask = *reinterpret_cast<const f32x4_t *>(&s_mask[b][wk * kUnit + t * 16 + 4 * g]);
-                    if (FMT == CRAFT_KV_E4M3) scale[t] = *reinterpret_cast<const f32x4_t *>(&s_scale[b][wk * kUnit + t * 16 + 4 * g]);
+            for (int i = 0; i < kAhead; ++i) read_keys(i);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x[t][j] = s[t][j] * (FMT == CRAFT_KV_E4M3 ? a.scale_log2 * scale[t][j] : a.scale_log2) + mask[j];
-                }
-                float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
-                const float base = z.raise(max_of_head(top));
-                float p[2][4];
+            for (int i = 0; i < S::NK; ++i) {
+                if (i + kAhead < S::NK) read_keys(i + kAhead);
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int e = 0; e < (FMT == CRAFT_KV_E4M3 ? 2 : 1); ++e)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        p[t][j] = __builtin_amdgcn_exp2f(x[t][j] - base);
-                        z.l += p[t][j];
-                        if (FMT == CRAFT_KV_E4M3) p[t][j] *= scale[t][j];
+                    for (int t = 0; t < 2; ++t) {
+                        const u32x4_t kc = kr[i % (kAhead + 1)][t];
+                        const bf16x8_t kf = FMT == CRAFT_KV_BF16 ? __builtin_bit_cast(bf16x8_t, kc) : widen((u32x2_t){kc[2 * e], kc[2 * e + 1]});
+                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, __builtin_bit_cast(bf16x8_t, q[FMT == CRAFT_KV_E4M3 ? 2 * key_step(i) + e : key_step(i)]), s[t], 0, 0, 0);
                     }
-                const wide_t pw = {bf16_pair(p[0][0], p[0][1]), bf16_pair(p[0][2], p[0][3]), bf16_pair(p[1][0], p[1][1]), bf16_pair(p[1][2], p[1][3])};
-                const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, pw);
-                // ---- values: columns of 16 out of LDS, transposed on the way (a lane gets four, or eight, tokens
-                // of its column out of the 8 bytes each that 16 lanes ask for)
-                bf16x8_t vf[kAhead + 1][kStep];
-                const uint32_t value0 = anew(rows + value_at);
-                auto read_values = [&](int step) __attribute__((always_inline)) {
-#pragma unroll
-                    for (int c = 0; c < kStep; ++c) {
-                        const int tile = value_tile(step * kStep + c);
-                        const uint32_t p = (value0 ^ (uint32_t)(tile % (256 / (16 * S::B))) * (16 * S::B)) + tile / (256 / (16 * S::B)) * 256;
-                        if (FMT == CRAFT_KV_BF16) {
-                            const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(uintptr_t)p);
-                            const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(uintptr_t)(p + 16 * RB));
-                            vf[step % (kAhead + 1)][c] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-                        } else {
-                            vf[step % (kAhead + 1)][c] = widen(__builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2_t)(uintptr_t)p)));
-                        }
-                    }
-                };
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) read_values(i);
-#pragma unroll
-                for (int i = 0; i < 32 / kStep; ++i) {
-                    if (i + kAhead < 32 / kStep) read_values(i + kAhead);
-#pragma unroll
-                    for (int c = 0; c < kStep; ++c)
-                        z.acc[value_tile(i * kStep + c)][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i % (kAhead + 1)][c], pf, z.acc[value_tile(i * kStep + c)][0], 0, 0, 0);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                if (more && i % (S::NK / kRequests) == 0) ask(i / (S::NK / kRequests), next);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            land(b ^ 1);
-        }
+        };
+        // The weights of the scores.  What the maximum's growth multiplies the sums by is left to the caller, behind
+        // the products that come first; only the sum of the weights has it already.
+        float factor = 1.0f;
+        auto weights = [&](int b) __attribute__((always_inline)) -> bf16x8_t {
+            f32x4_t scale[2];
+            float x[2][4];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const f32x4_t mask = *reinterpret_cast<const f32x4_t *>(&s_mask[b][t * 16 + 4 * g]);
+                if (FMT == CRAFT_KV_E4M3) scale[t] = *reinterpret_cast<const f32x4_t *>(&s_scale[b][t * 16 + 4 * g]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[t][j] = s[t][j] * (FMT == CRAFT_KV_E4M3 ? a.scale_log2 * scale[t][j] : a.scale_log2) + mask[j];
+            }
+            const float top = max_of_head(fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3]))));
+            const float up = top > z.m + kSlack ? top : z.m;
+            factor = up == z.m ? 1.0f : __builtin_amdgcn_exp2f(z.m - up);
+            z.m = up;
+            z.l *= factor;
+            const float base = up == -INFINITY ? 0.0f : up;
+            float p[2][4];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    p[t][j] = __builtin_amdgcn_exp2f(x[t][j] - base);
+                    z.l += p[t][j];
+                    if (FMT == CRAFT_KV_E4M3) p[t][j] *= scale[t][j];
+                }
+            const wide_t pw = {bf16_pair(p[0][0], p[0][1]), bf16_pair(p[0][2], p[0][3]), bf16_pair(p[1][0], p[1][1]), bf16_pair(p[1][2], p[1][3])};
+            return __builtin_bit_cast(bf16x8_t, pw);
+        };
+        // Values: columns of 16 out of LDS, transposed on the way (a lane gets four, or eight, tokens of its column
+        // out of the 8 bytes each that 16 lanes ask for).
+        auto values = [&](int b, bf16x8_t pf) __attribute__((always_inline)) {
+            bf16x8_t vf[kAhead + 1][kStep];
+            const uint32_t value0 = anew(lds0 + b * BUF + value_at);
+            auto read_values = [&](int step) __attribute__((always_inline)) {
+#pragma unroll
+                for (int c = 0; c < kStep; ++c) {
+                    const int tile = value_tile(step * kStep + c);
+                    const uint32_t p = (value0 ^ (uint32_t)(tile % (256 / (16 * S::B))) * (16 * S::B)) + tile / (256 / (16 * S::B)) * 256;
+                    if (FMT == CRAFT_KV_BF16) {
+                        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(uintptr_t)p);
+                        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(uintptr_t)(p + 16 * RB));
+                        vf[step % (kAhead + 1)][c] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                    } else {
+                        vf[step % (kAhead + 1)][c] = widen(__builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2_t)(uintptr_t)p)));
+                    }
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) read_values(i);
+#pragma unroll
+            for (int i = 0; i < 32 / kStep; ++i) {
+                if (i + kAhead < 32 / kStep) read_values(i + kAhead);
+#pragma unroll
+                for (int c = 0; c < kStep; ++c)
+                    z.acc[value_tile(i * kStep + c)][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i % (kAhead + 1)][c], pf, z.acc[value_tile(i * kStep + c)][0], 0, 0, 0);
+            }
+        };
+        auto rescale = [&]() __attribute__((always_inline)) {
+            if (__any(factor != 1.0f)) {
+#pragma unroll
+                for (int c = 0; c < 32; ++c) z.acc[c][0] *= factor;
+            }
+        };
 
-        // ---- the sums of the WK groups, in the first one
-        if (WK > 1) {
-            float *sums = reinterpret_cast<float *>(s_rows);
-            if (wk > 0) z.put(sums + ((wk - 1) * WH + wh) * State::kFloats, lane);
-            __syncthreads();
-            if (wk == 0)
-                for (int w = 0; w < WK - 1; ++w) z.add(sums + (w * WH + wh) * State::kFloats, lane);
-            __syncthreads();
+        for (int i = 0; i < kBuffers - 1; ++i) {
+            plan(i, i);
+#pragma unroll
+            for (int j = 0; j < kRequests; ++j) ask(j, i);
         }
+        dma_wait<2 * kRequests>();
+        meet();
+        bf16x8_t pf = {};
+        if (busy) {
+            scores(0, false, 0);
+            pf = weights(0);
+        }
+        for (int32_t tile = 0; tile + 1 < tiles; ++tile) {
+            dma_wait<kRequests>();
+            meet();
+            const int next = (tile + 3) % kBuffers;
+            plan(tile + 3, next);
+            if (busy) {
+                scores((tile + 1) % kBuffers, true, next);
+                const bf16x8_t pn = weights((tile + 1) % kBuffers);
+                values(tile % kBuffers, pf);
+                rescale();
+                pf = pn;
+            } else {
+#pragma unroll
+                for (int j = 0; j < kRequests; ++j) ask(j, next);
+            }
+        }
+        if (busy) values((tiles - 1) % kBuffers, pf);
+        dma_wait<0>();
+        meet();                                    // the buffers are free for the next item
+
         const bool starts = u0 == 0, ends = u1 == n_units;
-        if (wk == 0 && n_heads > 0) {
+        if (busy) {
             if (starts && ends) z.write(a, request, h * a.group + head_in_group, n_heads, lane);
-            else z.put(a.part + (((int64_t)worker * 2 + (starts ? 1 : 0)) * blocks * WH + block * WH + wh) * State::kFloats, lane);
+            else z.put(a.part + (((int64_t)worker * 2 + (starts ? 1 : 0)) * blocks * kWaves + block * kWaves + wave) * State::kFloats, lane);
         }
         if (starts && !ends && tid == 0 && block == 0) a.cuts[worker] = {request, h, runs.of(item_end - 1), 0};
     }
@@ -289,54 +347,37 @@ __global__ __launch_bounds__(64 * WH * WK) void latent_kernel(AttentionArgs a, i
 
 // Joins the parts of the items that are cut between workgroups: the last part of run blockIdx.x and the first ones of
 // those that follow.  A launch of its own, because the parts are many (33 KiB for every 16 heads) and their sum wants
-// many CUs: 16 heads and half their columns each; a wave has four tiles of columns.
-template <int WH>
-__global__ __launch_bounds__(256) void latent_join_kernel(AttentionArgs a, int32_t blocks) {
-    const int32_t run = blockIdx.x, set = blockIdx.y >> 1;
-    const int lane = threadIdx.x & 63, tile0 = (blockIdx.y & 1) * 16 + (threadIdx.x >> 6) * 4;
+// many CUs: a workgroup has four tiles of columns of 16 heads, its waves every fourth part.
+__global__ __launch_bounds__(64 * kWaves) void latent_join_kernel(AttentionArgs a, int32_t blocks) {
+    typedef Sums<4, 1, false> Four;
+    __shared__ float s_sums[kWaves][Four::kFloats];
+    const int32_t run = blockIdx.x, set = blockIdx.y >> 3;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tile0 = (blockIdx.y & 7) * 4;
     const LatentCut cut = a.cuts[run];
     const int32_t n_heads = min(16, a.group - set * 16);
-    if (cut.request < 0 || n_heads <= 0) return;
-    f32x4_t acc[4] = {};
-    float m = -INFINITY, l = 0.0f;
+    if (cut.request < 0 || n_heads <= 0 || tile0 * 16 >= a.dv) return;
+    Four z;
+    z.clear();
 #pragma unroll 4
-    for (int32_t w = run; w <= cut.last; ++w) {
-        const float *part = a.part + (((int64_t)w * 2 + (w == run ? 1 : 0)) * blocks * WH + set) * State::kFloats;
-        const float om = part[State::kFloats - 128 + lane], ol = part[State::kFloats - 64 + lane];
-        f32x4_t x[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) x[c] = *reinterpret_cast<const f32x4_t *>(part + ((tile0 + c) * 64 + lane) * 4);
-        const float up = fmaxf(m, om);
-        const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - up), of = om == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(om - up);
-        m = up;
-        l = l * f + ol * of;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) acc[c] = acc[c] * f + x[c] * of;
+    for (int32_t w = run + wave; w <= cut.last; w += kWaves) {
+        const float *part = a.part + (((int64_t)w * 2 + (w == run ? 1 : 0)) * blocks * kWaves + set) * State::kFloats;
+        z.join(part[State::kFloats - 128 + lane], part[State::kFloats - 64 + lane],
+               [&](int c, int) { return *reinterpret_cast<const f32x4_t *>(part + ((tile0 + c) * 64 + lane) * 4); });
     }
-    const int col = lane & 15, g = lane >> 4;
-    const float sum = sum_of_head(l);
-    if (col >= n_heads) return;
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    const int64_t head = (int64_t)cut.request * a.Hq + cut.head * a.group + set * 16 + col;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        const int d = (tile0 + c) * 16 + 4 * g;
-        if (d < a.dv)
-            *reinterpret_cast<u32x2_t *>(static_cast<unsigned char *>(a.out) + (head * a.dv + d) * 2) =
-                (u32x2_t){bf16_pair(acc[c][0] * inv, acc[c][1] * inv), bf16_pair(acc[c][2] * inv, acc[c][3] * inv)};
-    }
-    if (tile0 == 0 && g == 0 && a.lse) a.lse[head] = sum == 0.0f ? -INFINITY : (m + __log2f(sum)) * 0.6931471805599453f;
+    if (wave > 0) z.put(s_sums[wave], lane);
+    __syncthreads();
+    if (wave > 0) return;
+    for (int w = 1; w < kWaves && run + w <= cut.last; ++w) z.add(s_sums[w], lane);
+    z.write(a, cut.request, cut.head * a.group + set * 16, n_heads, lane, tile0);
 }
 
-constexpr int kWH = 4, kWK = 2;
-
-int32_t latent_blocks(const AttentionArgs &a) { return (a.group + 16 * kWH - 1) / (16 * kWH); }
+int32_t latent_blocks(const AttentionArgs &a) { return (a.group + 16 * kWaves - 1) / (16 * kWaves); }
 
 template <int FMT>
 void launch_format(const AttentionArgs &a, hipStream_t s) {
     const int32_t blocks = latent_blocks(a);
-    hipLaunchKernelGGL((latent_kernel<FMT, kWH, kWK>), dim3((unsigned)(a.workers * blocks)), dim3(64 * kWH * kWK), 0, s, a, blocks);
-    hipLaunchKernelGGL(latent_join_kernel<kWH>, dim3((unsigned)a.workers, (unsigned)(blocks * kWH * 2)), dim3(256), 0, s, a, blocks);
+    hipLaunchKernelGGL((latent_kernel<FMT>), dim3((unsigned)(a.workers * blocks)), dim3(64 * kWaves), 0, s, a, blocks);
+    hipLaunchKernelGGL(latent_join_kernel, dim3((unsigned)a.workers, (unsigned)(blocks * kWaves * 8)), dim3(64 * kWaves), 0, s, a, blocks);
 }
 
 }  // namespace
@@ -350,7 +391,7 @@ int32_t latent_workers(const AttentionArgs &a, int32_t num_cu) {
 
 size_t latent_workspace(const AttentionArgs &a, int32_t num_cu) {
     const size_t w = (size_t)latent_workers(a, num_cu);
-    return w * sizeof(LatentCut) + w * 2 * latent_blocks(a) * kWH * State::kFloats * sizeof(float);
+    return w * sizeof(LatentCut) + w * 2 * latent_blocks(a) * kWaves * State::kFloats * sizeof(float);
 }
 
 hipError_t launch_latent_attention(const AttentionArgs &args, void *workspace, hipStream_t s) {
