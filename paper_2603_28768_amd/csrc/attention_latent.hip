@@ -26,6 +26,9 @@ constexpr int kMinRun = 8;                         // of a workgroup, where ther
 __device__ const uint4 zero_row[72] = {};          // 1152 bytes
 
 // four bytes per lane
+static __device__ __forceinline__ void dma_word(ubase_t base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" :: "s"(lds), "v"(off), "s"(base) : "memory");
+}
 static __device__ __forceinline__ void dma_word_at(ubase_t p, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(lds), "v"(p) : "memory");
 }
@@ -71,7 +74,6 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_kernel(AttentionArgs a,
     __shared__ __attribute__((aligned(1024))) unsigned char s_rows[kBuffers * BUF];
     __shared__ __attribute__((aligned(16))) float s_mask[kBuffers][T], s_scale[kBuffers][FMT == CRAFT_KV_E4M3 ? T : 4];
     static_assert(RPW == 8, "a wave fetches eight rows");
-    static_assert(S::NK % kRequests == 0 || S::NK / kRequests * kRequests <= S::NK, "a request every few steps");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int32_t worker = blockIdx.x % a.workers, block = blockIdx.x / a.workers;
@@ -87,6 +89,12 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_kernel(AttentionArgs a,
     int32_t r = st.request, len = st.len;
     const int32_t head_in_group = (block * kWaves + wave) * 16, n_heads = min(16, a.group - head_in_group);
     State z;
+    // where this lane's pieces of eight whole rows lie: of the first row (or two) of the value part, and of the rest
+    const bool whole_rows = a.shift >= 3 && pieces == 72 / kRows;
+    const uint32_t main_row = FMT == CRAFT_KV_BF16 ? 0u : (uint32_t)(lane >> 5) * (uint32_t)a.k_token;
+    const uint32_t main_off = (uint32_t)((lane & (kLanes - 1)) ^ place_of<FMT>(wave * RPW + (FMT == CRAFT_KV_BF16 ? 0 : lane >> 5))) * 16;
+    const int in_rest = FMT == CRAFT_KV_BF16 ? lane >> 3 : lane >> 2 & (RPW - 1);
+    const uint32_t rest_off = (uint32_t)in_rest * (uint32_t)a.k_token + (kLanes + ((lane & (FMT == CRAFT_KV_BF16 ? 7 : 3)) ^ rest_place_of<FMT>(wave * RPW + in_rest))) * 16;
     // where this lane reads: its first key piece in the value part of a unit's rows and behind it, and its first
     // value.  Pieces and tiles of columns are read in the order of their places, so that those 256 bytes apart follow
     // one another and share an address.
@@ -121,63 +129,69 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_kernel(AttentionArgs a,
         auto entry = [&](int32_t i) -> int32_t { return table[min(i, a.max_pages - 1)]; };
         int32_t held0 = (token0 + wave * RPW) >> a.shift;
         int32_t held = entry(held0 + lane), behind = entry(held0 + 64 + lane);
-        // A tile's requests: where each starts for this lane.  They are issued one by one between the products, since a
-        // wave waits where it asks for more than the memory pipeline takes at once.  Tiles behind the last one are
-        // asked for like the others (as zeros): so many requests are on their way, always.
-        ubase_t from[kRequests];
-        uint32_t to_main = 0, to_rest = 0;
+        // A tile's requests go out one by one between the products, since a wave waits where it asks for more than the
+        // memory pipeline takes at once.  That is for eight whole rows of one page, which share an address; what else
+        // there is (rows that are not there, short rows, small pages) is asked for when it is planned.  Tiles behind
+        // the last one are asked for as well (as zeros), so that there are always as many requests on their way.
+        bool later = false;                        // the planned requests are still to be made
+        ubase_t from = nullptr, from_scale = nullptr;
+        uint32_t to_main = 0, to_rest = 0, to_scale = 0;
         auto plan = [&](int32_t tile, int b) __attribute__((always_inline)) {
-            const int lane = (int)anew(tid & 63), my_row = wave * RPW + (lane & (RPW - 1));
-            const int32_t token = token0 + tile * T + my_row;
-            if (((token0 + tile * T + wave * RPW + RPW - 1) >> a.shift) - held0 >= 64) {
-                // the entries held reach as far as a tile's step and a wave's rows, whatever the page size
+            const int32_t t0 = token0 + tile * T + wave * RPW;
+            // A wave's eight rows begin a page, or lie in one, or begin a whole number of pages (t0 is a multiple of
+            // eight): they never lie on either side of the 64 entries held.
+            if ((t0 >> a.shift) - held0 >= 64) {
                 held0 += 64;
                 held = behind;
                 behind = entry(held0 + 64 + lane);
             }
-            const int32_t i = (token >> a.shift) - held0;
-            const int32_t page = i < 64 ? __shfl(held, i & 63, 64) : -1;
-            const bool there = token >= first && token < token1 && (uint32_t)page < (uint64_t)a.pages;
-            const unsigned char *row = there ? kh + page * a.k_page + (token & in_page) * a.k_token : reinterpret_cast<const unsigned char *>(zero_row);
-            if (lane < RPW) s_mask[b][my_row] = there ? 0.0f : -INFINITY;
-            if (FMT == CRAFT_KV_E4M3)
-                from[kRequests - 1] = reinterpret_cast<ubase_t>(there ? a.k_scale + ((((int64_t)page * a.heads + h) << a.shift) + (token & in_page)) : reinterpret_cast<const float *>(zero_row));
-            const uint32_t lo = (uint32_t)(uintptr_t)row, hi = (uint32_t)((uintptr_t)row >> 32);
             to_main = lds0 + b * BUF + wave * RPW * RB;
             to_rest = lds0 + b * BUF + T * RB + wave * RPW * TB;
+            to_scale = scale0 + (b * T + wave * RPW) * 4;
+            const int32_t page0 = __builtin_amdgcn_readlane(held, ((t0 >> a.shift) - held0) & 63);
+            later = whole_rows && t0 >= first && t0 + RPW <= token1 && (uint32_t)page0 < (uint64_t)a.pages;
+            if (later) {
+                from = kh + page0 * a.k_page + (t0 & in_page) * a.k_token;
+                if (FMT == CRAFT_KV_E4M3) from_scale = reinterpret_cast<ubase_t>(a.k_scale + ((((int64_t)page0 * a.heads + h) << a.shift) + (t0 & in_page)));
+                if (lane < RPW) s_mask[b][wave * RPW + lane] = 0.0f;
+                return;
+            }
+            const int lane = (int)anew(tid & 63), my_row = lane & (RPW - 1);
+            const int32_t token = t0 + my_row;
+            const int32_t page = __shfl(held, ((token >> a.shift) - held0) & 63, 64);
+            const bool there = token >= first && token < token1 && (uint32_t)page < (uint64_t)a.pages;
+            const unsigned char *row = there ? kh + page * a.k_page + (token & in_page) * a.k_token : reinterpret_cast<const unsigned char *>(zero_row);
+            if (lane < RPW) s_mask[b][wave * RPW + lane] = there ? 0.0f : -INFINITY;
+            const uint32_t lo = (uint32_t)(uintptr_t)row, hi = (uint32_t)((uintptr_t)row >> 32);
+            // what a row lacks at its end is zeros
+            auto piece_at = [&](int from, int piece) {
+                const ubase_t base = reinterpret_cast<ubase_t>((uint64_t)(uint32_t)__shfl((int)hi, from, 64) << 32 | (uint32_t)__shfl((int)lo, from, 64));
+                return (piece < pieces ? base : reinterpret_cast<ubase_t>(zero_row)) + piece * 16;
+            };
             const int rest_row = FMT == CRAFT_KV_BF16 ? lane >> 3 : lane >> 2 & (RPW - 1);
             const int rest_piece = kLanes + ((lane & (FMT == CRAFT_KV_BF16 ? 7 : 3)) ^ rest_place_of<FMT>(wave * RPW + rest_row));
-            if (a.shift >= 3 && pieces == 72 / kRows && __all(there)) {
-                // eight rows of a page: one address and the distance between rows
-                ubase_t base = reinterpret_cast<ubase_t>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)hi) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)lo));
-                const uint32_t step = (uint32_t)a.k_token;
-                from[0] = base + ((uint32_t)rest_row * step + rest_piece * 16);
+            const ubase_t rest = piece_at(rest_row, rest_piece);
+            if (FMT == CRAFT_KV_BF16 || lane < 4 * RPW) dma_chunk_at(rest, to_rest);
 #pragma unroll
-                for (int i = 0; i < RPW; i += kRows) {
-                    const int in = FMT == CRAFT_KV_BF16 ? 0 : lane >> 5;
-                    from[1 + i / kRows] = base + ((uint32_t)(i + in) * step + ((lane & (kLanes - 1)) ^ place_of<FMT>(wave * RPW + i + in)) * 16);
-                }
-            } else {
-                // what a row lacks at its end is zeros
-                auto piece_at = [&](int from, int piece) {
-                    const ubase_t base = reinterpret_cast<ubase_t>((uint64_t)(uint32_t)__shfl((int)hi, from, 64) << 32 | (uint32_t)__shfl((int)lo, from, 64));
-                    return (piece < pieces ? base : reinterpret_cast<ubase_t>(zero_row)) + piece * 16;
-                };
-                from[0] = piece_at(rest_row, rest_piece);
-#pragma unroll
-                for (int i = 0; i < RPW; i += kRows) {
-                    const int in = FMT == CRAFT_KV_BF16 ? 0 : lane >> 5;
-                    from[1 + i / kRows] = piece_at(i + in, (lane & (kLanes - 1)) ^ place_of<FMT>(wave * RPW + i + in));
-                }
+            for (int i = 0; i < RPW; i += kRows) {
+                const int in = FMT == CRAFT_KV_BF16 ? 0 : lane >> 5;
+                dma_chunk_at(piece_at(i + in, (lane & (kLanes - 1)) ^ place_of<FMT>(wave * RPW + i + in)), to_main + i * RB);
+            }
+            if (FMT == CRAFT_KV_E4M3) {
+                const float *scale = there ? a.k_scale + ((((int64_t)page * a.heads + h) << a.shift) + (token & in_page)) : reinterpret_cast<const float *>(zero_row);
+                if (lane < RPW) dma_word_at(reinterpret_cast<ubase_t>(scale), to_scale);
             }
         };
-        auto ask = [&](int i, int b) __attribute__((always_inline)) {
-            if (i >= 1 && i <= RPW / kRows) {
-                dma_chunk_at(from[i], to_main + (i - 1) * kRows * RB);
-            } else if (i == 0) {
-                if (FMT == CRAFT_KV_BF16 || lane < 4 * RPW) dma_chunk_at(from[0], to_rest);
+        // request i of the planned ones, if they are still to be made
+        auto ask = [&](int i) __attribute__((always_inline)) {
+            if (!later) return;
+            if (i < RPW / kRows) {
+                // the place of row 8 w + i is that of row 8 w and 2 i, exclusive or
+                dma_chunk(from + (uint32_t)(i * kRows) * (uint32_t)a.k_token, (main_off ^ (uint32_t)(i * kRows * 32)) + main_row, to_main + i * kRows * RB);
+            } else if (i == RPW / kRows) {
+                if (FMT == CRAFT_KV_BF16 || lane < 4 * RPW) dma_chunk(from, rest_off, to_rest);
             } else if (i < kRequests && lane < RPW) {
-                dma_word_at(from[kRequests - 1], scale0 + (b * T + wave * RPW) * 4);
+                dma_word(from_scale, lane * 4, to_scale);
             }
         };
 
@@ -199,12 +213,14 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_kernel(AttentionArgs a,
 #pragma unroll
         for (int i = 0; i < S::QN; ++i) asm volatile("" : "+v"(q[i]));
 
+        constexpr int kEvery = FMT == CRAFT_KV_BF16 ? 4 : 2, kBehindScores = (S::NK + kEvery - 1) / kEvery;
+        static_assert(kBehindScores + 4 >= kRequests, "every request goes out behind some products");
         const int32_t tiles = u1 - u0;
         const bool busy = n_heads > 0;
         // every wave's part of a tile has landed, and everybody is done with the tile before the last one
         auto meet = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
         f32x4_t s[2];
-        auto scores = [&](int b, bool more, int next) __attribute__((always_inline)) {
+        auto scores = [&](int b, bool more) __attribute__((always_inline)) {
             const uint32_t rows = lds0 + b * BUF, rest = rows + T * RB;
             // a piece's place in its 256 bytes is exclusive-or'ed into the address of the lane's first one
             const uint32_t key0 = anew(rows + key_at), key1 = FMT == CRAFT_KV_E4M3 ? key0 ^ 16 : key0, rest0 = anew(rest + rest_at);
@@ -233,7 +249,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_kernel(AttentionArgs a,
                         const bf16x8_t kf = FMT == CRAFT_KV_BF16 ? __builtin_bit_cast(bf16x8_t, kc) : widen((u32x2_t){kc[2 * e], kc[2 * e + 1]});
                         s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, __builtin_bit_cast(bf16x8_t, q[FMT == CRAFT_KV_E4M3 ? 2 * key_step(i) + e : key_step(i)]), s[t], 0, 0, 0);
                     }
-                if (more && i % (S::NK / kRequests) == 0) ask(i / (S::NK / kRequests), next);
+                if (more && i % kEvery == 0) ask(i / kEvery);
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
@@ -270,7 +286,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_kernel(AttentionArgs a,
         };
         // Values: columns of 16 out of LDS, transposed on the way (a lane gets four, or eight, tokens of its column
         // out of the 8 bytes each that 16 lanes ask for).
-        auto values = [&](int b, bf16x8_t pf) __attribute__((always_inline)) {
+        auto values = [&](int b, bf16x8_t pf, bool more) __attribute__((always_inline)) {
             bf16x8_t vf[kAhead + 1][kStep];
             const uint32_t value0 = anew(lds0 + b * BUF + value_at);
             auto read_values = [&](int step) __attribute__((always_inline)) {
@@ -295,6 +311,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_kernel(AttentionArgs a,
 #pragma unroll
                 for (int c = 0; c < kStep; ++c)
                     z.acc[value_tile(i * kStep + c)][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i % (kAhead + 1)][c], pf, z.acc[value_tile(i * kStep + c)][0], 0, 0, 0);
+                if (more && i % 4 == 1) ask(kBehindScores + i / 4);
             }
         };
         auto rescale = [&]() __attribute__((always_inline)) {
@@ -307,13 +324,13 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_kernel(AttentionArgs a,
         for (int i = 0; i < kBuffers - 1; ++i) {
             plan(i, i);
 #pragma unroll
-            for (int j = 0; j < kRequests; ++j) ask(j, i);
+            for (int j = 0; j < kRequests; ++j) ask(j);
         }
         dma_wait<2 * kRequests>();
         meet();
         bf16x8_t pf = {};
         if (busy) {
-            scores(0, false, 0);
+            scores(0, false);
             pf = weights(0);
         }
         for (int32_t tile = 0; tile + 1 < tiles; ++tile) {
@@ -322,17 +339,17 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_kernel(AttentionArgs a,
             const int next = (tile + 3) % kBuffers;
             plan(tile + 3, next);
             if (busy) {
-                scores((tile + 1) % kBuffers, true, next);
+                scores((tile + 1) % kBuffers, true);
                 const bf16x8_t pn = weights((tile + 1) % kBuffers);
-                values(tile % kBuffers, pf);
+                values(tile % kBuffers, pf, true);
                 rescale();
                 pf = pn;
             } else {
 #pragma unroll
-                for (int j = 0; j < kRequests; ++j) ask(j, next);
+                for (int j = 0; j < kRequests; ++j) ask(j);
             }
         }
-        if (busy) values((tiles - 1) % kBuffers, pf);
+        if (busy) values((tiles - 1) % kBuffers, pf, false);
         dma_wait<0>();
         meet();                                    // the buffers are free for the next item
 
