@@ -483,6 +483,15 @@ class RankForward:
 
 # ---------------------------------------------------------- paged key/value cache
 
+def _stream_on(t, stream):
+    """The stream to launch on: the one given, or the current one of the tensor's device.  (Asked for by number: the
+    Stream object costs three microseconds, as much as a whole launch.)"""
+    if stream is not None:
+        return stream.cuda_stream
+    import torch
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
+
+
 class KvCache:
     """The paged cache of one layer over tensors that the caller made.
 
@@ -506,6 +515,7 @@ class KvCache:
         for sc in (k_scale, v_scale):
             assert sc is None or (sc.dtype == torch.float32 and tuple(sc.shape) == (pages, heads, page_size) and sc.is_contiguous())
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._int32 = torch.int32
         self.pages, self.heads, self.page_size, self.dk, self.dv = pages, heads, page_size, dk, dv
         self.dtype = torch.bfloat16 if eight else k.dtype          # of queries, new rows and outputs
         d = KvCacheDesc()
@@ -515,7 +525,7 @@ class KvCache:
             d.v, (d.v_page, d.v_head, d.v_token) = v.data_ptr(), self._strides(v)
         d.k_scale = k_scale.data_ptr() if k_scale is not None else None
         d.v_scale = v_scale.data_ptr() if v_scale is not None else None
-        self.desc = d
+        self.desc, self._ref, self._append = d, ctypes.byref(d), lib().craft_kv_append
 
     @staticmethod
     def _strides(t):
@@ -538,20 +548,23 @@ class KvCache:
     def append(self, k, v, slots, stream=None):
         """k: cuda [T][heads][dk], v: [T][heads][dv] (None for latent rows), of the cache's `dtype`, the heads of a
         token contiguous; slots: cuda int32 [T], negative ones skipped."""
-        import torch
         T = slots.shape[0]
-        assert slots.dtype == torch.int32 and slots.is_cuda and slots.is_contiguous()
+        assert slots.dtype == self._int32 and slots.is_cuda and slots.dim() == 1 and (T < 2 or slots.stride(0) == 1)
         row_k = self._rows(k, T, self.dk)
-        row_v = self._rows(v, T, self.dv) if self.v is not None else 0
-        assert self.v is not None or v is None
-        _check(lib().craft_kv_append(ctypes.byref(self.desc), T, c_vp(k.data_ptr()), row_k,
-                                     c_vp(v.data_ptr()) if v is not None else None, row_v, c_vp(slots.data_ptr()), _stream_ptr(stream)),
-               "craft_kv_append")
+        if self.v is None:
+            assert v is None
+            rc = self._append(self._ref, T, k.data_ptr(), row_k, None, 0, slots.data_ptr(), _stream_on(slots, stream))
+        else:
+            row_v = self._rows(v, T, self.dv)
+            rc = self._append(self._ref, T, k.data_ptr(), row_k, v.data_ptr(), row_v, slots.data_ptr(), _stream_on(slots, stream))
+        if rc:
+            _check(rc, "craft_kv_append")
 
     def _rows(self, t, T, d):
-        assert t.is_cuda and t.dtype == self.dtype and tuple(t.shape) == (T, self.heads, d)
-        assert (d == 1 or t.stride(2) == 1) and (self.heads == 1 or t.stride(1) == d)
-        return t.stride(0) if T > 1 else self.heads * d
+        assert t.dtype == self.dtype and t.is_cuda and t.shape == (T, self.heads, d)
+        row, head, one = t.stride()
+        assert one == 1 and (self.heads == 1 or head == d)
+        return row if T > 1 else self.heads * d
 
 
 class KvTables:
@@ -586,19 +599,19 @@ class KvTables:
         _check(lib().craft_kv_tables_workspace(ctypes.byref(a), n), "craft_kv_tables_workspace")
         self.workspace = torch.empty(n.value, dtype=torch.uint8, device=dev)
         a.workspace, a.workspace_bytes = self.workspace.data_ptr(), n.value
-        self.args = a
+        self.args, self._ref, self._step = a, ctypes.byref(a), lib().craft_kv_tables
 
     def step(self, add, lens_out=None, pool_out=None, stream=None):
         """add: cuda int32 [requests], new tokens per request, negative: it has ended.  The new lengths and pool
         counters replace the old ones, or go to `lens_out` and `pool_out`.  Returns slots."""
-        import torch
         lens_out, pool_out = self.lens if lens_out is None else lens_out, self.pool if pool_out is None else pool_out
-        assert add.is_cuda and add.dtype == torch.int32 and add.shape == self.lens.shape and add.is_contiguous()
-        assert lens_out.dtype == torch.int32 and lens_out.shape == self.lens.shape and lens_out.is_contiguous()
-        assert pool_out.dtype == torch.int64 and pool_out.shape == self.pool.shape and pool_out.is_contiguous()
+        for t, like in ((add, self.lens), (lens_out, self.lens), (pool_out, self.pool)):
+            assert t is like or (t.dtype == like.dtype and t.is_cuda and t.shape == like.shape and t.is_contiguous())
         a = self.args
         a.add, a.lens_out, a.pool_out = add.data_ptr(), lens_out.data_ptr(), pool_out.data_ptr()
-        _check(lib().craft_kv_tables(ctypes.byref(a), _stream_ptr(stream)), "craft_kv_tables")
+        rc = self._step(self._ref, _stream_on(add, stream))
+        if rc:
+            _check(rc, "craft_kv_tables")
         return self.slots
 
 
@@ -621,22 +634,26 @@ class DecodeAttention:
         _check(lib().craft_decode_attention_workspace(ctypes.byref(cache.desc), ctypes.byref(a), n), "craft_decode_attention_workspace")
         self.workspace = torch.zeros(n.value, dtype=torch.uint8, device=dev)       # the counters in it start at zero
         a.workspace, a.workspace_bytes = self.workspace.data_ptr(), n.value
-        self.args = a
+        self.args, self._ref, self._cache_ref, self._call = a, ctypes.byref(a), ctypes.byref(cache.desc), lib().craft_decode_attention
+        self._int32, self._q_shape, self._table_shape = torch.int32, (requests, query_heads, cache.dk), (requests, max_pages)
 
     def __call__(self, q, lens, table, stream=None):
         """q: cuda [requests][query_heads][dk]; lens: int32 [requests]; table: int32 [requests][max_pages].  Returns
         the (reused) output tensor."""
-        import torch
-        assert q.is_cuda and q.dtype == self.cache.dtype and tuple(q.shape) == (self.R, self.Hq, self.cache.dk) and q.stride(2) == 1
-        assert lens.is_cuda and lens.dtype == torch.int32 and tuple(lens.shape) == (self.R,) and lens.is_contiguous()
-        assert table.is_cuda and table.dtype == torch.int32 and tuple(table.shape) == (self.R, self.max_pages)
-        assert self.max_pages == 1 or table.stride(1) == 1
+        assert q.is_cuda and q.dtype == self.cache.dtype and q.shape == self._q_shape
+        assert lens.is_cuda and lens.dtype == self._int32 and lens.shape == self._q_shape[:1] and (self.R < 2 or lens.stride(0) == 1)
+        assert table.is_cuda and table.dtype == self._int32 and table.shape == self._table_shape
+        row, head, one = q.stride()
+        table_row, entry = table.stride()
+        assert one == 1 and (entry == 1 or self.max_pages == 1)
         a = self.args
         a.q, a.lens, a.table = q.data_ptr(), lens.data_ptr(), table.data_ptr()
-        a.q_head_stride = q.stride(1) if self.Hq > 1 else self.cache.dk
-        a.q_stride = q.stride(0) if self.R > 1 else self.Hq * self.cache.dk
-        a.table_stride = table.stride(0) if self.R > 1 else self.max_pages
-        _check(lib().craft_decode_attention(ctypes.byref(self.cache.desc), ctypes.byref(a), _stream_ptr(stream)), "craft_decode_attention")
+        a.q_head_stride = head if self.Hq > 1 else self.cache.dk
+        a.q_stride = row if self.R > 1 else self.Hq * self.cache.dk
+        a.table_stride = table_row if self.R > 1 else self.max_pages
+        rc = self._call(self._cache_ref, self._ref, _stream_on(q, stream))
+        if rc:
+            _check(rc, "craft_decode_attention")
         return self.out
 
 
