@@ -3,11 +3,11 @@
 // Tables.  With n the tokens a request has, a the ones it gets and P the tokens of a page, it takes
 // need = ceil((n + a) / P) - ceil(n / P) pages.  Three prefix sums over the requests (tokens, pages taken,
 // pages given back) decide who is served and give every token and page its place: one workgroup does them.
-// What follows is independent per token: the request is found by binary search among the token offsets,
-// the page comes out of the table or, for a new page, out of the ring of free pages, and the token that is
-// first on its page writes the table entry.  The bytes are next to nothing; a step is a chain of a few
-// dependent round trips (lengths, ring, slots).  So a small step is one launch, everything in LDS; a large
-// one fills in a second launch on many CUs.
+// What follows is independent per token: its page comes out of the table or, for a new page, out of the ring of
+// free pages, and the token that is first on its page writes the table entry.  The bytes are next to nothing; a
+// step is a chain of a few dependent round trips (lengths, ring, slots).  So a small step is one launch, and where
+// no request gets more than one token, as in decoding, its thread writes it; otherwise a token's request is found
+// by binary search among the token offsets in LDS.  A large step fills in a second launch on many CUs.
 //
 // Writes.  Bound by HBM: every row read once and written once, 16 bytes per lane.  In 8 bits the lanes of a
 // row share its maximum (codes and scales as of expert weights).
@@ -21,18 +21,42 @@ namespace {
 
 // ------------------------------------------------------------------------ tables
 
-constexpr int kScanThreads = 1024;
-constexpr int kFusedRequests = 1024;              // most requests of a step of one launch: one per thread
+constexpr int kScanThreads = 1024;                // also the most requests of a step of one launch: one per thread
 constexpr int kFillThreads = 256;
-constexpr int kFillTokens = 4;                    // per thread
-constexpr int kFillRequests = 8192;               // most requests whose offsets a filling workgroup keeps in LDS
+constexpr int kFillTokens = 2;                    // per thread
+constexpr int kFillRequests = 4096;               // most requests of which a filling workgroup keeps its own copy
 
-// Prefixes of one request in front of it.
-struct Before {
-    int64_t tokens, need, back;
+// Sums over some requests, in 32 bits that saturate: what exceeds 2^31 exceeds every bound there is.
+struct Counts {
+    uint32_t tokens, need, back;
 };
-__device__ __forceinline__ Before operator+(const Before &a, const Before &b) {
-    return {a.tokens + b.tokens, a.need + b.need, a.back + b.back};
+__device__ __forceinline__ Counts operator+(const Counts &a, const Counts &b) {
+    return {__builtin_elementwise_add_sat(a.tokens, b.tokens), __builtin_elementwise_add_sat(a.need, b.need),
+            __builtin_elementwise_add_sat(a.back, b.back)};
+}
+// x of the lane DPP names, 0 where there is none
+template <int DPP, int ROWS> __device__ __forceinline__ uint32_t lane_of(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, DPP, ROWS, 0xf, false);
+}
+template <int DPP, int ROWS> __device__ __forceinline__ Counts lane_of(const Counts &x) {
+    return {lane_of<DPP, ROWS>(x.tokens), lane_of<DPP, ROWS>(x.need), lane_of<DPP, ROWS>(x.back)};
+}
+// Sums over a wave's lanes up to each: within rows of 16 lanes (shifts by 1, 2, 4, 8), then the last lane of a row
+// to the next one, and of the second row to the upper half.
+__device__ __forceinline__ Counts wave_sums(Counts x) {
+    x = x + lane_of<0x111, 0xf>(x);
+    x = x + lane_of<0x112, 0xf>(x);
+    x = x + lane_of<0x114, 0xf>(x);
+    x = x + lane_of<0x118, 0xf>(x);
+    x = x + lane_of<0x142, 0xa>(x);
+    x = x + lane_of<0x143, 0xc>(x);
+    return x;
+}
+// i mod n for i of either sign
+__device__ __forceinline__ uint32_t ring_place(int64_t i, int64_t n) {
+    if ((uint64_t)i >> 32 == 0) return (uint32_t)i % (uint32_t)n;
+    const int64_t m = i % n;
+    return (uint32_t)(m < 0 ? m + n : m);
 }
 
 struct Request {
@@ -71,110 +95,116 @@ __device__ __forceinline__ void put_token(const KvTablesArgs &a, int32_t t, int3
 }
 
 // The pages of the ended requests among the 64 from r0 on, one request after the other by a whole wave.
-// n, back_off: of request r0 + lane.
-__device__ __forceinline__ void give_back(const KvTablesArgs &a, int32_t r0, bool ended, int32_t n, int64_t back_off, int64_t tail) {
+// n, back_off: of request r0 + lane; tail: the first place behind the free pages.
+__device__ __forceinline__ void give_back(const KvTablesArgs &a, int32_t r0, bool ended, int32_t n, uint32_t back_off, uint32_t tail) {
     const int lane = threadIdx.x & 63;
     unsigned long long m = __ballot(ended && n > 0);
     while (m) {
         const int j = __ffsll((long long)m) - 1;
         m &= m - 1;
         const int32_t have = (int32_t)(((int64_t)__shfl(n, j, 64) + (1ll << a.shift) - 1) >> a.shift);
-        const uint32_t base = (uint32_t)((tail + __shfl(back_off, j, 64)) % a.pages);
+        const uint32_t base = (uint32_t)(((uint64_t)tail + (uint32_t)__shfl((int)back_off, j, 64)) % (uint64_t)a.pages);
         const int32_t *row = a.table + (int64_t)(r0 + j) * a.table_stride;
         for (int32_t c = lane; c < have; c += 64) a.ring[(base + (uint32_t)c) % (uint32_t)a.pages] = row[c];
     }
 }
+__device__ __forceinline__ void no_token(const KvTablesArgs &a, int64_t t) {
+    a.slots[t] = -1;
+    if (a.positions) a.positions[t] = -1;
+}
 
-// FUSED: the whole step in this launch (R <= kFusedRequests).  Otherwise the workspace gets what the filling
-// launch needs: [0] the ring's first free entry, [2..3] its end, then lengths, page offsets and back offsets.
-template <bool FUSED>
-__global__ __launch_bounds__(kScanThreads) void tables_scan_kernel(KvTablesArgs a) {
-    __shared__ Before wave_sum[kScanThreads / 64];
-    __shared__ int64_t wave_most[2][kScanThreads / 64];
-    __shared__ int32_t s_off[FUSED ? kFusedRequests : 1], s_n[FUSED ? kFusedRequests : 1], s_page[FUSED ? kFusedRequests : 1];
+// FUSED: the whole step in this launch, of THREADS requests at most.  Otherwise the workspace gets what the filling
+// launch needs: the ring's first free entry and its end, the number of tokens, then lengths, page and back offsets.
+template <bool FUSED, int THREADS>
+__global__ __launch_bounds__(THREADS) void tables_scan_kernel(KvTablesArgs a) {
+    constexpr int kWaves = THREADS / 64;
+    __shared__ Counts wave_sum[kWaves];
+    __shared__ uint32_t wave_most[kWaves][2], wave_asked[kWaves];
+    __shared__ int32_t s_off[FUSED ? THREADS : 1], s_n[FUSED ? THREADS : 1], s_page[FUSED ? THREADS : 1];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t taken = a.pool[0], returned = a.pool[1];
-    const int64_t spare = min(max(returned - taken, (int64_t)0), a.pages);
-    const int64_t head = ((taken % a.pages) + a.pages) % a.pages, tail = ((returned % a.pages) + a.pages) % a.pages;
     // this thread's requests: a run of `per`
-    const int32_t per = FUSED ? 1 : (a.R + kScanThreads - 1) / kScanThreads;
+    const int32_t per = FUSED ? 1 : (a.R + THREADS - 1) / THREADS;
     const int64_t r0 = (int64_t)tid * per, r1 = min((int64_t)a.R, r0 + per);
-    Before sum = {0, 0, 0};
+    Counts sum = {0, 0, 0};
     Request q = {0, 0, 0, 0, 0};
     int32_t add = 0;
     for (int64_t r = r0; r < r1; ++r) {
         add = a.add[r];
         q = request_of(a, add, a.lens[r]);
-        sum = sum + Before{q.asked, q.need, q.back};
+        sum = sum + Counts{(uint32_t)q.asked, (uint32_t)q.need, (uint32_t)q.back};
     }
-    Before incl = sum;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const Before up = {__shfl_up(incl.tokens, d, 64), __shfl_up(incl.need, d, 64), __shfl_up(incl.back, d, 64)};
-        if (lane >= d) incl = incl + up;
-    }
+    const Counts incl = wave_sums(sum);
     if (lane == 63) wave_sum[wave] = incl;
+    const bool several = __any(q.asked > 1);       // one launch: some request gets more than one token
+    if (FUSED && lane == 0) wave_asked[wave] = several;
+    const uint32_t spare = (uint32_t)min(max(returned - taken, (int64_t)0), a.pages);
+    const uint32_t head = ring_place(taken, a.pages), tail = ring_place(returned, a.pages);
     __syncthreads();
-    Before at = {incl.tokens - sum.tokens, incl.need - sum.need, incl.back - sum.back};
-    int64_t back_total = 0;
+    Counts before = {0, 0, 0}, total = {0, 0, 0};
+    bool search = false;
 #pragma unroll
-    for (int w = 0; w < kScanThreads / 64; ++w) {
-        if (w < wave) at = at + wave_sum[w];
-        back_total += wave_sum[w].back;
+    for (int w = 0; w < kWaves; ++w) {
+        if (w == wave) before = total;
+        total = total + wave_sum[w];
+        if (FUSED) search = search || wave_asked[w];
     }
-    // what the served ones get: prefixes only grow, so the served requests that ask for anything are the first few
-    int64_t tokens = 0, pages = 0;
-    {
-        Before b = at;
+    // the sums in front of this thread's requests: of the waves before, and of the lanes before
+    before = before + lane_of<0x138, 0xf>(incl);
+    uint32_t tokens = total.tokens, pages = total.need;
+    if (total.need > spare || total.tokens > (uint32_t)a.max_new) {
+        // Not all are served.  Sums only grow, so those that ask for anything and are served are the first few.
+        tokens = pages = 0;
+        Counts b = before;
         for (int64_t r = r0; r < r1; ++r) {
             const Request p = FUSED ? q : request_of(a, a.add[r], a.lens[r]);
-            b = b + Before{p.asked, p.need, p.back};
-            if (b.need <= spare && b.tokens <= a.max_new) {
+            b = b + Counts{(uint32_t)p.asked, (uint32_t)p.need, (uint32_t)p.back};
+            if (b.need <= spare && b.tokens <= (uint32_t)a.max_new) {
                 tokens = b.tokens;
                 pages = b.need;
             }
         }
-    }
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        tokens = max(tokens, __shfl_xor(tokens, d, 64));
-        pages = max(pages, __shfl_xor(pages, d, 64));
-    }
-    if (lane == 0) { wave_most[0][wave] = tokens; wave_most[1][wave] = pages; }
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kScanThreads / 64; ++w) {
-        tokens = max(tokens, wave_most[0][w]);
-        pages = max(pages, wave_most[1][w]);
-    }
-    int64_t back_off = at.back;
-    {
-        Before b = at;
-        for (int64_t r = r0; r < r1; ++r) {
-            const int32_t ad = FUSED ? add : a.add[r];
-            const Request p = FUSED ? q : request_of(a, ad, a.lens[r]);
-            const int32_t off = (int32_t)min(b.tokens, tokens), page_off = (int32_t)min(b.need, pages);
-            const bool served = b.need + p.need <= spare && b.tokens + p.asked <= a.max_new;
-            a.token_off[r] = off;
-            // lens_out may be lens: this thread has read its requests, and nobody else reads them
-            a.lens_out[r] = ad < 0 ? 0 : p.n + (served ? p.asked : 0);
-            if (FUSED) {
-                s_off[r] = off;
-                s_n[r] = p.n;
-                s_page[r] = page_off;
-            } else {
-                a.ws_len[r] = p.n;
-                a.ws_page[r] = page_off;
-                a.ws_back[r] = (int32_t)(b.back % a.pages);
-            }
-            b = b + Before{p.asked, p.need, p.back};
+        for (int d = 32; d > 0; d >>= 1) {
+            tokens = max(tokens, (uint32_t)__shfl_xor((int)tokens, d, 64));
+            pages = max(pages, (uint32_t)__shfl_xor((int)pages, d, 64));
         }
+        if (lane == 0) { wave_most[wave][0] = tokens; wave_most[wave][1] = pages; }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            tokens = max(tokens, wave_most[w][0]);
+            pages = max(pages, wave_most[w][1]);
+        }
+    }
+    const uint32_t back_off = before.back;
+    for (int64_t r = r0; r < r1; ++r) {
+        const int32_t ad = FUSED ? add : a.add[r];
+        const Request p = FUSED ? q : request_of(a, ad, a.lens[r]);
+        const Counts here = {(uint32_t)p.asked, (uint32_t)p.need, (uint32_t)p.back}, after = before + here;
+        const int32_t off = (int32_t)min(before.tokens, tokens), page_off = (int32_t)min(before.need, pages);
+        const bool served = after.need <= spare && after.tokens <= (uint32_t)a.max_new;
+        a.token_off[r] = off;
+        // lens_out may be lens: this thread has read its requests, and nobody else reads them
+        a.lens_out[r] = ad < 0 ? 0 : p.n + (served ? p.asked : 0);
+        if (!FUSED) {
+            a.ws_len[r] = p.n;
+            a.ws_page[r] = page_off;
+            a.ws_back[r] = (int32_t)before.back;
+        } else if (!search) {
+            if (served && p.asked) put_token(a, off, (int32_t)r, off, p.n, page_off, head);
+        } else {
+            s_off[r] = off;
+            s_n[r] = p.n;
+            s_page[r] = page_off;
+        }
+        before = after;
     }
     if (tid == 0) {
         a.token_off[a.R] = (int32_t)tokens;
-        // every thread has read the counters before the barriers above
+        // every thread has read the counters before the barrier above
         a.pool_out[0] = taken + pages;
-        a.pool_out[1] = returned + back_total;
+        a.pool_out[1] = returned + total.back;
         if (!FUSED) {
             a.ws_ctrl[0] = (int32_t)head;
             a.ws_ctrl[1] = (int32_t)tail;
@@ -182,44 +212,46 @@ __global__ __launch_bounds__(kScanThreads) void tables_scan_kernel(KvTablesArgs 
         }
     }
     if (FUSED) {
-        __syncthreads();
-        for (int32_t t = tid; t < a.max_new; t += kScanThreads) {
-            if (t < tokens) {
+        if (search) {
+            __syncthreads();
+            for (int32_t t = tid; t < (int32_t)tokens; t += THREADS) {
                 int32_t lo = 0, hi = a.R;          // the last request that starts at t or before
                 while (hi - lo > 1) {
                     const int32_t mid = (lo + hi) >> 1;
                     if (s_off[mid] <= t) lo = mid; else hi = mid;
                 }
-                put_token(a, t, lo, s_off[lo], s_n[lo], s_page[lo], (uint32_t)head);
-            } else {
-                a.slots[t] = -1;
-                if (a.positions) a.positions[t] = -1;
+                put_token(a, t, lo, s_off[lo], s_n[lo], s_page[lo], head);
             }
         }
+        for (int64_t t = (int64_t)tokens + tid; t < a.max_new; t += THREADS) no_token(a, t);
         give_back(a, wave * 64, tid < a.R && add < 0, q.n, back_off, tail);
     }
 }
 
 // Workgroups below `token_groups` take kFillTokens tokens a thread; the others give back the pages of 256
-// requests each.  SEARCH_LDS: the token offsets fit there.
-template <bool SEARCH_LDS>
+// requests each.  IN_LDS: what the tokens need of the requests fits there.
+template <bool IN_LDS>
 __global__ __launch_bounds__(kFillThreads) void tables_fill_kernel(KvTablesArgs a, int32_t token_groups) {
-    __shared__ int32_t s_off[SEARCH_LDS ? kFillRequests : 1];
+    constexpr int kRoom = IN_LDS ? kFillRequests : 1;
+    __shared__ int32_t s_off[kRoom], s_n[kRoom], s_page[kRoom];
     if ((int32_t)blockIdx.x >= token_groups) {
         const int64_t r = (int64_t)(blockIdx.x - token_groups) * kFillThreads + threadIdx.x;
         const bool live = r < a.R;
         const int32_t add = live ? a.add[r] : 0, n = live ? a.ws_len[r] : 0, back = live ? a.ws_back[r] : 0;
-        give_back(a, (int32_t)(r - (threadIdx.x & 63)), add < 0, n, back, a.ws_ctrl[1]);
+        give_back(a, (int32_t)(r - (threadIdx.x & 63)), add < 0, n, (uint32_t)back, (uint32_t)a.ws_ctrl[1]);
         return;
+    }
+    if (IN_LDS) {
+        for (int32_t i = threadIdx.x; i < a.R; i += kFillThreads) {
+            s_off[i] = a.token_off[i];
+            s_n[i] = a.ws_len[i];
+            s_page[i] = a.ws_page[i];
+        }
     }
     const int32_t tokens = a.ws_ctrl[2];
     const uint32_t head = (uint32_t)a.ws_ctrl[0];
+    if (IN_LDS) __syncthreads();
     const int64_t t0 = (int64_t)blockIdx.x * (kFillThreads * kFillTokens) + threadIdx.x;
-    if (SEARCH_LDS) {
-        if ((int64_t)blockIdx.x * (kFillThreads * kFillTokens) < tokens)
-            for (int32_t i = threadIdx.x; i < a.R; i += kFillThreads) s_off[i] = a.token_off[i];
-        __syncthreads();
-    }
 #pragma unroll
     for (int i = 0; i < kFillTokens; ++i) {
         const int64_t t = t0 + i * kFillThreads;
@@ -228,12 +260,12 @@ __global__ __launch_bounds__(kFillThreads) void tables_fill_kernel(KvTablesArgs 
             int32_t lo = 0, hi = a.R;
             while (hi - lo > 1) {
                 const int32_t mid = lo + ((hi - lo) >> 1);
-                if ((SEARCH_LDS ? s_off[mid] : a.token_off[mid]) <= t) lo = mid; else hi = mid;
+                if ((IN_LDS ? s_off[mid] : a.token_off[mid]) <= t) lo = mid; else hi = mid;
             }
-            put_token(a, (int32_t)t, lo, SEARCH_LDS ? s_off[lo] : a.token_off[lo], a.ws_len[lo], a.ws_page[lo], head);
+            if (IN_LDS) put_token(a, (int32_t)t, lo, s_off[lo], s_n[lo], s_page[lo], head);
+            else put_token(a, (int32_t)t, lo, a.token_off[lo], a.ws_len[lo], a.ws_page[lo], head);
         } else {
-            a.slots[t] = -1;
-            if (a.positions) a.positions[t] = -1;
+            no_token(a, t);
         }
     }
 }
@@ -313,11 +345,15 @@ void launch_e4m3(const KvAppendArgs &a, hipStream_t s) {
 constexpr int32_t kFusedTokens = 4096;
 
 hipError_t launch_kv_tables(const KvTablesArgs &a, hipStream_t s) {
-    if (a.R <= kFusedRequests && a.max_new <= kFusedTokens) {
-        hipLaunchKernelGGL(tables_scan_kernel<true>, dim3(1), dim3(kScanThreads), 0, s, a);
+    if (a.R <= 256 && a.max_new <= kFusedTokens / 4) {
+        hipLaunchKernelGGL((tables_scan_kernel<true, 256>), dim3(1), dim3(256), 0, s, a);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL(tables_scan_kernel<false>, dim3(1), dim3(kScanThreads), 0, s, a);
+    if (a.R <= kScanThreads && a.max_new <= kFusedTokens) {
+        hipLaunchKernelGGL((tables_scan_kernel<true, kScanThreads>), dim3(1), dim3(kScanThreads), 0, s, a);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((tables_scan_kernel<false, kScanThreads>), dim3(1), dim3(kScanThreads), 0, s, a);
     const int64_t token_groups = ((int64_t)a.max_new + kFillThreads * kFillTokens - 1) / (kFillThreads * kFillTokens);
     const int64_t back_groups = ((int64_t)a.R + kFillThreads - 1) / kFillThreads;
     const dim3 grid((unsigned)(token_groups + back_groups));
