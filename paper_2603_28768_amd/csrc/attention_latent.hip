@@ -26,8 +26,14 @@ constexpr int kMinRun = 8;                         // of a workgroup, where ther
 __device__ const uint4 zero_row[72] = {};          // 1152 bytes
 
 // four bytes per lane
-static __device__ __forceinline__ void dma_word(ubase_t base, uint32_t off, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" :: "s"(lds), "v"(off), "s"(base) : "memory");
+// The same by the lanes of a mask, between instructions that all lanes run: no branch parts the products.
+static __device__ __forceinline__ void dma_chunk_by(uint64_t lanes, ubase_t base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
+                 :: "s"(lds), "v"(off), "s"(base), "s"(lanes) : "memory");
+}
+static __device__ __forceinline__ void dma_word_by(uint64_t lanes, ubase_t base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b64 exec, -1"
+                 :: "s"(lds), "v"(off), "s"(base), "s"(lanes) : "memory");
 }
 static __device__ __forceinline__ void dma_word_at(ubase_t p, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(lds), "v"(p) : "memory");
@@ -184,14 +190,14 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_kernel(AttentionArgs a,
         };
         // request i of the planned ones, if they are still to be made
         auto ask = [&](int i) __attribute__((always_inline)) {
-            if (!later) return;
+            const uint64_t all = later ? ~0ull : 0ull;
             if (i < RPW / kRows) {
                 // the place of row 8 w + i is that of row 8 w and 2 i, exclusive or
-                dma_chunk(from + (uint32_t)(i * kRows) * (uint32_t)a.k_token, (main_off ^ (uint32_t)(i * kRows * 32)) + main_row, to_main + i * kRows * RB);
+                dma_chunk_by(all, from + (uint32_t)(i * kRows) * (uint32_t)a.k_token, (main_off ^ (uint32_t)(i * kRows * 32)) + main_row, to_main + i * kRows * RB);
             } else if (i == RPW / kRows) {
-                if (FMT == CRAFT_KV_BF16 || lane < 4 * RPW) dma_chunk(from, rest_off, to_rest);
-            } else if (i < kRequests && lane < RPW) {
-                dma_word(from_scale, lane * 4, to_scale);
+                dma_chunk_by(FMT == CRAFT_KV_BF16 ? all : all & ((1ull << 4 * RPW) - 1), from, rest_off, to_rest);
+            } else if (i < kRequests) {
+                dma_word_by(all & ((1ull << RPW) - 1), from_scale, lane * 4, to_scale);
             }
         };
 
