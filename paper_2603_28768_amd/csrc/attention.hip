@@ -424,11 +424,22 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
     }
 }
 
-template <int FMT, int DK, int DV, bool AHEAD, int WPS>
+// Workgroups of a CU, by the bytes of a unit's rows (keys and values, padded), that is by what a wave has on its
+// way.  Waves that have 16 KiB each need only be four to a CU, and more of them read less in order: two requests of
+// 100001 and 131072 tokens, 8 heads of 128 in bf16, with one / two workgroups 159 / 170 us.  Shorter rows, which
+// take more instructions for their bytes, need more waves: 250 requests of 1000 to 8000 tokens, 4 heads of 128 in
+// 8 bits, 179 / 151 us.  So do small pages, for their chains of lookups: the former with pages of 8 211 / 183 us.
+constexpr int groups_of(int format, int dim, bool small) {
+    const int unit = kUnit * 2 * dim * (format == CRAFT_KV_F32 ? 4 : format == CRAFT_KV_BF16 ? 2 : 1);
+    return unit >= 65536 ? 1 : small ? 2 : unit >= 16384 ? 1 : unit >= 8192 ? 2 : 4;
+}
+
+template <int FMT, int D>
 void launch(const AttentionArgs &a, int32_t blocks, hipStream_t s) {
+    constexpr int DK = D, DV = D == 576 ? 512 : D;
     const dim3 grid((unsigned)a.workers), block(kThreads);
-    if (a.shift < 4) hipLaunchKernelGGL((decode_kernel<FMT, DK, DV, true, AHEAD, WPS>), grid, block, 0, s, a, blocks);
-    else hipLaunchKernelGGL((decode_kernel<FMT, DK, DV, false, AHEAD, WPS>), grid, block, 0, s, a, blocks);
+    if (a.shift < 4) hipLaunchKernelGGL((decode_kernel<FMT, DK, DV, true, D != 576, groups_of(FMT, D, true)>), grid, block, 0, s, a, blocks);
+    else hipLaunchKernelGGL((decode_kernel<FMT, DK, DV, false, D != 576, groups_of(FMT, D, false)>), grid, block, 0, s, a, blocks);
 }
 
 int padded_dim(const AttentionArgs &a) {
@@ -439,11 +450,11 @@ int padded_dim(const AttentionArgs &a) {
 template <int FMT>
 void launch_format(const AttentionArgs &a, int32_t blocks, hipStream_t s) {
     switch (padded_dim(a)) {
-    case 64: launch<FMT, 64, 64, true, 2>(a, blocks, s); break;
-    case 128: launch<FMT, 128, 128, true, 2>(a, blocks, s); break;
-    case 256: launch<FMT, 256, 256, FMT != CRAFT_KV_F32, 2>(a, blocks, s); break;
+    case 64: launch<FMT, 64>(a, blocks, s); break;
+    case 128: launch<FMT, 128>(a, blocks, s); break;
+    case 256: launch<FMT, 256>(a, blocks, s); break;
     default:
-        if constexpr (FMT == CRAFT_KV_F32) launch<FMT, 576, 512, false, 1>(a, blocks, s);
+        if constexpr (FMT == CRAFT_KV_F32) launch<FMT, 576>(a, blocks, s);
         break;
     }
 }
@@ -456,7 +467,7 @@ bool wide_latent(const AttentionArgs &a) { return padded_dim(a) == 576 && a.form
 
 int32_t attention_workers(const AttentionArgs &a, int32_t num_cu) {
     if (wide_latent(a)) return latent_workers(a, num_cu);
-    return std::min(kCounters, (padded_dim(a) == 576 ? 1 : 2) * num_cu);
+    return std::min(kCounters, groups_of(a.format, padded_dim(a), a.shift < 4) * num_cu);
 }
 
 size_t attention_counters_bytes() { return 3 * kCounters * sizeof(int32_t); }
