@@ -488,7 +488,7 @@ craft_status craft_kv_append(const craft_kv_cache *cache, int64_t T, const void 
 /* Attention of one new token per request over the cache (which holds that token's row already):
  *   s[i] = scale * q . K[i],  out = sum_i softmax(s)[i] V[i]   over the tokens i of the request,
  * the last `window` of them if window > 0.  Query head h reads cache head h / (Hq / heads).
- *   q       DEVICE [R][Hq][dk], a request every q_stride elements, a head every q_head_stride
+ *   q       DEVICE [R][Hq][dk], a request every q_stride elements, a head every q_head_stride (< 2^24)
  *   lens    DEVICE [R] int32; 0 or less (a place of the batch that is not in use): out is zeros, lse
  *           -infinity.  A length over max_pages * page_size counts as that
  *   table   DEVICE [R][table_stride] int32.  Tokens whose page is outside [0, pages) are left out

@@ -39,6 +39,7 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kItemCost = 2;                       // what an item costs beside its units
+constexpr int kWholeUnits = 24;                    // of an item that is left to one workgroup, where those suffice for all
 constexpr int kMinRun = 2;                         // of a wave, where there is little to do
 
 template <int NV, int CE, bool F32>
@@ -67,15 +68,38 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int32_t per_request = a.heads * blocks, rank = blockIdx.x * kWaves + wave;
-    Runs runs;
-    const Start st = find_start<kWaves, kWaves>(a, per_request, kItemCost, a.workers * kWaves, kMinRun, blockIdx.x * kWaves, runs);
-    if ((int32_t)blockIdx.x * kWaves >= runs.n) return;
-    int64_t at = 0, end = 0, before = st.before;
-    if (rank < runs.n) {
-        at = runs.start(rank);
-        end = runs.start(rank + 1);
+    Runs runs = {};
+    int64_t at = 0, end = 0, before = 0;
+    int32_t r = 0, len = 0;
+    // Few short items: a workgroup for each, and nothing to be joined.  Its table entries can be asked for at once.
+    const int64_t items = (int64_t)a.R * per_request;
+    bool whole_items = a.R <= kThreads && items <= a.workers;
+    int32_t early = 0;
+    if (whole_items) {
+        r = min((int32_t)(blockIdx.x / (uint32_t)per_request), a.R - 1);
+        early = a.table[(int64_t)r * a.table_stride + min(lane, a.max_pages - 1)];
+        int32_t most = 0;
+        for (int32_t i = lane; i < a.R; i += 64) most = max(most, units_of(a, length_of(a, i)));
+        whole_items = __all(most <= kWholeUnits);
     }
-    int32_t r = st.request, len = st.len;
+    if (whole_items) {
+        if (blockIdx.x >= items) return;
+        len = uniform(length_of(a, r));
+        const int32_t units = units_of(a, len), item = (int32_t)(blockIdx.x % (uint32_t)per_request);
+        const int64_t begin = (int64_t)item * (units + kItemCost);
+        at = begin + (wave > 0 ? kItemCost + units * wave / kWaves : 0);
+        end = begin + kItemCost + units * (wave + 1) / kWaves;
+    } else {
+        const Start st = find_start<kWaves, kWaves>(a, per_request, kItemCost, a.workers * kWaves, kMinRun, blockIdx.x * kWaves, runs);
+        if ((int32_t)blockIdx.x * kWaves >= runs.n) return;
+        if (rank < runs.n) {
+            at = runs.start(rank);
+            end = runs.start(rank + 1);
+        }
+        before = st.before;
+        r = st.request;
+        len = st.len;
+    }
     if (lane == 0) s_found[wave] = kNone;
     if (tid < 2) s_cut[tid].mine = 0;
     State z;
@@ -109,12 +133,12 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
         {
             const bool live = col < n_heads;
             constexpr int QB = FMT == CRAFT_KV_F32 ? 4 : 2, QE = 16 / QB;     // bytes of an element, elements of a piece
-            const unsigned char *qr = static_cast<const unsigned char *>(a.q) + ((int64_t)here.request * a.q_stride + (int64_t)(head0 + (live ? col : 0)) * a.q_head) * QB;
-            const u32x4_t none = {0u, 0u, 0u, 0u};
+            const __amdgpu_buffer_rsrc_t qr = rows_of(static_cast<const unsigned char *>(a.q) + ((int64_t)here.request * a.q_stride + (int64_t)head0 * a.q_head) * QB, kFar);
+            const uint32_t q_off = (uint32_t)col * (uint32_t)a.q_head * QB;
 #pragma unroll
             for (int i = 0; i < S::QN; ++i) {
                 const int d = FMT == CRAFT_KV_E4M3 ? (i >> 1) * 64 + g * 16 + (i & 1) * 8 : i * 4 * QE + g * QE;
-                q[i] = live && d < a.dk ? *reinterpret_cast<const u32x4_t *>(qr + d * QB) : none;
+                q[i] = __builtin_amdgcn_raw_buffer_load_b128(qr, live && d < a.dk ? q_off + d * QB : kFar, 0, 0);
             }
         }
 
@@ -133,7 +157,13 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
         auto entry = [&](int32_t i) -> int32_t { return table[min(i, a.max_pages - 1)]; };
         // a wave holds the next 64 entries of the table, and the 64 behind them
         int32_t held0 = ((unit_base + u0) * kUnit) >> a.shift;
-        int32_t held = SMALL ? 0 : entry(held0 + lane), behind = SMALL ? 0 : entry(held0 + 64 + lane);
+        int32_t held = early, behind = 0;
+        if (whole_items && ((unit_base + u1) * kUnit - 1) >> a.shift < 64) {
+            held0 = 0;
+        } else if (!SMALL) {
+            held = entry(held0 + lane);
+            behind = entry(held0 + 64 + lane);
+        }
         auto pages_of = [&](int32_t u, bool live) -> Pages<SMALL> {
             Pages<SMALL> pg;
             if constexpr (SMALL) {
@@ -370,6 +400,7 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
     if (open) {
         bool ended = false;
         for (int w = wave + 1; w < kWaves && !ended; ++w) {
+            if (s_found[w] == kNone) continue;
             z.add(s_sums[w], lane);
             ended = s_found[w] == kEnded;
         }

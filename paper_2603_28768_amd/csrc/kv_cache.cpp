@@ -197,7 +197,7 @@ craft_status craft_decode_attention(const craft_kv_cache *cache, const craft_att
     if (a.R == 0) return CRAFT_OK;
     const int es = cache->format == CRAFT_KV_F32 ? 4 : 2;
     if (!args->q || !aligned(args->q, 16) || args->q_stride <= 0 || args->q_head_stride < cache->dk) return CRAFT_EINVAL;
-    if (args->q_stride > kFarthest || args->q_head_stride > kFarthest || args->q_stride * es % 16 || args->q_head_stride * es % 16)
+    if (args->q_stride > kFarthest || args->q_head_stride >= ((int64_t)1 << 24) || args->q_stride * es % 16 || args->q_head_stride * es % 16)
         return CRAFT_EINVAL;
     if (!args->lens || !args->table || !args->out || !aligned(args->lens, 4) || !aligned(args->table, 4) || !aligned(args->out, 16))
         return CRAFT_EINVAL;
