@@ -153,9 +153,10 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
         typename VWords::type vr[8][AHEAD ? S::NV : 1];
         f32x4_t ks[2], vs[2], vs_next[2];
 
-        auto checked = [&](int32_t page) -> int32_t { return (uint32_t)page < (uint64_t)a.pages ? page : -1; };
+        auto checked = [&](int32_t page) -> int32_t { return (uint32_t)page < (uint32_t)a.pages ? page : -1; };
         auto entry = [&](int32_t i) -> int32_t { return table[min(i, a.max_pages - 1)]; };
-        // a wave holds the next 64 entries of the table, and the 64 behind them
+        // A wave holds 64 entries of the table and the 64 behind them.  They are renewed between runs of units that
+        // need no others: a request for them among the units' would have its wait among theirs.
         int32_t held0 = ((unit_base + u0) * kUnit) >> a.shift;
         int32_t held = early, behind = 0;
         if (whole_items && ((unit_base + u1) * kUnit - 1) >> a.shift < 64) {
@@ -181,14 +182,9 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const int32_t token = u * kUnit + t * 16;
-                    int32_t i = (token >> a.shift) - held0;
-                    if (i >= 64) {
-                        held0 += 64;
-                        i -= 64;
-                        held = behind;
-                        behind = entry(held0 + 64 + lane);
-                    }
-                    const int32_t page = checked(__builtin_amdgcn_readlane(held, i & 63));
+                    const int32_t i = (token >> a.shift) - held0;
+                    const int32_t in_held = __builtin_amdgcn_readlane(held, i & 63), in_behind = __builtin_amdgcn_readlane(behind, i & 63);
+                    const int32_t page = checked(i < 64 ? in_held : in_behind);
                     pg.tile[t] = live && token < n ? page : -1;
                 }
             }
@@ -272,114 +268,128 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
         Pages<SMALL> pages = pages_of(unit_base + u0, true);
         load_keys(unit_base + u0, pages);
         load_values(unit_base + u0, pages);
-        for (int32_t i = u0; i < u1; ++i) {
-            const int32_t u = unit_base + i;
-            const bool more = i + 1 < u1;
-            const Pages<SMALL> next = pages_of(u + 1, more);
-            // ---- scores
-            f32x4_t s[2];
+        for (int32_t i = u0; i < u1;) {
+            // up to the first unit whose page is not held; the one behind it is (pages have half a unit at least)
+            const int32_t stop_at = SMALL ? u1 : min(u1, (int32_t)min((int64_t)u1, (((int64_t)held0 + 64) << a.shift) / kUnit - unit_base));
+            for (; i < stop_at; ++i) {
+                const int32_t u = unit_base + i;
+                const bool more = i + 1 < u1;
+                const Pages<SMALL> next = pages_of(u + 1, more);
+                // ---- scores
+                f32x4_t s[2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                s[t] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
+                for (int t = 0; t < 2; ++t) {
+                    s[t] = (f32x4_t){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int c = 0; c < S::NK; ++c) {
-                    const u32x4_t kc = AHEAD ? kr[t][AHEAD ? c : 0] : load_key(u, pages, t, c);
-                    if (FMT == CRAFT_KV_BF16) {
-                        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kc), __builtin_bit_cast(bf16x8_t, q[c]), s[t], 0, 0, 0);
-                    } else if (FMT == CRAFT_KV_E4M3) {
+                    for (int c = 0; c < S::NK; ++c) {
+                        const u32x4_t kc = AHEAD ? kr[t][AHEAD ? c : 0] : load_key(u, pages, t, c);
+                        if (FMT == CRAFT_KV_BF16) {
+                            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kc), __builtin_bit_cast(bf16x8_t, q[c]), s[t], 0, 0, 0);
+                        } else if (FMT == CRAFT_KV_E4M3) {
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const u32x2_t codes = {kc[2 * e], kc[2 * e + 1]};
-                            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(codes), __builtin_bit_cast(bf16x8_t, q[2 * c + e]), s[t], 0, 0, 0);
+                            for (int e = 0; e < 2; ++e) {
+                                const u32x2_t codes = {kc[2 * e], kc[2 * e + 1]};
+                                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(codes), __builtin_bit_cast(bf16x8_t, q[2 * c + e]), s[t], 0, 0, 0);
+                            }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kc[e]), __uint_as_float(q[c][e]), s[t], 0, 0, 0);
                         }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kc[e]), __uint_as_float(q[c][e]), s[t], 0, 0, 0);
                     }
                 }
-            }
-            float x[2][4];
+                float x[2][4];
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[t][j] = s[t][j] * (FMT == CRAFT_KV_E4M3 ? a.scale_log2 * ks[t][j] : a.scale_log2);
-            if (FMT == CRAFT_KV_E4M3) { vs[0] = vs_next[0]; vs[1] = vs_next[1]; }
-            // which of the lane's tokens have a page
-            bool there[8];
-            bool whole = all_seen(u);
+                    for (int j = 0; j < 4; ++j) x[t][j] = s[t][j] * (FMT == CRAFT_KV_E4M3 ? a.scale_log2 * ks[t][j] : a.scale_log2);
+                if (FMT == CRAFT_KV_E4M3) { vs[0] = vs_next[0]; vs[1] = vs_next[1]; }
+                // which of the lane's tokens have a page
+                bool whole = all_seen(u);
+                const Pages<SMALL> seen_pages = pages;
+                auto there = [&](int j) {
+                    if constexpr (SMALL) return seen_pages.value[j] >= 0;
+                    else return seen_pages.tile[j >> 2] >= 0;
+                };
+                if constexpr (SMALL) {
+                    int32_t all = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if constexpr (SMALL) there[j] = pages.value[j] >= 0;
-                else there[j] = pages.tile[j >> 2] >= 0;
-                whole = whole && there[j];
-            }
-            if (SMALL) whole = __all(whole);
-            load_keys(u + 1, next);
-            // ---- weights
-            if (!whole) {
+                    for (int j = 0; j < 8; ++j) all |= seen_pages.value[j];
+                    whole = whole && __all(all >= 0);
+                } else {
+                    whole = whole && (seen_pages.tile[0] | seen_pages.tile[1]) >= 0;
+                }
+                load_keys(u + 1, next);
+                // ---- weights
+                if (!whole) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int32_t token = u * kUnit + t * 16 + 4 * g + j;
+                            if (token < first || token >= n || !there(4 * t + j)) {
+                                x[t][j] = -INFINITY;
+                                if (FMT == CRAFT_KV_E4M3) vs[t][j] = 0.0f;      // the scale of a row never written
+                            }
+                        }
+                }
+                float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
+                top = max_of_head(top);
+                const float base = z.raise(top);
+                float p[2][4];
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const int32_t token = u * kUnit + t * 16 + 4 * g + j;
-                        if (token < first || token >= n || !there[4 * t + j]) {
-                            x[t][j] = -INFINITY;
-                            if (FMT == CRAFT_KV_E4M3) vs[t][j] = 0.0f;      // the scale of a row never written
+                        p[t][j] = __builtin_amdgcn_exp2f(x[t][j] - base);
+                        z.l += p[t][j];
+                        if (FMT == CRAFT_KV_E4M3) p[t][j] *= vs[t][j];
+                    }
+                // ---- values
+                const bool seen = all_seen(u);
+                if (FMT == CRAFT_KV_F32) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int c = 0; c < S::NV; ++c) {
+                                const typename VWords::type vc = AHEAD ? vr[4 * t + j][AHEAD ? c : 0] : load_value(u, pages, seen, t, j, c);
+#pragma unroll
+                                for (int e = 0; e < S::CE; ++e)
+                                    z.acc[c][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word<S::VW>(vc, e)), p[t][j], z.acc[c][e], 0, 0, 0);
+                            }
+                } else {
+                    const wide_t pw = {bf16_pair(p[0][0], p[0][1]), bf16_pair(p[0][2], p[0][3]), bf16_pair(p[1][0], p[1][1]), bf16_pair(p[1][2], p[1][3])};
+                    const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, pw);
+#pragma unroll
+                    for (int c = 0; c < S::NV; ++c) {
+                        typename VWords::type vc[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) vc[j] = AHEAD ? vr[j][AHEAD ? c : 0] : load_value(u, pages, seen, j >> 2, j & 3, c);
+                        // two neighbouring columns at a time: pairs of tokens out of eight words
+#pragma unroll
+                        for (int e = 0; e < S::CE / 2; ++e) {
+                            uint32_t w[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                w[j] = FMT == CRAFT_KV_BF16 ? word<S::VW>(vc[j], e)
+                                       : (e & 1) ? widen_pair<true>(word<S::VW>(vc[j], e >> 1)) : widen_pair<false>(word<S::VW>(vc[j], e >> 1));
+                            const wide_t even = {perm(w[1], w[0], 0x05040100u), perm(w[3], w[2], 0x05040100u), perm(w[5], w[4], 0x05040100u), perm(w[7], w[6], 0x05040100u)};
+                            const wide_t odd = {perm(w[1], w[0], 0x07060302u), perm(w[3], w[2], 0x07060302u), perm(w[5], w[4], 0x07060302u), perm(w[7], w[6], 0x07060302u)};
+                            z.acc[c][2 * e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, even), pf, z.acc[c][2 * e], 0, 0, 0);
+                            z.acc[c][2 * e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, odd), pf, z.acc[c][2 * e + 1], 0, 0, 0);
                         }
                     }
-            }
-            float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
-            top = max_of_head(top);
-            const float base = z.raise(top);
-            float p[2][4];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    p[t][j] = __builtin_amdgcn_exp2f(x[t][j] - base);
-                    z.l += p[t][j];
-                    if (FMT == CRAFT_KV_E4M3) p[t][j] *= vs[t][j];
                 }
-            // ---- values
-            const bool seen = all_seen(u);
-            if (FMT == CRAFT_KV_F32) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int c = 0; c < S::NV; ++c) {
-                            const typename VWords::type vc = AHEAD ? vr[4 * t + j][AHEAD ? c : 0] : load_value(u, pages, seen, t, j, c);
-#pragma unroll
-                            for (int e = 0; e < S::CE; ++e)
-                                z.acc[c][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word<S::VW>(vc, e)), p[t][j], z.acc[c][e], 0, 0, 0);
-                        }
-            } else {
-                const wide_t pw = {bf16_pair(p[0][0], p[0][1]), bf16_pair(p[0][2], p[0][3]), bf16_pair(p[1][0], p[1][1]), bf16_pair(p[1][2], p[1][3])};
-                const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, pw);
-#pragma unroll
-                for (int c = 0; c < S::NV; ++c) {
-                    typename VWords::type vc[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) vc[j] = AHEAD ? vr[j][AHEAD ? c : 0] : load_value(u, pages, seen, j >> 2, j & 3, c);
-                    // two neighbouring columns at a time: pairs of tokens out of eight words
-#pragma unroll
-                    for (int e = 0; e < S::CE / 2; ++e) {
-                        uint32_t w[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            w[j] = FMT == CRAFT_KV_BF16 ? word<S::VW>(vc[j], e)
-                                   : (e & 1) ? widen_pair<true>(word<S::VW>(vc[j], e >> 1)) : widen_pair<false>(word<S::VW>(vc[j], e >> 1));
-                        const wide_t even = {perm(w[1], w[0], 0x05040100u), perm(w[3], w[2], 0x05040100u), perm(w[5], w[4], 0x05040100u), perm(w[7], w[6], 0x05040100u)};
-                        const wide_t odd = {perm(w[1], w[0], 0x07060302u), perm(w[3], w[2], 0x07060302u), perm(w[5], w[4], 0x07060302u), perm(w[7], w[6], 0x07060302u)};
-                        z.acc[c][2 * e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, even), pf, z.acc[c][2 * e], 0, 0, 0);
-                        z.acc[c][2 * e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, odd), pf, z.acc[c][2 * e + 1], 0, 0, 0);
-                    }
-                }
+                load_values(u + 1, next);
+                pages = next;
             }
-            load_values(u + 1, next);
-            pages = next;
+            if (i < u1) {
+                held0 += 64;
+                held = behind;
+                behind = entry(held0 + 64 + lane);
+            }
         }
 
         if (u0 > 0) {
