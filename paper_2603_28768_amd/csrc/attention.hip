@@ -144,7 +144,7 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
 
         const unsigned char *kh = a.k + h * a.k_head, *vh = a.v + h * a.v_head;
         const int32_t *table = a.table + (int64_t)here.request * a.table_stride;
-        const uint32_t k_span = 16u * (uint32_t)a.k_token, v_span = 16u * (uint32_t)a.v_token;
+        const uint32_t k_span = 15u * (uint32_t)a.k_token + (uint32_t)a.dk * S::B, v_span = 15u * (uint32_t)a.v_token + (uint32_t)a.dv * S::B;
         const uint32_t k_off = (uint32_t)col * (uint32_t)a.k_token + g * 16;
 
         z.clear();

@@ -11,6 +11,7 @@ inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 constexpr int64_t kInts = (int64_t)1 << 31;       // 32-bit indices stay below this
+constexpr int32_t kMostShared = 65536;            // query heads of a cache head: a launch has one workgroup or more for each 16 or 64
 constexpr int64_t kFarthest = (int64_t)1 << 46;   // bytes a stride may span
 
 // log2 of a page size, -1 if it is none
@@ -74,6 +75,7 @@ craft_status attention_args(const craft_kv_cache *c, const craft_attention_args 
     const craft_status st = view_of(c, &w);
     if (st != CRAFT_OK) return st;
     if (!a || a->R < 0 || a->Hq <= 0 || a->Hq % c->heads || (int64_t)a->R * a->Hq >= kInts) return CRAFT_EINVAL;
+    if (a->Hq / c->heads > kMostShared) return CRAFT_EINVAL;
     // twice the longest request is still a 32-bit number
     if (a->max_pages <= 0 || (int64_t)a->max_pages * c->page_size > kInts / 2 || a->window < 0) return CRAFT_EINVAL;
     AttentionArgs o{};

@@ -384,6 +384,20 @@ def test_attention_is_the_same_every_time(torch_cuda):
             assert torch.equal(s.attn(s.q, s.d_lens, s.d_table), first)
 
 
+def test_attention_rows_that_overlap(torch_cuda):
+    # a row starts inside the one before: the last rows of a page end behind 16 (or page_size) strides
+    torch = torch_cuda
+    pages, P, d, step = 3, 16, 64, 24
+    g = torch.Generator(device=DEV).manual_seed(9)
+    store = torch.randn(pages * 500, generator=g, device=DEV).bfloat16()
+    k = torch.as_strided(store, (pages, 1, P, d), (496, 496, step, 1))
+    table = torch.tensor([[1, 0, 2]], dtype=torch.int32, device=DEV)
+    q = torch.randn((1, 4, d), generator=g, device=DEV).bfloat16()
+    out = binding.DecodeAttention(binding.KvCache(k, k), 1, 4, 3)(q, torch.tensor([47], dtype=torch.int32, device=DEV), table)
+    want, _, bound, _ = ref.attention(q, k, k, None, None, [47], table, d ** -0.5)
+    assert bool(((out.double().cpu() - want).abs() <= bound).all())
+
+
 def test_attention_places_beyond_4_gib(torch_cuda):
     # pages farther apart than 32-bit offsets reach; the rows in use are at both ends
     torch = torch_cuda

@@ -85,6 +85,15 @@ def test_bad_attention_calls_are_refused(bad):
     assert binding.lib().craft_decode_attention(ctypes.byref(cache()), ctypes.byref(a), None) == EINVAL
 
 
+def test_heads_that_share_a_key_are_limited():
+    c = cache(heads=1, v=None, dk=576, dv=512, k_token=576)
+    for Hq, rc in ((65536, OK), (65537, EINVAL), (1 << 27, EINVAL)):
+        assert size_of(c, attention(Hq=Hq))[0] == rc
+        if rc != OK:
+            a = attention(Hq=Hq, q_stride=1 << 40, q_head_stride=576, workspace_bytes=1 << 40)
+            assert binding.lib().craft_decode_attention(ctypes.byref(c), ctypes.byref(a), None) == rc
+
+
 def test_null_structs_and_small_workspaces():
     lib = binding.lib()
     c, a = cache(), attention()
