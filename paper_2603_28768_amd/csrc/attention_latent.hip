@@ -5,7 +5,7 @@
 // used where the first product leaves them).  What is different is the ratio: 128 heads make 2 (576 + 512) 128
 // operations of 1152 bytes, more than the matrix units' share of what HBM delivers, so every row is fetched once
 // for many heads, into LDS.  From there K is read as rows and V by columns, by each of the waves that hold the
-// heads.  
+// heads.
 //
 // A workgroup holds 64 heads, 16 a wave, one wave per SIMD unit: Q, the sums of 512 columns and what is on its way
 // from LDS take more than half of a SIMD unit's registers.  The products of a tile's scores run before those of the
@@ -23,10 +23,14 @@ namespace {
 constexpr int kItemCost = 4;                       // what an item costs beside its units
 constexpr int kMinRun = 8;                         // of a workgroup, where there is little to do
 
+// Whether there are fewer items than runs: every item then has a place among the cuts, otherwise every run has (it
+// leaves at most one item open).  The join has a workgroup or more for each place.
+__host__ __device__ __forceinline__ bool cuts_by_item(const AttentionArgs &a) { return (int64_t)a.R * a.heads <= a.workers; }
+
 __device__ const uint4 zero_row[72] = {};          // 1152 bytes
 
-// four bytes per lane
-// The same by the lanes of a mask, between instructions that all lanes run: no branch parts the products.
+// dma_chunk (16 bytes a lane) and the same of 4 bytes a lane, by the lanes of a mask, between instructions that all
+// lanes run: no branch parts the products.
 static __device__ __forceinline__ void dma_chunk_by(uint64_t lanes, ubase_t base, uint32_t off, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
                  :: "s"(lds), "v"(off), "s"(base), "s"(lanes) : "memory");
@@ -35,6 +39,7 @@ static __device__ __forceinline__ void dma_word_by(uint64_t lanes, ubase_t base,
     asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b64 exec, -1"
                  :: "s"(lds), "v"(off), "s"(base), "s"(lanes) : "memory");
 }
+// from an address of each lane's own
 static __device__ __forceinline__ void dma_word_at(ubase_t p, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(lds), "v"(p) : "memory");
 }
@@ -87,7 +92,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_kernel(AttentionArgs a,
     const uint32_t scale0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float *)&s_scale[0][0];
     Runs runs;
     const Start st = find_start<kWaves, 1>(a, a.heads, kItemCost, a.workers, kMinRun, worker, runs);
-    if (tid == 0 && block == 0) a.cuts[worker].request = -1;
+    if (tid == 0 && block == 0 && !cuts_by_item(a)) a.cuts[worker].request = -1;
     if (worker >= runs.n) return;
     const int32_t pieces = a.dk / (16 / S::B);     // of a row, 16 bytes each
     int64_t at = runs.start(worker), before = st.before;
@@ -364,19 +369,21 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_kernel(AttentionArgs a,
             if (starts && ends) z.write(a, request, h * a.group + head_in_group, n_heads, lane);
             else z.put(a.part + (((int64_t)worker * 2 + (starts ? 1 : 0)) * blocks * kWaves + block * kWaves + wave) * State::kFloats, lane);
         }
-        if (starts && !ends && tid == 0 && block == 0) a.cuts[worker] = {request, h, runs.of(item_end - 1), 0};
+        if (starts && tid == 0 && block == 0 && (!ends || cuts_by_item(a)))
+            a.cuts[cuts_by_item(a) ? request * a.heads + h : worker] = {ends ? -1 : request, h, worker, ends ? 0 : runs.of(item_end - 1)};
     }
 }
 
-// Joins the parts of the items that are cut between workgroups: the last part of run blockIdx.x and the first ones of
-// those that follow.  A launch of its own, because the parts are many (33 KiB for every 16 heads) and their sum wants
-// many CUs: a workgroup has four tiles of columns of 16 heads, its waves every fourth part.
+// Joins the parts of the items that are cut between workgroups: the last part of the run that an item starts in and the
+// first ones of those that follow.  A launch of its own, because the parts are many (33 KiB for every 16 heads) and
+// their sum wants many CUs: a workgroup has four tiles of columns of 16 heads, its waves every fourth part.
 __global__ __launch_bounds__(64 * kWaves) void latent_join_kernel(AttentionArgs a, int32_t blocks) {
     typedef Sums<4, 1, false> Four;
     __shared__ float s_sums[kWaves][Four::kFloats];
-    const int32_t run = blockIdx.x, set = blockIdx.y >> 3;
+    const int32_t set = blockIdx.y >> 3;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tile0 = (blockIdx.y & 7) * 4;
-    const LatentCut cut = a.cuts[run];
+    const LatentCut cut = a.cuts[blockIdx.x];
+    const int32_t run = cut.first;
     const int32_t n_heads = min(16, a.group - set * 16);
     if (cut.request < 0 || n_heads <= 0 || tile0 * 16 >= a.dv) return;
     Four z;
@@ -400,7 +407,8 @@ template <int FMT>
 void launch_format(const AttentionArgs &a, hipStream_t s) {
     const int32_t blocks = latent_blocks(a);
     hipLaunchKernelGGL((latent_kernel<FMT>), dim3((unsigned)(a.workers * blocks)), dim3(64 * kWaves), 0, s, a, blocks);
-    hipLaunchKernelGGL(latent_join_kernel, dim3((unsigned)a.workers, (unsigned)(blocks * kWaves * 8)), dim3(64 * kWaves), 0, s, a, blocks);
+    const int32_t cuts = cuts_by_item(a) ? a.R * a.heads : a.workers;
+    hipLaunchKernelGGL(latent_join_kernel, dim3((unsigned)cuts, (unsigned)(blocks * kWaves * 8)), dim3(64 * kWaves), 0, s, a, blocks);
 }
 
 }  // namespace

@@ -297,9 +297,9 @@ struct KvAppendArgs {
 };
 hipError_t launch_kv_append(const KvAppendArgs &a, bool e4m3, hipStream_t s);
 
-// An item that starts in a run of the latent kernel and ends in run `last`; request -1: none.
+// An item that starts in a run of the latent kernel and ends in another one; request -1: none.
 struct LatentCut {
-    int32_t request, head, last, unused;
+    int32_t request, head, first, last;
 };
 struct AttentionArgs {
     int32_t format;                // CRAFT_KV_*
@@ -319,7 +319,7 @@ struct AttentionArgs {
     float *lse;
     int32_t *counters;             // workspace: zero between calls
     float *part;                   // behind them
-    LatentCut *cuts;               // latent kernel: [workers], in front of its parts
+    LatentCut *cuts;               // latent kernel: [workers], an item's or a run's each, in front of its parts
     int32_t workers;
 };
 // Workgroups a launch may have, whatever the lengths; the workspace is sized for them.
