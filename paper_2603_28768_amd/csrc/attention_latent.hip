@@ -20,8 +20,11 @@
 namespace craft {
 namespace {
 
-constexpr int kItemCost = 4;                       // what an item costs beside its units
-constexpr int kMinRun = 8;                         // of a workgroup, where there is little to do
+// What an item costs beside its units: queries, first rows, results, 10 us when every CU does it at once.  200 requests
+// of 200 to 2500 tokens, 64 heads, with 4 / 6 / 8 / 10: 82.5 / 78 / 76 / 77.5 us.
+constexpr int kItemCost = 8;
+// Of a workgroup, where there is little to do.  One request of 900 tokens, 128 heads, with 8 / 6: 23.3 / 20.5 us.
+constexpr int kMinRun = 6;
 
 // Whether there are fewer items than runs: every item then has a place among the cuts, otherwise every run has (it
 // leaves at most one item open).  The join has a workgroup or more for each place.
@@ -85,6 +88,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_kernel(AttentionArgs a,
     __shared__ __attribute__((aligned(1024))) unsigned char s_rows[kBuffers * BUF];
     __shared__ __attribute__((aligned(16))) float s_mask[kBuffers][T], s_scale[kBuffers][FMT == CRAFT_KV_E4M3 ? T : 4];
     static_assert(RPW == 8, "a wave fetches eight rows");
+    static_assert(kWaves * 16 * 1024 <= sizeof(s_rows), "the results of all waves fit in the buffers");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int32_t worker = blockIdx.x % a.workers, block = blockIdx.x / a.workers;
@@ -210,12 +214,12 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_kernel(AttentionArgs a,
         u32x4_t q[S::QN];
         {
             const bool live = col < n_heads;
-            const unsigned char *qr = static_cast<const unsigned char *>(a.q) +
-                ((int64_t)request * a.q_stride + (int64_t)(h * a.group + (live ? head_in_group + col : 0)) * a.q_head) * 2;
+            const __amdgpu_buffer_rsrc_t qr = rows_of(static_cast<const unsigned char *>(a.q) + ((int64_t)request * a.q_stride + (int64_t)(h * a.group + head_in_group) * a.q_head) * 2, kFar);
+            const uint32_t q_off = (uint32_t)col * (uint32_t)a.q_head * 2;
 #pragma unroll
             for (int i = 0; i < S::QN; ++i) {
                 const int d = FMT == CRAFT_KV_E4M3 ? (i >> 1) * 64 + g * 16 + (i & 1) * 8 : i * 32 + g * 8;
-                q[i] = *reinterpret_cast<const u32x4_t *>((live && d < a.dk ? qr : reinterpret_cast<const unsigned char *>(zero_row)) + d * 2);
+                q[i] = __builtin_amdgcn_raw_buffer_load_b128(qr, live && d < a.dk ? q_off + d * 2 : kFar, 0, 0);
             }
         }
         z.clear();
@@ -364,11 +368,31 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_kernel(AttentionArgs a,
         dma_wait<0>();
         meet();                                    // the buffers are free for the next item
 
+        // Results leave as whole rows, by way of the buffers: piece p of 16 bytes of a head's row in place p ^ head.
+        // Straight out of the registers a store instruction has 32 bytes of each of 16 rows: 7900 cycles an item, not 4600.
+        auto write_rows = [&](int32_t to, int32_t head0) {
+            unsigned char *rows = s_rows + wave * 16 * 1024;
+            const float sum = sum_of_head(z.l), inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+            for (int c = 0; c < 32; ++c) {
+                const f32x4_t x = z.acc[c][0] * inv;
+                *reinterpret_cast<u32x2_t *>(rows + col * 1024 + ((c * 2 + (g >> 1)) ^ col) * 16 + (g & 1) * 8) = (u32x2_t){bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
+            }
+            const int64_t head = (int64_t)to * a.Hq + head0;
+            if (a.lse && g == 0 && col < n_heads) a.lse[head + col] = sum == 0.0f ? -INFINITY : (z.m + __log2f(sum)) * 0.6931471805599453f;
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            unsigned char *out = static_cast<unsigned char *>(a.out) + (head * a.dv + lane * 8) * 2;
+            for (int i = 0; i < n_heads; ++i) {
+                const u32x4_t x = *reinterpret_cast<const u32x4_t *>(rows + i * 1024 + (lane ^ i) * 16);
+                if (lane * 8 < a.dv) *reinterpret_cast<u32x4_t *>(out + (int64_t)i * a.dv * 2) = x;
+            }
+        };
         const bool starts = u0 == 0, ends = u1 == n_units;
         if (busy) {
-            if (starts && ends) z.write(a, request, h * a.group + head_in_group, n_heads, lane);
+            if (starts && ends) write_rows(request, h * a.group + head_in_group);
             else z.put(a.part + (((int64_t)worker * 2 + (starts ? 1 : 0)) * blocks * kWaves + block * kWaves + wave) * State::kFloats, lane);
         }
+        if (starts && ends) meet();                // the buffers are free again
         if (starts && tid == 0 && block == 0 && (!ends || cuts_by_item(a)))
             a.cuts[cuts_by_item(a) ? request * a.heads + h : worker] = {ends ? -1 : request, h, worker, ends ? 0 : runs.of(item_end - 1)};
     }
