@@ -13,6 +13,12 @@
 // into LDS, up to three tiles of 32 tokens ahead, 16-byte pieces in an order (exclusive or with the row's number) in
 // which neither way of reading meets a bank twice.  Rows that a tile lacks (behind the last
 // token, in front of the window, without a page) are fetched from a row of zeros and masked by -infinity.
+//
+// 64 requests of 1000 to 8000 tokens, 128 heads, bf16: 105 us, 2.5 TB/s and 570 TFLOP/s; 7 of 20000 to 50000 in 8 bits 130
+// us, 490 TFLOP/s.  A tile of 32 tokens takes a workgroup 1.3 us (8 bits 1.8), 1.0 of them without any row fetched, and
+// 0.45 its 68 matrix instructions.  Reads of a tile out of LDS, by four waves, take 0.9 at 128 bytes a clock; but with 32
+// heads a wave, which halves them (and what is widened in 8 bits) for a head and takes all registers, the first takes 134
+// us and the second 137.
 #include <algorithm>
 
 #include "attention_common.h"
