@@ -1,5 +1,5 @@
 """The paged cache on the GPU: tables against a request-by-request walk (equal), writes (equal; 8 bits against the CPU
-checker's codes and scales), attention against 64 bits within the bound that kv_reference.attention derives."""
+oracle's codes and scales), attention against 64 bits within the bound that kv_reference.attention derives."""
 import numpy as np
 import pytest
 
