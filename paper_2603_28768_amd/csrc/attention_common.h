@@ -3,6 +3,7 @@
 #pragma once
 
 #include "ffn_common.h"
+#include "shares.h"
 
 namespace craft {
 
@@ -117,7 +118,7 @@ static __device__ __forceinline__ Start find_start(const AttentionArgs &a, int32
     __shared__ Start found[COUNT];
     constexpr int kThreads = 64 * WAVES;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int32_t per = (a.R + kThreads - 1) / kThreads;
+    const int32_t per = share_of<kThreads>(a.R);
     const int64_t r0 = min((int64_t)a.R, (int64_t)tid * per), r1 = min((int64_t)a.R, r0 + per);
     int64_t sum = 0;
     int32_t len = 0;                               // of the last request: of the only one, up to kThreads requests

@@ -15,6 +15,7 @@
 
 #include "e4m3.h"
 #include "kernels.h"
+#include "shares.h"
 
 namespace craft {
 namespace {
@@ -124,7 +125,7 @@ __global__ __launch_bounds__(THREADS) void tables_scan_kernel(KvTablesArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t taken = a.pool[0], returned = a.pool[1];
     // this thread's requests: a run of `per`
-    const int32_t per = FUSED ? 1 : (a.R + THREADS - 1) / THREADS;
+    const int32_t per = FUSED ? 1 : share_of<THREADS>(a.R);
     const int64_t r0 = (int64_t)tid * per, r1 = min((int64_t)a.R, r0 + per);
     Counts sum = {0, 0, 0};
     Request q = {0, 0, 0, 0, 0};
