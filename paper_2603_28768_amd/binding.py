@@ -483,17 +483,19 @@ class RankForward:
 
 # ---------------------------------------------------------- paged key/value cache
 
-def _stream_on(t, stream):
-    """The stream to launch on: the one given, or the current one of the tensor's device.  (Asked for by number: the
+def _stream_on(gpu, stream):
+    """The stream to launch on: the one given, or the current one of GPU number `gpu`.  (Asked for by number: the
     Stream object costs three microseconds, as much as a whole launch.)"""
-    if stream is not None:
-        return stream.cuda_stream
     import torch
-    return torch._C._cuda_getCurrentRawStream(t.get_device())
+    number = torch._C._cuda_getCurrentRawStream(gpu) if stream is None else stream.cuda_stream
+    # number 0 is the default stream of whichever GPU is current
+    assert number or torch._C._cuda_getDevice() == gpu, "the tensors are not on the current GPU"
+    return number
 
 
 class KvCache:
-    """The paged cache of one layer over tensors that the caller made.
+    """The paged cache of one layer over tensors that the caller made, all on one GPU.  What is given to its calls, or
+    to a DecodeAttention over it, lies there too.
 
     k, v: cuda [pages][heads][page_size][d], float32, bfloat16 or float8_e4m3fn; any strides with a contiguous last
     dimension.  v=None: latent rows, a token's value row is the first `dv` elements of its key row.
@@ -503,17 +505,18 @@ class KvCache:
         import torch
         formats = {torch.float32: CRAFT_KV_F32, torch.bfloat16: CRAFT_KV_BF16, torch.float8_e4m3fn: CRAFT_KV_E4M3}
         assert k.dtype in formats and k.dim() == 4 and k.stride(3) == 1 and k.is_cuda
+        self._gpu = k.get_device()
         pages, heads, page_size, dk = k.shape
         if v is None:
             assert dv is not None, "latent rows need the number of value elements"
         else:
-            assert v.dtype == k.dtype and v.shape[:3] == k.shape[:3] and v.stride(3) == 1 and v.device == k.device
+            assert v.dtype == k.dtype and v.shape[:3] == k.shape[:3] and v.stride(3) == 1 and v.get_device() == self._gpu
             assert dv is None or dv == v.shape[3]
             dv = v.shape[3]
         eight = k.dtype == torch.float8_e4m3fn
         assert (k_scale is not None) == eight and (v_scale is not None) == (eight and v is not None)
         for sc in (k_scale, v_scale):
-            assert sc is None or (sc.dtype == torch.float32 and tuple(sc.shape) == (pages, heads, page_size) and sc.is_contiguous())
+            assert sc is None or (sc.get_device() == self._gpu and sc.dtype == torch.float32 and tuple(sc.shape) == (pages, heads, page_size) and sc.is_contiguous())
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self._int32 = torch.int32
         self.pages, self.heads, self.page_size, self.dk, self.dv = pages, heads, page_size, dk, dv
@@ -549,19 +552,19 @@ class KvCache:
         """k: cuda [T][heads][dk], v: [T][heads][dv] (None for latent rows), of the cache's `dtype`, the heads of a
         token contiguous; slots: cuda int32 [T], negative ones skipped."""
         T = slots.shape[0]
-        assert slots.dtype == self._int32 and slots.is_cuda and slots.dim() == 1 and (T < 2 or slots.stride(0) == 1)
+        assert slots.dtype == self._int32 and slots.get_device() == self._gpu and slots.dim() == 1 and (T < 2 or slots.stride(0) == 1)
         row_k = self._rows(k, T, self.dk)
         if self.v is None:
             assert v is None
-            rc = self._append(self._ref, T, k.data_ptr(), row_k, None, 0, slots.data_ptr(), _stream_on(slots, stream))
+            rc = self._append(self._ref, T, k.data_ptr(), row_k, None, 0, slots.data_ptr(), _stream_on(self._gpu, stream))
         else:
             row_v = self._rows(v, T, self.dv)
-            rc = self._append(self._ref, T, k.data_ptr(), row_k, v.data_ptr(), row_v, slots.data_ptr(), _stream_on(slots, stream))
+            rc = self._append(self._ref, T, k.data_ptr(), row_k, v.data_ptr(), row_v, slots.data_ptr(), _stream_on(self._gpu, stream))
         if rc:
             _check(rc, "craft_kv_append")
 
     def _rows(self, t, T, d):
-        assert t.dtype == self.dtype and t.is_cuda and t.shape == (T, self.heads, d)
+        assert t.dtype == self.dtype and t.get_device() == self._gpu and t.shape == (T, self.heads, d)
         row, head, one = t.stride()
         assert one == 1 and (self.heads == 1 or head == d)
         return row if T > 1 else self.heads * d
@@ -584,7 +587,9 @@ class KvTables:
         self.pool = torch.tensor([0, pages], dtype=torch.int64, device=device) if pool is None else pool
         for t, shape, dtype in ((self.lens, (requests,), torch.int32), (self.ring, (pages,), torch.int32), (self.pool, (2,), torch.int64)):
             assert t.is_cuda and t.dtype == dtype and tuple(t.shape) == shape and t.is_contiguous()
-        assert self.table.is_cuda and self.table.dtype == torch.int32 and tuple(self.table.shape) == (requests, max_pages)
+        self._gpu = self.lens.get_device()
+        assert self.ring.get_device() == self.pool.get_device() == self.table.get_device() == self._gpu
+        assert self.table.dtype == torch.int32 and tuple(self.table.shape) == (requests, max_pages)
         assert max_pages == 1 or self.table.stride(1) == 1
         dev = self.lens.device
         self.slots = torch.full((max_new,), -1, dtype=torch.int32, device=dev)
@@ -606,10 +611,10 @@ class KvTables:
         counters replace the old ones, or go to `lens_out` and `pool_out`.  Returns slots."""
         lens_out, pool_out = self.lens if lens_out is None else lens_out, self.pool if pool_out is None else pool_out
         for t, like in ((add, self.lens), (lens_out, self.lens), (pool_out, self.pool)):
-            assert t is like or (t.dtype == like.dtype and t.is_cuda and t.shape == like.shape and t.is_contiguous())
+            assert t is like or (t.dtype == like.dtype and t.get_device() == self._gpu and t.shape == like.shape and t.is_contiguous())
         a = self.args
         a.add, a.lens_out, a.pool_out = add.data_ptr(), lens_out.data_ptr(), pool_out.data_ptr()
-        rc = self._step(self._ref, _stream_on(add, stream))
+        rc = self._step(self._ref, _stream_on(self._gpu, stream))
         if rc:
             _check(rc, "craft_kv_tables")
         return self.slots
@@ -621,7 +626,7 @@ class DecodeAttention:
     def __init__(self, cache: KvCache, requests: int, query_heads: int, max_pages: int, scale: Optional[float] = None,
                  window: int = 0, want_lse: bool = False):
         import torch
-        self.cache, self.R, self.Hq, self.max_pages = cache, requests, query_heads, max_pages
+        self.cache, self.R, self.Hq, self.max_pages, self._gpu = cache, requests, query_heads, max_pages, cache._gpu
         dev = cache.k.device
         self.out = torch.empty((requests, query_heads, cache.dv), dtype=cache.dtype, device=dev)
         self.lse = torch.empty((requests, query_heads), dtype=torch.float32, device=dev) if want_lse else None
@@ -640,9 +645,9 @@ class DecodeAttention:
     def __call__(self, q, lens, table, stream=None):
         """q: cuda [requests][query_heads][dk]; lens: int32 [requests]; table: int32 [requests][max_pages].  Returns
         the (reused) output tensor."""
-        assert q.is_cuda and q.dtype == self.cache.dtype and q.shape == self._q_shape
-        assert lens.is_cuda and lens.dtype == self._int32 and lens.shape == self._q_shape[:1] and (self.R < 2 or lens.stride(0) == 1)
-        assert table.is_cuda and table.dtype == self._int32 and table.shape == self._table_shape
+        assert q.get_device() == self._gpu and q.dtype == self.cache.dtype and q.shape == self._q_shape
+        assert lens.get_device() == self._gpu and lens.dtype == self._int32 and lens.shape == self._q_shape[:1] and (self.R < 2 or lens.stride(0) == 1)
+        assert table.get_device() == self._gpu and table.dtype == self._int32 and table.shape == self._table_shape
         row, head, one = q.stride()
         table_row, entry = table.stride()
         assert one == 1 and (entry == 1 or self.max_pages == 1)
@@ -651,7 +656,7 @@ class DecodeAttention:
         a.q_head_stride = head if self.Hq > 1 else self.cache.dk
         a.q_stride = row if self.R > 1 else self.Hq * self.cache.dk
         a.table_stride = table_row if self.R > 1 else self.max_pages
-        rc = self._call(self._cache_ref, self._ref, _stream_on(q, stream))
+        rc = self._call(self._cache_ref, self._ref, _stream_on(self._gpu, stream))
         if rc:
             _check(rc, "craft_decode_attention")
         return self.out
