@@ -503,7 +503,8 @@ craft_status craft_kv_append(const craft_kv_cache *cache, int64_t T, const void 
  * in front of the product with 16- and 8-bit values.  The result depends on the arguments only (the
  * order of the sums: on the lengths and on the GPU's number of compute units), never on scheduling.
  * Rows of the pages behind a request's last token may hold anything.
- * Limits: Hq a multiple of heads, up to 65536 times as many; R * Hq < 2^31; max_pages * page_size <= 2^30.  R may be 0.
+ * Limits: Hq a multiple of heads, up to 65536 times as many; R * Hq < 2^31; max_pages * page_size <= 2^30; scale * log2(e)
+ * finite in fp32.  R may be 0.
  */
 #define CRAFT_ATTENTION_COUNTER_BYTES (48u << 10)
 

@@ -12,6 +12,7 @@ inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 constexpr int64_t kInts = (int64_t)1 << 31;       // 32-bit indices stay below this
 constexpr int32_t kMostShared = 65536;            // query heads of a cache head: a launch has one workgroup or more for each 16 or 64
+constexpr float kLog2e = 1.4426950408889634f;     // scores are powers of two in the kernels
 constexpr int64_t kFarthest = (int64_t)1 << 46;   // bytes a stride may span
 
 // log2 of a page size, -1 if it is none
@@ -195,7 +196,7 @@ craft_status craft_decode_attention(const craft_kv_cache *cache, const craft_att
     AttentionArgs a;
     const craft_status st = attention_args(cache, args, &a);
     if (st != CRAFT_OK) return st;
-    if (!std::isfinite(args->scale)) return CRAFT_EINVAL;
+    if (!std::isfinite(args->scale * kLog2e)) return CRAFT_EINVAL;
     if (a.R == 0) return CRAFT_OK;
     const int es = cache->format == CRAFT_KV_F32 ? 4 : 2;
     if (!args->q || !aligned(args->q, 16) || args->q_stride <= 0 || args->q_head_stride < cache->dk) return CRAFT_EINVAL;
@@ -214,7 +215,7 @@ craft_status craft_decode_attention(const craft_kv_cache *cache, const craft_att
     a.lens = args->lens;
     a.table = args->table;
     a.table_stride = args->table_stride;
-    a.scale_log2 = args->scale * 1.4426950408889634f;
+    a.scale_log2 = args->scale * kLog2e;
     a.out = args->out;
     a.lse = args->lse;
     a.workers = attention_workers(a, cus);
