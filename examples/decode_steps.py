@@ -30,6 +30,12 @@ CONFIG = synth.scaled(synth.CONFIGS["qwen3"], H=256, I=128, E=16, k=4, D=1, repl
 LAYERS, VOCABULARY, HEADS = 2, 512, 8
 
 
+def cache_rows(cache):
+    """Heads of a layer's cache, elements of a key row and of a value row.  Latent rows, which all query heads share, are
+    as long as models have them: those of up to 256 elements go through the kernel of ordinary rows."""
+    return (1, 576, 512) if cache.startswith("latent") else (HEADS // 4, 64, 64)
+
+
 class Layer:
     """Weights, cache and kernels of one layer; `hidden` is the step's activations, one row per request."""
 
@@ -37,7 +43,7 @@ class Layer:
         H = CONFIG.H
         matrix = lambda rows, cols: (torch.randn((cols, rows), generator=gen, device=device) * rows ** -0.5).bfloat16()  # noqa: E731
         latent = cache.startswith("latent")
-        self.heads, self.dk, self.dv = (1, 96, 64) if latent else (HEADS // 4, 64, 64)
+        self.heads, self.dk, self.dv = cache_rows(cache)
         self.cache = binding.KvCache.allocate(pages, page_size, self.heads, self.dk, self.dv, "e4m3" if cache.endswith("e4m3") else "bf16",
                                               latent=latent, device=device)
         self.attention = binding.DecodeAttention(self.cache, R, HEADS, max_pages)
