@@ -500,8 +500,11 @@ craft_status craft_kv_append(const craft_kv_cache *cache, int64_t T, const void 
  *           call leaves them at zero.  Calls that share a workspace (of any shapes) must be ordered
  *           on one stream
  * Scores, maxima, sums and the weighted sum are fp32; the weights exp(s - max) are rounded to bf16
- * in front of the product with 16- and 8-bit values.  The result depends on the arguments only (the
- * order of the sums: on the lengths and on the GPU's number of compute units), never on scheduling.
+ * in front of the product with 16- and 8-bit values.  The result depends on the arguments only, never
+ * on scheduling.  The order of the sums depends on the sizes, on the lengths, on whether pages have
+ * fewer than 16 tokens, and on the GPU's number of compute units; where the rows lie does not change it.
+ * Weights are up to 256 before the division by their sum: values beyond 2^119 / (a request's tokens) may
+ * overflow on the way.
  * Rows of the pages behind a request's last token may hold anything.
  * Limits: Hq a multiple of heads, up to 65536 times as many; R * Hq < 2^31; max_pages * page_size <= 2^30; scale * log2(e)
  * finite in fp32.  R may be 0.

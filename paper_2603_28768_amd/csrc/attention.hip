@@ -514,7 +514,8 @@ int32_t attention_workers(const AttentionArgs &a, int32_t num_cu) {
     return std::min(kCounters, groups_of(a.format, padded_dim(a), a.shift < 4) * num_cu);
 }
 
-size_t attention_counters_bytes() { return 3 * kCounters * sizeof(int32_t); }
+size_t attention_counters_bytes() { return CRAFT_ATTENTION_COUNTER_BYTES; }
+static_assert(CRAFT_ATTENTION_COUNTER_BYTES == 3 * kCounters * sizeof(int32_t), "three counters for every workgroup of a launch");
 
 size_t attention_workspace(const AttentionArgs &a, int32_t num_cu) {
     const int dv = padded_dim(a) == 576 ? 512 : padded_dim(a);
