@@ -170,7 +170,7 @@ craft_status craft_kv_append(const craft_kv_cache *cache, int64_t T, const void 
     a.k = static_cast<const unsigned char *>(k);
     a.v = w.latent ? nullptr : static_cast<const unsigned char *>(v);
     a.k_stride = k_stride * es;
-    a.v_stride = v_stride * es;
+    a.v_stride = w.latent ? 0 : v_stride * es;     // ignored for latent rows, whatever it is
     a.slots = slots;
     a.slots_total = cache->pages * cache->page_size;
     a.shift = w.shift;
