@@ -499,8 +499,9 @@ craft_status craft_kv_append(const craft_kv_cache *cache, int64_t T, const void 
  *           CRAFT_ATTENTION_COUNTER_BYTES have to be zero before the first call that uses it; every
  *           call leaves them at zero.  Calls that share a workspace (of any shapes) must be ordered
  *           on one stream
- * Scores, maxima, sums and the weighted sum are fp32; the weights exp(s - max) are rounded to bf16
- * in front of the product with 16- and 8-bit values.  The result depends on the arguments only, never
+ * Scores, maxima, sums and the weighted sum are fp32.  In front of the product with 16- and 8-bit
+ * values the weights exp(s - max) are rounded, to 2^-16 of themselves; over latent rows of more than
+ * 256 elements to bf16 (2^-8).  The result depends on the arguments only, never
  * on scheduling.  The order of the sums depends on the sizes, on the lengths, on whether pages have
  * fewer than 16 tokens, and on the GPU's number of compute units; where the rows lie does not change it.
  * Weights are up to 256 before the division by their sum: values beyond 2^119 / (a request's tokens) may

@@ -18,6 +18,10 @@
 //                   r of tile j is column CE r + j, so that a lane reads CE neighbouring elements of a token,
 //                   the 16 lanes of a group a contiguous stretch, and transposes 8 tokens x CE within its own
 //                   registers.  No LDS and no shuffle in the loop.
+// The weights of 16- and 8-bit values go into the second product as two bf16 numbers, the nearest one and the nearest
+// one to what is left of the weight: off by 2^-16 of it, not 2^-8.  The second set of products hides behind HBM: two
+// requests of 100001 and 131072 tokens, 8 heads of 128 in bf16, 155 us with one number a weight and with two; 250 of 1000
+// to 8000 in 8 bits 151 and 151; 64 of 1 to 16384 in 8 bits, heads of 64, the fewest bytes for an instruction, 33.1 and 33.8.
 // A wave has the keys of the next unit in flight while it works on the weights and values of this one, and the
 // other way round.
 //
@@ -363,8 +367,15 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
                                     z.acc[c][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word<S::VW>(vc, e)), p[t][j], z.acc[c][e], 0, 0, 0);
                             }
                 } else {
-                    const wide_t pw = {bf16_pair(p[0][0], p[0][1]), bf16_pair(p[0][2], p[0][3]), bf16_pair(p[1][0], p[1][1]), bf16_pair(p[1][2], p[1][3])};
-                    const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, pw);
+                    // the weights in bf16, and what that left of them
+                    wide_t pw, pr;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float lo = p[i >> 1][2 * (i & 1)], hi = p[i >> 1][2 * (i & 1) + 1];
+                        pw[i] = bf16_pair(lo, hi);
+                        pr[i] = bf16_pair(lo - __uint_as_float(pw[i] << 16), hi - __uint_as_float(pw[i] & 0xffff0000u));
+                    }
+                    const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, pw), rest = __builtin_bit_cast(bf16x8_t, pr);
 #pragma unroll
                     for (int c = 0; c < S::NV; ++c) {
                         typename VWords::type vc[8];
@@ -382,6 +393,8 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
                             const wide_t odd = {perm(w[1], w[0], 0x07060302u), perm(w[3], w[2], 0x07060302u), perm(w[5], w[4], 0x07060302u), perm(w[7], w[6], 0x07060302u)};
                             z.acc[c][2 * e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, even), pf, z.acc[c][2 * e], 0, 0, 0);
                             z.acc[c][2 * e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, odd), pf, z.acc[c][2 * e + 1], 0, 0, 0);
+                            z.acc[c][2 * e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, even), rest, z.acc[c][2 * e], 0, 0, 0);
+                            z.acc[c][2 * e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, odd), rest, z.acc[c][2 * e + 1], 0, 0, 0);
                         }
                     }
                 }
