@@ -35,7 +35,9 @@
 // on a few short requests.  Of an item cut into many parts, 16 at a time are joined first.
 //
 // Two requests of 100001 and 131072 tokens, 8 heads of 128 in bf16: 155 us, 6.1 TB/s (reads of a large array reach 6.2); 250
-// of 1000 to 8000 in 8 bits 151 us, 6.0 TB/s; 64 of 1 to 16384 82 us, 5.4 TB/s; 8 of 40 to 1500 13 us, a chain of round trips.
+// of 1000 to 8000 in 8 bits 151 us, 5.9 TB/s; 64 of 1 to 16384 82 us, 5.4 TB/s; two of 50001 and 65536 in fp32 157 us, 6.0 TB/s.
+// 8 of 40 to 1500, 4 heads: 13 us, of which 1 is the bytes'.  The longest is 38 units, so the work is cut: prefix sums, two
+// units a wave on 60 workgroups, and the joins of items that lie on up to five of them, one round trip behind another.
 #include <algorithm>
 
 #include "attention_common.h"
@@ -45,9 +47,16 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
-constexpr int kItemCost = 2;                       // what an item costs beside its units
-constexpr int kWholeUnits = 24;                    // of an item that is left to one workgroup, where those suffice for all
-constexpr int kMinRun = 2;                         // of a wave, where there is little to do
+// What an item costs beside its units.  A recorded call with 1 / 2 / 4: 64 requests of 1 to 16384 tokens, 8 heads, 90.7 / 84.4
+// / 84.4 us; 250 of 1 to 500 tokens 27.9 / 26.9 / 30.6.
+constexpr int kItemCost = 2;
+// Most units of an item that is left to one workgroup, where those suffice for all.  With 12 / 24 / 48, 32 requests, 8 heads of
+// 128 in bf16: of 600 tokens 24.9 / 18.7 / 18.7 us, of 1000 32.4 / 32.4 / 25.8, of 1500 43.5 / 43.5 / 36.1; but 8 requests, 4 heads: of
+// 600 14.0 / 12.7 / 12.7, of 768 13.4 / 14.4 / 14.5, of 1000 14.3 / 14.3 / 17.5, of 1500 15.4 / 15.5 / 23.0.  Cutting wins where the items are few.
+constexpr int kWholeUnits = 24;
+// Of a wave, where there is little to do.  With 1 / 2 / 4: 2 requests of 2000 tokens, 8 heads, 16.4 / 14.9 / 17.9 us; 8 of 1000, 4 heads,
+// 14.3 / 14.3 / 17.4.
+constexpr int kMinRun = 2;
 
 template <int NV, int CE, bool F32>
 __device__ __forceinline__ void write_item(const Sums<NV, CE, F32> &z, const AttentionArgs &a, const Place &p, int32_t blocks, int lane) {
@@ -481,11 +490,16 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
     }
 }
 
-// Workgroups of a CU, by the bytes of a unit's rows (keys and values, padded), that is by what a wave has on its
-// way.  Waves that have 16 KiB each need only be four to a CU, and more of them read less in order: two requests of
-// 100001 and 131072 tokens, 8 heads of 128 in bf16, with one / two workgroups 159 / 170 us.  Shorter rows, which
-// take more instructions for their bytes, need more waves: 250 requests of 1000 to 8000 tokens, 4 heads of 128 in
-// 8 bits, 179 / 151 us.  So do small pages, for their chains of lookups: the former with pages of 8 211 / 183 us.
+// Workgroups of a CU, by the bytes of a unit's rows (keys and values) as they are padded, which is what a wave has
+// registers and loads for.  More waves hide more latency, and read less in order.
+//   16 KiB and more: one.  Two requests of 100001 and 131072 tokens, 8 heads of 128 in bf16, with one / two 155 / 163 us.  Rows
+//     of 80 and 96 elements have 10 and 12 KiB of these on their way and do no better with two: 64 requests of 1 to
+//     16384, 8 heads, 57 / 60 and 65 / 68 us.
+//   8 KiB: two.  The same requests, rows of 128 in 8 bits, with one / two 59 / 51.5 us, of 64 in bf16 50 / 47.
+//   4 KiB: four.  1000 requests of 100 to 1000 tokens, 8 heads of 64 in 8 bits, with two / four 108 / 97 us; 500 of 1000 to 4000
+//     227 / 221.
+//   Pages of fewer than 16 tokens, for their chains of lookups: two.  The two long requests in pages of 8 with one / two 206
+//     / 181 us.  64 KiB (rows of 256 in fp32): one, all that the registers hold.
 constexpr int groups_of(int format, int dim, bool small) {
     const int unit = kUnit * 2 * dim * (format == CRAFT_KV_F32 ? 4 : format == CRAFT_KV_BF16 ? 2 : 1);
     return unit >= 65536 ? 1 : small ? 2 : unit >= 16384 ? 1 : unit >= 8192 ? 2 : 4;

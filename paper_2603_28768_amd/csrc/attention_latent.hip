@@ -14,6 +14,11 @@
 // which neither way of reading meets a bank twice.  Rows that a tile lacks (behind the last
 // token, in front of the window, without a page) are fetched from a row of zeros and masked by -infinity.
 //
+// Weights are rounded to bf16, the operand's type, in front of the second product: off by 2^-8 of themselves at most.  As two
+// bf16 numbers, which attention.hip uses, they would need as many products again, here where the products count: 64
+// requests of 1000 to 8000 tokens, 128 heads, 104 us would be 120, 7 of 20000 to 50000 in 8 bits 127 would be 140, and the
+// largest errors, at values of 2 to 4, 0.0078 and 0.0151 (the result's own rounding), not 0.0114 and 0.0208.
+//
 // 64 requests of 1000 to 8000 tokens, 128 heads, bf16: 105 us, 2.5 TB/s and 570 TFLOP/s; 7 of 20000 to 50000 in 8 bits 130
 // us, 490 TFLOP/s.  A tile of 32 tokens takes a workgroup 1.3 us (8 bits 1.8), 1.0 of them without any row fetched, and
 // 0.45 its 68 matrix instructions.  Reads of a tile out of LDS, by four waves, take 0.9 at 128 bytes a clock; but with 32
@@ -29,7 +34,8 @@ namespace {
 // What an item costs beside its units: queries, first rows, results, 10 us when every CU does it at once.  200 requests
 // of 200 to 2500 tokens, 64 heads, with 4 / 6 / 8 / 10: 82.5 / 78 / 76 / 77.5 us.
 constexpr int kItemCost = 8;
-// Of a workgroup, where there is little to do.  One request of 900 tokens, 128 heads, with 8 / 6: 23.3 / 20.5 us.
+// Of a workgroup, where there is little to do.  With 4 / 6 / 8 / 12, 128 heads: one request of 900 tokens 18.5 / 19.7 / 22.8 / 24.8 us, 8
+// of 600 22.1 / 23.7 / 26.0 / 30.0; 3 of 5000 to 50000 in 8 bits, 32 heads, 37.8 / 37.8 / 37.0 / 41.2; longer ones do not come to it.
 constexpr int kMinRun = 6;
 
 // Whether there are fewer items than runs: every item then has a place among the cuts, otherwise every run has (it
@@ -440,8 +446,9 @@ void launch_format(const AttentionArgs &a, hipStream_t s) {
     const int32_t blocks = latent_blocks(a);
     hipLaunchKernelGGL((latent_kernel<FMT>), dim3((unsigned)(a.workers * blocks)), dim3(64 * kWaves), 0, s, a, blocks);
     const int32_t cuts = cuts_by_item(a) ? a.R * a.heads : a.workers;
-    // Items of many parts have few workgroups at four tiles each: 3 of up to 50000 tokens in 8 bits, 32 heads, 45.5 us, at
-    // two tiles 38.  Items of few parts have enough.
+    // Items of many parts have few workgroups at four tiles each: 3 of 5000 to 50000 tokens in 8 bits, 32 heads, 48.5 us, at two
+    // tiles 38; 30 of 500 to 20000, 16 heads, 52.6 and 50.6.  Items of few parts have enough: 64 of 1000 to 8000, 128 heads,
+    // 110 us at four, 112 at two.
     if (cuts * 8 <= a.workers) hipLaunchKernelGGL(latent_join_kernel<2>, dim3((unsigned)cuts, (unsigned)(blocks * kWaves * 16)), dim3(64 * kWaves), 0, s, a, blocks);
     else hipLaunchKernelGGL(latent_join_kernel<4>, dim3((unsigned)cuts, (unsigned)(blocks * kWaves * 8)), dim3(64 * kWaves), 0, s, a, blocks);
 }
