@@ -19,8 +19,8 @@
 // requests of 1000 to 8000 tokens, 128 heads, 104 us would be 120, 7 of 20000 to 50000 in 8 bits 127 would be 140, and the
 // largest errors, at values of 2 to 4, 0.0078 and 0.0151 (the result's own rounding), not 0.0114 and 0.0208.
 //
-// 64 requests of 1000 to 8000 tokens, 128 heads, bf16: 105 us, 2.5 TB/s and 570 TFLOP/s; 7 of 20000 to 50000 in 8 bits 130
-// us, 490 TFLOP/s.  A tile of 32 tokens takes a workgroup 1.3 us (8 bits 1.8), 1.0 of them without any row fetched, and
+// 64 requests of 1000 to 8000 tokens, 128 heads, bf16: 107 us, 2.5 TB/s and 560 TFLOP/s; 7 of 20000 to 50000 in 8 bits 127
+// us, 500 TFLOP/s.  A tile of 32 tokens takes a workgroup 1.3 us (8 bits 1.8), 1.0 of them without any row fetched, and
 // 0.45 its 68 matrix instructions.  Reads of a tile out of LDS, by four waves, take 0.9 at 128 bytes a clock; but with 32
 // heads a wave, which halves them (and what is widened in 8 bits) for a head and takes all registers, the first takes 134
 // us and the second 137.
