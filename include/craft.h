@@ -500,7 +500,7 @@ craft_status craft_kv_append(const craft_kv_cache *cache, int64_t T, const void 
  *           call leaves them at zero.  Calls that share a workspace (of any shapes) must be ordered
  *           on one stream
  * Scores, maxima, sums and the weighted sum are fp32.  In front of the product with 16- and 8-bit
- * values the weights exp(s - max) are rounded, to 2^-16 of themselves; over latent rows of more than
+ * values the weights exp(s - max) are rounded, to 2^-15 of themselves; over latent rows of more than
  * 256 elements to bf16 (2^-8).  The result depends on the arguments only, never
  * on scheduling.  The order of the sums depends on the sizes, on the lengths, on whether pages have
  * fewer than 16 tokens, and on the GPU's number of compute units; where the rows lie does not change it.

@@ -18,10 +18,11 @@
 //                   r of tile j is column CE r + j, so that a lane reads CE neighbouring elements of a token,
 //                   the 16 lanes of a group a contiguous stretch, and transposes 8 tokens x CE within its own
 //                   registers.  No LDS and no shuffle in the loop.
-// The weights of 16- and 8-bit values go into the second product as two bf16 numbers, the nearest one and the nearest
-// one to what is left of the weight: off by 2^-16 of it, not 2^-8.  The second set of products hides behind HBM: two
-// requests of 100001 and 131072 tokens, 8 heads of 128 in bf16, 155 us with one number a weight and with two; 250 of 1000
-// to 8000 in 8 bits 151 and 151; 64 of 1 to 16384 in 8 bits, heads of 64, the fewest bytes for an instruction, 33.1 and 33.8.
+// The weights of 16- and 8-bit values go into the second product as two bf16 numbers, a weight's upper half and the nearest
+// number to the rest of it: off by 2^-15 of it, not 2^-8.  The second set of products hides behind HBM: two requests of
+// 100001 and 131072 tokens, 8 heads of 128 in bf16, with one number a weight / with two 155.8 / 156.1 us; 64 of 1 to 16384 82.2 /
+// 82.1; 250 of 1000 to 8000 in 8 bits 150.7 / 151.8; rows of 64 and 80 in 8 bits, the fewest bytes for an instruction, 33.7 / 34.5 and
+// 115.9 / 118.6.
 // A wave has the keys of the next unit in flight while it works on the weights and values of this one, and the
 // other way round.
 //
@@ -376,13 +377,15 @@ __global__ __launch_bounds__(kThreads, WPS) void decode_kernel(AttentionArgs a, 
                                     z.acc[c][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word<S::VW>(vc, e)), p[t][j], z.acc[c][e], 0, 0, 0);
                             }
                 } else {
-                    // the weights in bf16, and what that left of them
+                    // the weights' upper halves, and what that leaves of them: never zero where the weight is not, so that
+                    // an infinite value stays one in both products (an infinite weight, of an infinite scale, as well)
                     wide_t pw, pr;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float lo = p[i >> 1][2 * (i & 1)], hi = p[i >> 1][2 * (i & 1) + 1];
-                        pw[i] = bf16_pair(lo, hi);
-                        pr[i] = bf16_pair(lo - __uint_as_float(pw[i] << 16), hi - __uint_as_float(pw[i] & 0xffff0000u));
+                        const float p0 = p[i >> 1][2 * (i & 1)], p1 = p[i >> 1][2 * (i & 1) + 1];
+                        const uint32_t h0 = __float_as_uint(p0) & 0xffff0000u, h1 = __float_as_uint(p1) & 0xffff0000u;
+                        pw[i] = perm(h1, h0, 0x07060302u);
+                        pr[i] = bf16_pair(fmaxf(p0 - __uint_as_float(h0), p0 * 0x1p-20f), fmaxf(p1 - __uint_as_float(h1), p1 * 0x1p-20f));
                     }
                     const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, pw), rest = __builtin_bit_cast(bf16x8_t, pr);
 #pragma unroll
