@@ -45,6 +45,8 @@ const char *craft_status_str(craft_status s);
 
 /* Element types of activations and expert weights. */
 enum { CRAFT_F32 = 0, CRAFT_BF16 = 1 };
+/* 8-bit integers with fp32 scales: craft_matmul_i8 and craft_grouped_matmul only. */
+enum { CRAFT_I8 = 2 };
 
 /* -------------------------------------------------------------- gating network
  * Sec. 2.1 (routing): expert scores per token come from a gating network whose form the paper
@@ -531,6 +533,79 @@ craft_status craft_decode_attention_workspace(const craft_kv_cache *cache, const
                                               size_t *bytes);
 craft_status craft_decode_attention(const craft_kv_cache *cache, const craft_attention_args *args,
                                     void *stream);
+
+/* ------------------------------------------------------- 8-bit integers, products by expert
+ * Not in the paper: what a rank multiplies besides its fused layer.  Activations and weights of 8
+ * bits take half the time of bf16 on the matrix cores, and a grouped product by itself serves
+ * experts that are no SwiGLU, or an order of rows that is not the dispatch's.  A chain of
+ *   craft_quantize_i8 -> craft_grouped_matmul (w_up given) -> craft_quantize_i8 ->
+ *   craft_grouped_matmul
+ * is the expert FFN in 8 bits; craft_matmul_i8 is the dense product of projections.
+ *
+ * craft_quantize_i8: rows of activations or weights to signed 8-bit integers with a scale each,
+ *   scale[r] = max_k |x[r][k]| / 127 in fp32, at least 2^-126; 1 for an all-zero row
+ *   codes[r][k] = the integer nearest to the fp32 quotient x[r][k] / scale[r], ties to even
+ *   A row with a NaN or an infinity gets scale NaN and codes 0: all products with it are NaN.
+ *     dtype CRAFT_F32 or CRAFT_BF16;  x DEVICE [rows][K], a row every x_stride elements (rows and x
+ *     16-byte aligned);  codes DEVICE [rows][K] contiguous, 16-byte aligned;  scale DEVICE [rows]
+ *     K % 16 == 0;  rows may be 0
+ *
+ * craft_matmul_i8: out[m][n] = x_scale[m] * w_scale[n] * sum_k x[m][k] * w[n][k]
+ *   The sum is a 32-bit integer and exact; it is converted to fp32, multiplied by x_scale[m], then by
+ *   w_scale[n], and rounded to out_dtype (CRAFT_F32 or CRAFT_BF16).
+ *     x DEVICE [M][K], a row every x_stride bytes (a multiple of 16);  w DEVICE [N][K] contiguous;
+ *     both 16-byte aligned;  x_scale DEVICE [M];  w_scale DEVICE [N];  out DEVICE [M][N], a row every
+ *     out_stride elements (faster where rows are 16-byte aligned)
+ *     K % 16 == 0, K < 131072;  N <= 2^30;  M < 2^31, may be 0
+ */
+craft_status craft_quantize_i8(int32_t dtype, const void *x, int64_t x_stride, int64_t rows, int32_t K,
+                               int8_t *codes, float *scale, void *stream);
+craft_status craft_matmul_i8(int64_t M, int32_t N, int32_t K, const int8_t *x, int64_t x_stride,
+                             const float *x_scale, const int8_t *w, const float *w_scale,
+                             int32_t out_dtype, void *out, int64_t out_stride, void *stream);
+
+/* Rows sorted by group (expert slot) against each group's matrix:
+ *   out[p][n] = sum_k X[p][k] * w[g][n][k]                      for off[g] <= p < off[g+1]
+ *   out[p][n] = silu(sum_k X[p][k] w[g][n][k]) * (sum_k X[p][k] w_up[g][n][k])  where w_up is given
+ * X[p] is row p of x, or row src[p] / k where src is given (as craft_moe_rank_forward's src and k).
+ *   format     CRAFT_F32, CRAFT_BF16 (fp32 sums, rounded once) or CRAFT_I8 (as craft_matmul_i8, with
+ *              x_scale[row of x], w_scale[g][n] and up_scale[g][n])
+ *   out_dtype  the format itself; CRAFT_F32 or CRAFT_BF16 for CRAFT_I8
+ *   M          places of out (and of x or src): off[G] <= M.  Places behind off[G] are left as they
+ *              were, and so are those in front of off[0].  Offsets outside [0, M] count as the nearer
+ *              end, a group that ends before it begins has no rows; groups that overlap leave any of
+ *              their results
+ *   x          DEVICE [M][K], or [x_rows][K] with src; a row every x_stride elements, rows 16-byte
+ *              aligned
+ *   src        DEVICE [M] int32, optional; a place whose row is outside [0, x_rows) gets zeros.
+ *              x_rows and k are ignored without src
+ *   off        DEVICE [G+1] int32
+ *   w, w_up    DEVICE arrays of G device pointers to [N][K] matrices, 16-byte aligned; the same matrix
+ *              may stand in several places, and groups without rows may hold any pointer
+ *   w_scale, up_scale  DEVICE arrays of G device pointers to [N] fp32, CRAFT_I8 only
+ *   out        DEVICE [M][N], a row every out_stride elements; must not overlap x
+ * Which rows a group has is read on the GPU: a recorded call follows the offsets of each replay.  The
+ * result depends on the arguments only, never on scheduling.
+ * Limits: G <= 1024;  rows of x and w are whole multiples of 16 bytes, shorter than 8 MiB;
+ * K < 131072 for CRAFT_I8;  N <= 2^30;  M, x_rows < 2^31, M may be 0. */
+typedef struct {
+    int32_t format, out_dtype;
+    int32_t G, N, K, k;
+    int64_t M, x_rows;
+    const void *x;
+    int64_t x_stride;
+    const float *x_scale;
+    const int32_t *src;
+    const int32_t *off;
+    const void *const *w;
+    const void *const *w_up;
+    const float *const *w_scale;
+    const float *const *up_scale;
+    void *out;
+    int64_t out_stride;
+} craft_grouped_matmul_args;
+
+craft_status craft_grouped_matmul(const craft_grouped_matmul_args *args, void *stream);
 
 /* ------------------------------------------------------------ kernel timing
  * Optional HIP-event timing of the kernels inside craft_moe_rank_forward, recorded on the

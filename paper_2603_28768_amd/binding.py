@@ -15,7 +15,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcraft.so")
 
-CRAFT_F32, CRAFT_BF16 = 0, 1
+CRAFT_F32, CRAFT_BF16, CRAFT_I8 = 0, 1, 2
 CRAFT_W_BF16, CRAFT_W_E4M3 = 0, 1
 CRAFT_KV_F32, CRAFT_KV_BF16, CRAFT_KV_E4M3 = 0, 1, 2
 KERNEL_NAMES = ["route", "scan", "dispatch", "gateup", "down", "combine", "gate"]
@@ -62,6 +62,12 @@ class AttentionArgs(ctypes.Structure):
                 ("out", c_vp), ("lse", c_vp), ("workspace", c_vp), ("workspace_bytes", c_sz)]
 
 
+class GroupedMatmulArgs(ctypes.Structure):
+    _fields_ = [("format", c_i32), ("out_dtype", c_i32), ("G", c_i32), ("N", c_i32), ("K", c_i32), ("k", c_i32),
+                ("M", c_i64), ("x_rows", c_i64), ("x", c_vp), ("x_stride", c_i64), ("x_scale", c_vp), ("src", c_vp), ("off", c_vp),
+                ("w", c_vp), ("w_up", c_vp), ("w_scale", c_vp), ("up_scale", c_vp), ("out", c_vp), ("out_stride", c_i64)]
+
+
 EXPORTS = {
     "craft_status_str": (ctypes.c_char_p, [ctypes.c_int]),
     "craft_router_logits_workspace": (ctypes.c_int, [c_i32, c_i64, c_i32, c_i32, P(c_sz)]),
@@ -101,6 +107,9 @@ EXPORTS = {
     "craft_kv_append": (ctypes.c_int, [P(KvCacheDesc), c_i64, c_vp, c_i64, c_vp, c_i64, c_vp, c_vp]),
     "craft_decode_attention_workspace": (ctypes.c_int, [P(KvCacheDesc), P(AttentionArgs), P(c_sz)]),
     "craft_decode_attention": (ctypes.c_int, [P(KvCacheDesc), P(AttentionArgs), c_vp]),
+    "craft_quantize_i8": (ctypes.c_int, [c_i32, c_vp, c_i64, c_i64, c_i32, c_vp, c_vp, c_vp]),
+    "craft_matmul_i8": (ctypes.c_int, [c_i64, c_i32, c_i32, c_vp, c_i64, c_vp, c_vp, c_vp, c_i32, c_vp, c_i64, c_vp]),
+    "craft_grouped_matmul": (ctypes.c_int, [P(GroupedMatmulArgs), c_vp]),
     "craft_probe_copy": (ctypes.c_int, [c_vp, c_vp, c_i64, c_vp]),
     "craft_probe_read": (ctypes.c_int, [c_vp, c_i64, c_i32, c_i32, c_vp, P(ctypes.c_double), c_vp]),
     "craft_probe_mfma_bf16": (ctypes.c_int, [c_i32, c_i32, c_vp, P(ctypes.c_double), c_vp]),
@@ -660,6 +669,140 @@ class DecodeAttention:
         if rc:
             _check(rc, "craft_decode_attention")
         return self.out
+
+
+# ---------------------------------------------- 8-bit integers, products by expert
+
+def _matrix(t, rows, row_elements, gpu, dtype):
+    """Checks a cuda matrix with contiguous rows; the elements between its rows."""
+    assert t.dtype == dtype and t.get_device() == gpu and t.shape == (rows, row_elements)
+    stride, one = t.stride()
+    assert one == 1 or row_elements == 1
+    return stride if rows > 1 else max(stride, row_elements)
+
+
+def quantize_i8(x, codes=None, scale=None, stream=None):
+    """cuda [rows][K], float32 or bfloat16, rows contiguous and 16-byte aligned -> (codes int8 [rows][K], scale float32
+    [rows]), new or written into those given."""
+    import torch
+    assert x.is_cuda and x.dim() == 2 and x.dtype in (torch.float32, torch.bfloat16)
+    rows, K = x.shape
+    gpu = x.get_device()
+    stride = _matrix(x, rows, K, gpu, x.dtype)
+    if codes is None:
+        codes = torch.empty((rows, K), dtype=torch.int8, device=x.device)
+    if scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    assert codes.dtype == torch.int8 and codes.get_device() == gpu and codes.shape == (rows, K) and codes.is_contiguous()
+    assert scale.dtype == torch.float32 and scale.get_device() == gpu and scale.shape == (rows,) and scale.is_contiguous()
+    rc = lib().craft_quantize_i8(CRAFT_BF16 if x.dtype == torch.bfloat16 else CRAFT_F32, x.data_ptr(), stride if rows > 1 else K, rows, K,
+                                 codes.data_ptr(), scale.data_ptr(), _stream_on(gpu, stream))
+    if rc:
+        _check(rc, "craft_quantize_i8")
+    return codes, scale
+
+
+def matmul_i8(x, x_scale, w, w_scale, dtype: str = "bf16", out=None, stream=None):
+    """x: cuda int8 [M][K] (rows 16-byte aligned), w: int8 [N][K], with float32 scales [M] and [N], as quantize_i8 makes them
+    -> [M][N] of `dtype` ("bf16" or "f32"), new or written into `out`, whose type then counts."""
+    import torch
+    assert x.is_cuda and x.dim() == 2 and w.dim() == 2
+    (M, K), N, gpu = x.shape, w.shape[0], x.get_device()
+    stride = _matrix(x, M, K, gpu, torch.int8)
+    assert w.dtype == torch.int8 and w.get_device() == gpu and w.shape == (N, K) and w.is_contiguous()
+    for t, n in ((x_scale, M), (w_scale, N)):
+        assert t.dtype == torch.float32 and t.get_device() == gpu and t.shape == (n,) and t.is_contiguous()
+    if out is None:
+        out = torch.empty((M, N), dtype=_torch_dtype(dtype), device=x.device)
+    assert out.dtype in (torch.float32, torch.bfloat16)
+    rc = lib().craft_matmul_i8(M, N, K, x.data_ptr(), stride if M > 1 else K, x_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(),
+                               CRAFT_BF16 if out.dtype == torch.bfloat16 else CRAFT_F32, out.data_ptr(), _matrix(out, M, N, gpu, out.dtype),
+                               _stream_on(gpu, stream))
+    if rc:
+        _check(rc, "craft_matmul_i8")
+    return out
+
+
+class GroupedMatmul:
+    """Products of rows sorted by expert with each expert's matrix, for repeated calls with the same weights.
+
+    weights: cuda [G][N][K], or a sequence of G contiguous cuda [N][K] matrices (the same one may stand in several places),
+    float32, bfloat16 or int8; `up`, likewise: the product is silu(x w^T) * (x up^T).  scales, up_scales: for int8, float32
+    [G][N] or a sequence of G of [N].  dtype: of the result, "f32" or "bf16"; given for int8 only (bf16 unless given)."""
+
+    def __init__(self, weights, scales=None, up=None, up_scales=None, dtype: Optional[str] = None):
+        import torch
+        weights = list(weights)
+        assert weights, "no experts"
+        first = weights[0]
+        formats = {torch.float32: CRAFT_F32, torch.bfloat16: CRAFT_BF16, torch.int8: CRAFT_I8}
+        assert first.is_cuda and first.dim() == 2 and first.dtype in formats
+        self.G, (self.N, self.K), self._gpu, dev = len(weights), first.shape, first.get_device(), first.device
+        eight = first.dtype == torch.int8
+        natural = {torch.float32: "f32", torch.bfloat16: "bf16", torch.int8: "bf16"}[first.dtype]
+        assert dtype is None or eight or dtype == natural, "only 8-bit products have a choice of result"
+        self.dtype, self.out_dtype = first.dtype, _torch_dtype(dtype or natural)
+        assert (scales is not None) == eight and (up_scales is not None) == (eight and up is not None)
+        self._keep = []
+
+        def pointers(items, shape, kind):
+            if items is None:
+                return None
+            items = list(items)
+            assert len(items) == self.G
+            for t in items:
+                assert t.dtype == kind and t.get_device() == self._gpu and t.shape == shape and t.is_contiguous() and t.data_ptr() % 16 == 0
+            table = torch.tensor([t.data_ptr() for t in items], dtype=torch.int64, device=dev)
+            self._keep += [items, table]
+            return table.data_ptr()
+
+        def scale_pointers(items):
+            # (a row of an odd [G][N] need not be 16-byte aligned)
+            if items is None:
+                return None
+            items = list(items)
+            assert len(items) == self.G
+            for t in items:
+                assert t.dtype == torch.float32 and t.get_device() == self._gpu and t.shape == (self.N,) and t.is_contiguous()
+            table = torch.tensor([t.data_ptr() for t in items], dtype=torch.int64, device=dev)
+            self._keep += [items, table]
+            return table.data_ptr()
+
+        a = GroupedMatmulArgs()
+        a.format, a.out_dtype = formats[first.dtype], CRAFT_BF16 if self.out_dtype == torch.bfloat16 else CRAFT_F32
+        a.G, a.N, a.K = self.G, self.N, self.K
+        a.w, a.w_up = pointers(weights, first.shape, first.dtype), pointers(up, first.shape, first.dtype)
+        a.w_scale, a.up_scale = scale_pointers(scales), scale_pointers(up_scales)
+        self.args, self._ref, self._call = a, ctypes.byref(a), lib().craft_grouped_matmul
+        self._int32, self._float32 = torch.int32, torch.float32
+
+    def __call__(self, x, off, x_scale=None, src=None, k: int = 1, out=None, stream=None):
+        """x: cuda [rows][K] of the weights' type, rows 16-byte aligned; x_scale: float32 [rows], for int8; off: int32 [G + 1], group
+        g's products are rows off[g] .. off[g + 1]; src: int32 [M], product p then takes row src[p] // k of x.  Returns
+        [M][N], new or written into `out`; rows of no group are left as they were (a new result: anything)."""
+        import torch
+        a, gpu = self.args, self._gpu
+        assert x.dim() == 2 and off.dtype == self._int32 and off.get_device() == gpu and off.shape == (self.G + 1,) and off.is_contiguous()
+        rows = x.shape[0]
+        stride = _matrix(x, rows, self.K, gpu, self.dtype)
+        M = rows
+        if src is not None:
+            M = src.shape[0]
+            assert src.dtype == self._int32 and src.get_device() == gpu and src.shape == (M,) and src.is_contiguous()
+        assert (x_scale is not None) == (a.format == CRAFT_I8)
+        if x_scale is not None:
+            assert x_scale.dtype == self._float32 and x_scale.get_device() == gpu and x_scale.shape == (rows,) and x_scale.is_contiguous()
+        if out is None:
+            out = torch.empty((M, self.N), dtype=self.out_dtype, device=x.device)
+        a.M, a.x_rows, a.k = M, rows, k
+        a.x, a.x_stride, a.off = x.data_ptr(), stride if rows > 1 else self.K, off.data_ptr()
+        a.x_scale = None if x_scale is None else x_scale.data_ptr()
+        a.src = None if src is None else src.data_ptr()
+        a.out, a.out_stride = out.data_ptr(), _matrix(out, M, self.N, gpu, self.out_dtype)
+        rc = self._call(self._ref, _stream_on(gpu, stream))
+        if rc:
+            _check(rc, "craft_grouped_matmul")
+        return out
 
 
 def probe_copy(src, dst, stream=None):

@@ -14,7 +14,8 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcraft.so")
 
 SOURCES = ["planner.cpp", "forward.cpp", "route.hip", "router.hip", "dispatch.hip", "load.hip", "ffn.hip", "ffn_packed.hip", "ffn_stream.hip", "pack.hip", "quant.hip", "probe.hip",
-           "combine.hip", "kv_cache.cpp", "kv_cache.hip", "attention.hip", "attention_latent.hip"]
+           "combine.hip", "kv_cache.cpp", "kv_cache.hip", "attention.hip", "attention_latent.hip",
+           "product.cpp", "product_stream.hip", "quant_i8.hip"]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

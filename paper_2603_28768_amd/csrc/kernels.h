@@ -332,4 +332,39 @@ int32_t latent_workers(const AttentionArgs &a, int32_t num_cu);
 size_t latent_workspace(const AttentionArgs &a, int32_t num_cu);
 hipError_t launch_latent_attention(const AttentionArgs &a, void *workspace, hipStream_t s);
 
+// ---- products, alone and grouped by expert (product_stream.hip), 8-bit integers (quant_i8.hip) ----
+struct QuantizeI8Args {
+    int32_t dtype;
+    int64_t rows;
+    int32_t K;
+    int64_t x_stride;              // bytes
+    const unsigned char *x;
+    int8_t *codes;
+    float *scale;
+};
+hipError_t launch_quantize_i8(const QuantizeI8Args &a, hipStream_t s);
+
+struct ProductArgs {
+    int32_t format, out_dtype;     // CRAFT_F32, _BF16, _I8 of x and w; CRAFT_F32 or _BF16
+    int32_t G, N;
+    int32_t row_bytes;             // of the contraction
+    int32_t k;
+    int64_t M, x_rows;
+    int64_t x_stride;              // bytes
+    int64_t out_stride;            // elements
+    const unsigned char *x;
+    const float *x_scale;          // [x_rows], 8 bits only
+    const int32_t *src;            // [M] or null
+    const int32_t *off;            // [G + 1]; null: one group of M rows
+    const unsigned char *const *w, *const *up;      // [G] matrices; up null: no gate
+    const float *const *w_scale, *const *up_scale;
+    const unsigned char *w_one;    // the matrix and its scales where off is null
+    const float *w_one_scale;
+    void *out;
+    int32_t out_whole;             // rows of the result aligned to four elements
+    int32_t num_cu;
+};
+constexpr int32_t kMostGroups = 1024;
+hipError_t launch_product(const ProductArgs &a, hipStream_t s);
+
 }  // namespace craft

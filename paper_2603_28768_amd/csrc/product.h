@@ -1,0 +1,94 @@
+// Matrix products whose operands are both stored row by row along the contraction, out = x w^T, of three kinds of numbers:
+// fp32, bf16 (fp32 sums) and 8-bit integers (32-bit integer sums, exact), alone or grouped by expert.
+//
+// All kernels see rows as bytes: an operand fragment is 16 rows x 64 bytes, lane l holding bytes 16 (l >> 4) .. + 15 of row
+// l & 15.  That is 16 codes, 8 bf16 values or 4 floats of the contraction; which of them meet in one matrix
+// instruction does not matter as long as both operands agree.
+#pragma once
+
+#include "kernels.h"
+
+namespace craft {
+
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+typedef float pf32x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 pbf16x8_t __attribute__((ext_vector_type(8)));
+typedef unsigned int raw_t __attribute__((ext_vector_type(4)));        // 16 bytes of a row
+
+template <int FMT> struct Numbers;
+template <> struct Numbers<CRAFT_F32> {
+    typedef pf32x4_t acc_t;
+    static __device__ __forceinline__ void multiply(raw_t w, raw_t x, acc_t &c) {
+        const pf32x4_t a = __builtin_bit_cast(pf32x4_t, w), b = __builtin_bit_cast(pf32x4_t, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    }
+};
+template <> struct Numbers<CRAFT_BF16> {
+    typedef pf32x4_t acc_t;
+    static __device__ __forceinline__ void multiply(raw_t w, raw_t x, acc_t &c) {
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pbf16x8_t, w), __builtin_bit_cast(pbf16x8_t, x), c, 0, 0, 0);
+    }
+};
+template <> struct Numbers<CRAFT_I8> {
+    typedef i32x4_t acc_t;
+    static __device__ __forceinline__ void multiply(raw_t w, raw_t x, acc_t &c) {
+        c = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4_t, w), __builtin_bit_cast(i32x4_t, x), c, 0, 0, 0);
+    }
+};
+
+// Two fp32 values to a pair of bf16, to nearest even: one instruction.
+static __device__ __forceinline__ uint32_t product_bf16_pair(float lo, float hi) {
+    typedef __bf16 pair_t __attribute__((ext_vector_type(2)));
+    typedef float floats_t __attribute__((ext_vector_type(2)));
+    const floats_t v = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, pair_t));
+}
+
+// Four neighbouring columns of one row into the result, whatever its alignment: `whole` where rows and columns allow
+// one store.
+static __device__ __forceinline__ void store_columns(const ProductArgs &a, int64_t row, int32_t col, const float (&v)[4], bool whole) {
+    if (a.out_dtype == CRAFT_BF16) {
+        uint16_t *p = static_cast<uint16_t *>(a.out) + row * a.out_stride + col;
+        const uint2 two = make_uint2(product_bf16_pair(v[0], v[1]), product_bf16_pair(v[2], v[3]));
+        if (whole && col + 4 <= a.N) {
+            *reinterpret_cast<uint2 *>(p) = two;
+        } else {
+            const uint32_t u[2] = {two.x, two.y};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (col + i < a.N) p[i] = (uint16_t)(u[i >> 1] >> (16 * (i & 1)));
+        }
+    } else {
+        float *p = static_cast<float *>(a.out) + row * a.out_stride + col;
+        if (whole && col + 4 <= a.N) {
+            *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (col + i < a.N) p[i] = v[i];
+        }
+    }
+}
+
+// Row p of the products is row `token` of x; -1: the permutation names no row of x, and the result is zeros.
+static __device__ __forceinline__ int64_t token_of(const ProductArgs &a, int64_t p) {
+    if (!a.src) return p;
+    const int32_t s = a.src[p];
+    const int64_t t = s >= 0 ? s / a.k : -1;
+    return t < a.x_rows ? t : -1;
+}
+
+// Rows of group g, inside [0, M) whatever the offsets are.
+static __device__ __forceinline__ void group_rows(const ProductArgs &a, int32_t g, int64_t &lo, int64_t &hi) {
+    if (!a.off) {
+        lo = 0;
+        hi = a.M;
+        return;
+    }
+    const int64_t l = a.off[g], h = a.off[g + 1];
+    lo = l < 0 ? 0 : l < a.M ? l : a.M;
+    hi = h < lo ? lo : h < a.M ? h : a.M;
+}
+
+}  // namespace craft

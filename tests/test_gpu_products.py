@@ -1,0 +1,365 @@
+"""Products of 8-bit integers, their quantisation and products grouped by expert, on the GPU against plain forms on the host
+(product_reference.py says what is compared bit for bit and what within which bound)."""
+import numpy as np
+import pytest
+
+from paper_2603_28768_amd import binding
+
+import product_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+def _dev(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+
+
+# ---------------------------------------------------------------------- quantize
+
+def _hard_rows(g, rows, K):
+    """Rows of every size a float has: ties, powers of two, zeros, rows near both ends of the range."""
+    x = g.standard_normal((rows, K)).astype(np.float32)
+    kind = np.arange(rows) % 8
+    x[kind == 1] *= np.float32(1e-38)
+    x[kind == 2] *= np.float32(1e37)
+    x[kind == 3] = 0.0
+    # whole and half multiples of the scale: ties of the rounding
+    x[kind == 4] = np.rint(x[kind == 4] * 60).clip(-127, 127) * np.float32(0.5)
+    x[kind == 4, 0] = 127.0
+    x[kind == 5] *= np.float32(2.0 ** -140)
+    x[kind == 6, 1:] = 0.0
+    x[kind == 7] = np.ldexp(np.float32(1.0), g.integers(-120, 100, (int((kind == 7).sum()), 1))).astype(np.float32) * x[kind == 7]
+    return x
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,K,pad", [(1, 16, 0), (17, 48, 16), (40, 256, 0), (33, 272, 0), (9, 1040, 8), (250, 4096, 4096), (16, 6160, 0),
+                                        (8, 7168, 0), (16, 8192, 32), (24, 8208, 0), (8, 40000, 0), (3001, 64, 0)])
+def test_quantize_is_the_definition(torch_cuda, dtype, rows, K, pad):
+    torch = torch_cuda
+    print(f"quantize {dtype} {rows}x{K}+{pad}", flush=True)
+    x = _dev(_hard_rows(np.random.default_rng(rows + K), rows, K + pad)).to(binding._torch_dtype(dtype))[:, :K]
+    codes, scale = binding.quantize_i8(x)
+    want_codes, want_scale = ref.quantize(x.float().cpu().numpy())
+    assert np.array_equal(scale.cpu().numpy(), want_scale)
+    assert np.array_equal(codes.cpu().numpy(), want_codes)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("K", [16, 512, 7168, 16384])
+def test_quantize_marks_rows_that_are_not_finite(torch_cuda, dtype, K):
+    torch = torch_cuda
+    x = torch.randn((7, K), device=DEV).to(binding._torch_dtype(dtype))
+    x[1, 3], x[2, K - 1], x[3, 0], x[5, K // 2] = float("inf"), float("nan"), float("-inf"), float("-nan")
+    codes, scale = binding.quantize_i8(x)
+    want_codes, want_scale = ref.quantize(x.float().cpu().numpy())
+    assert np.array_equal(scale.cpu().numpy(), want_scale, equal_nan=True) and np.isnan(want_scale).sum() == 4
+    assert np.array_equal(codes.cpu().numpy(), want_codes)
+
+
+# ------------------------------------------------------------------------ matmul
+
+def _codes(g, rows, K, most=127):
+    return g.integers(-most, most + 1, (rows, K)).astype(np.int8), np.exp(g.uniform(-9, 3, rows)).astype(np.float32)
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", [
+    (1, 1, 16), (1, 64, 64), (1, 7168, 4096), (2, 17, 144), (16, 16, 128), (17, 33, 2064), (31, 5, 48), (61, 4099, 272), (64, 257, 1040), (65, 200, 512),
+    (128, 130, 8192), (129, 512, 112), (250, 1000, 640), (256, 256, 256), (257, 511, 400), (777, 300, 1552), (1025, 1537, 2048), (3000, 70, 96), (40, 40, 131056)])
+def test_matmul_is_exact(torch_cuda, out, M, N, K):
+    torch = torch_cuda
+    print(f"matmul {M}x{N}x{K} {out}", flush=True)
+    g = np.random.default_rng(M * 31 + N)
+    (x, xs), (w, ws) = _codes(g, M, K), _codes(g, N, K)
+    got = binding.matmul_i8(_dev(x), _dev(xs), _dev(w), _dev(ws), dtype=out)
+    want = _dev(ref.product(x, w, xs, ws)[0]).to(got.dtype)
+    assert torch.equal(got, want)
+
+
+def test_matmul_at_the_ends_of_the_integers(torch_cuda):
+    # the longest contraction of the largest codes stays inside 32 bits, with either sign
+    torch = torch_cuda
+    K = 131056
+    x = np.full((20, K), -128, np.int8)
+    x[1::2] = 127
+    w = np.full((18, K), -128, np.int8)
+    w[::3] = 127
+    one = np.ones(20, np.float32)
+    got = binding.matmul_i8(_dev(x), _dev(one), _dev(w), _dev(one[:18]), dtype="f32")
+    assert torch.equal(got.cpu(), torch.from_numpy(ref.product(x, w, one, one[:18])[0]))
+
+
+@pytest.mark.parametrize("M,N,K,pad,out_pad,out", [(37, 70, 208, 48, 1, "bf16"), (300, 257, 512, 16, 3, "f32"), (600, 96, 1024, 512, 32, "bf16"), (1, 50, 64, 0, 7, "f32")])
+def test_matmul_of_views(torch_cuda, M, N, K, pad, out_pad, out):
+    torch = torch_cuda
+    g = np.random.default_rng(M)
+    (x, xs), (w, ws) = _codes(g, M, K), _codes(g, N, K)
+    wide = torch.full((M, K + pad), 99, dtype=torch.int8, device=DEV)
+    wide[:, :K] = _dev(x)
+    room = torch.full((M + 2, N + out_pad), -7.0, dtype=binding._torch_dtype(out), device=DEV)
+    view = room[1:M + 1, :N]
+    assert binding.matmul_i8(wide[:, :K], _dev(xs), _dev(w), _dev(ws), out=view) is view
+    assert torch.equal(view, _dev(ref.product(x, w, xs, ws)[0]).to(view.dtype))
+    room[1:M + 1, :N] = -7.0
+    assert bool((room == -7.0).all())
+
+
+def test_matmul_shows_a_row_that_was_not_finite(torch_cuda):
+    torch = torch_cuda
+    x = torch.randn((70, 512), device=DEV)
+    x[3, 5], x[66, 0] = float("inf"), float("nan")
+    got = binding.matmul_i8(*binding.quantize_i8(x), *binding.quantize_i8(torch.randn((300, 512), device=DEV)))
+    bad = got.isnan().all(dim=1)
+    assert bad.nonzero().flatten().tolist() == [3, 66] and not bool(got[~bad].isnan().any())
+
+
+def test_no_rows_is_no_work(torch_cuda):
+    torch = torch_cuda
+    w, ws = torch.zeros((4, 32), dtype=torch.int8, device=DEV), torch.ones(4, device=DEV)
+    assert binding.matmul_i8(torch.zeros((0, 32), dtype=torch.int8, device=DEV), ws[:0], w, ws).shape == (0, 4)
+    assert binding.quantize_i8(torch.zeros((0, 32), device=DEV))[0].shape == (0, 32)
+    off = torch.zeros(2, dtype=torch.int32, device=DEV)
+    assert binding.GroupedMatmul(torch.zeros((1, 4, 32), device=DEV))(torch.zeros((0, 32), device=DEV), off).shape == (0, 4)
+
+
+# ----------------------------------------------------------------------- grouped
+
+class Problem:
+    """Operands of a grouped product on the host and on the GPU."""
+
+    def __init__(self, seed, fmt, sizes, N, K, is_gated, out="bf16", k=0, front=0, spare=0, whole=False, pad=0, out_pad=0):
+        import torch
+        g = np.random.default_rng(seed)
+        self.fmt, self.N, self.K, self.k, self.gated = fmt, N, K, k, is_gated
+        self.off = np.concatenate([[front], front + np.cumsum(sizes)]).astype(np.int32)
+        self.M = int(self.off[-1]) + spare
+        self.G = len(sizes)
+        rows = self.M if k == 0 else max(1, self.M // 2)
+        self.src = g.integers(0, rows * k, self.M).astype(np.int32) if k else None
+        self.xs = self.ws = self.us = None
+        self.out_dtype = {"bf16": torch.bfloat16, "f32": torch.float32}[out if fmt == "i8" else fmt]
+        if fmt == "i8":
+            self.x, self.xs = _codes(g, rows, K)
+            self.xs *= np.float32(K ** -0.5 / 2000)
+            mats = [_codes(g, N, K) for _ in range(2 * self.G)]
+            self.w, self.ws = np.stack([m[0] for m in mats[:self.G]]), np.stack([m[1] for m in mats[:self.G]])
+            self.u, self.us = np.stack([m[0] for m in mats[self.G:]]), np.stack([m[1] for m in mats[self.G:]])
+        else:
+            # small whole numbers: sums of up to 2^14 products of at most 2^6 are exact in fp32
+            make = (lambda *s: g.integers(-8, 9, s).astype(np.float32)) if whole else lambda *s: g.standard_normal(s).astype(np.float32)
+            kind = binding._torch_dtype(fmt)
+            stored = lambda a: torch.from_numpy(a).to(kind).float().numpy()  # noqa: E731
+            scale = np.float32(1.0 if whole else K ** -0.5)
+            self.x, self.w, self.u = stored(make(rows, K)), stored(make(self.G, N, K) * scale), stored(make(self.G, N, K) * scale)
+        t = (lambda a: _dev(a)) if fmt == "i8" else (lambda a: _dev(a).to(binding._torch_dtype(fmt)))  # noqa: E731
+        wide = torch.zeros((rows, K + pad), dtype=torch.int8 if fmt == "i8" else binding._torch_dtype(fmt), device=DEV)
+        wide[:, :K] = t(self.x)
+        self.d_x = wide[:, :K]
+        self.d_w, self.d_u = t(self.w), t(self.u) if is_gated else None
+        self.d_xs = None if self.xs is None else _dev(self.xs)
+        self.d_off, self.d_src = _dev(self.off), None if self.src is None else _dev(self.src)
+        s = lambda a: None if a is None else _dev(a)  # noqa: E731
+        self.handle = binding.GroupedMatmul(self.d_w, scales=s(self.ws), up=self.d_u, up_scales=s(self.us) if is_gated else None,
+                                            dtype=out if fmt == "i8" else None)
+        self.room = torch.full((self.M, N + out_pad), -7.0, dtype=self.out_dtype, device=DEV)
+        self.out = self.room[:, :N]
+
+    def run(self, **kw):
+        args = dict(x_scale=self.d_xs, src=self.d_src, k=max(self.k, 1), out=self.out)
+        args.update(kw)
+        return self.handle(self.d_x, self.d_off, **args)
+
+    def check(self, got, off=None):
+        """Rows of groups within their bounds (equal where nothing is gated and sums are exact), others untouched."""
+        import torch
+        got = got.cpu()
+        off = self.off if off is None else off
+        seen = np.zeros(self.M, bool)
+        rows = self.x.shape[0]
+        for g, lo, hi in ref.rows_of(None, off, self.M):
+            seen[lo:hi] = True
+            token = np.arange(lo, hi) if self.src is None else np.where(self.src[lo:hi] >= 0, self.src[lo:hi] // max(self.k, 1), -1)
+            live = (token >= 0) & (token < rows)
+            at = np.where(live, token, 0)
+            xs = None if self.xs is None else self.xs[at]
+            a, ea = ref.product(self.x[at], self.w[g], xs, None if self.ws is None else self.ws[g])
+            mine = got[lo:hi]
+            assert bool((mine[torch.from_numpy(~live)] == 0).all())
+            if self.gated:
+                b, eb = ref.product(self.x[at], self.u[g], xs, None if self.us is None else self.us[g])
+                a, bound = ref.gated(a, ea, b, eb, self.out_dtype)
+            elif ea is not None:
+                bound = ea + np.abs(a) * ref.U[self.out_dtype]
+            if not self.gated and (ea is None or self.exact):
+                want = torch.from_numpy(np.ascontiguousarray(a)).float().to(self.out_dtype)
+                assert torch.equal(mine[torch.from_numpy(live)], want[torch.from_numpy(live)]), g
+            else:
+                off_by = np.abs(mine.double().numpy() - a)[live]
+                assert bool((off_by <= bound[live]).all()), (g, float((off_by / bound[live]).max()))
+        rest = torch.from_numpy(~seen)
+        assert bool((got[rest] == -7.0).all())
+        assert bool((self.room[:, self.N:] == -7.0).all())
+
+    exact = False
+
+
+SIZES = [[1], [0, 1, 0], [3, 0, 16, 17, 1], [64, 65, 0, 31], [255, 0, 256, 257, 1], [700, 5, 90], [0] * 40 + [33] + [0] * 25 + [2], [2] * 130]
+
+
+@pytest.mark.parametrize("fmt,out", [("i8", "bf16"), ("i8", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("is_gated", [False, True])
+@pytest.mark.parametrize("which", range(len(SIZES)))
+def test_grouped_rows(torch_cuda, fmt, out, is_gated, which):
+    sizes = SIZES[which]
+    for N, K, k in ((48, 128, 0), (131, 272, 2), (300, 1040 if fmt != "f32" else 100, 8)):
+        print(f"grouped {fmt} {out} gated={is_gated} sizes={sizes[:6]} N={N} K={K} k={k}", flush=True)
+        p = Problem(which * 7 + N, fmt, sizes, N, K, is_gated, out=out, k=k, front=which % 3, spare=which % 4, whole=not is_gated)
+        p.exact = True
+        p.check(p.run())
+
+
+@pytest.mark.parametrize("fmt,out", [("i8", "bf16"), ("i8", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("is_gated", [False, True])
+@pytest.mark.parametrize("sizes,N,K,pad,out_pad", [([300, 17, 0, 520], 520, 1168, 32, 5), ([40, 1000], 257, 2000, 16, 0), ([5, 9, 2, 30], 1000, 4112, 0, 8)])
+def test_grouped_drawn_values(torch_cuda, fmt, out, is_gated, sizes, N, K, pad, out_pad):
+    if fmt == "f32":
+        K = K // 4 // 4 * 4
+    print(f"grouped drawn {fmt} {out} gated={is_gated} {sizes} N={N} K={K}", flush=True)
+    p = Problem(N, fmt, sizes, N, K, is_gated, out=out, k=3, spare=2, pad=pad, out_pad=out_pad)
+    p.check(p.run())
+
+
+@pytest.mark.parametrize("fmt", ["i8", "bf16", "f32"])
+@pytest.mark.parametrize("off", [[5, 2, 9, 9], [-4, 30, 20, 1000], [40, 60, 80, 33], [90, 95, 95, 2000000000], [-2000000000, 0, 0, 0]])
+def test_offsets_that_are_none_stay_inside(torch_cuda, fmt, off):
+    torch = torch_cuda
+    print(f"offsets {fmt} {off}", flush=True)
+    p = Problem(3, fmt, [20, 30, 27], 72, 320, False, out="bf16", whole=True, spare=3)
+    p.exact = True
+    off = np.asarray(off, np.int32)
+    got = p.handle(p.d_x, _dev(off), x_scale=p.d_xs, out=p.out)
+    covered = [r for g, lo, hi in ref.rows_of(None, off, p.M) for r in range(lo, hi)]
+    if len(set(covered)) == len(covered):
+        p.check(got, off)
+
+
+@pytest.mark.parametrize("fmt", ["i8", "bf16", "f32"])
+@pytest.mark.parametrize("is_gated", [False, True])
+@pytest.mark.parametrize("rows", [20, 300])
+def test_places_that_name_no_row_are_zeros(torch_cuda, fmt, is_gated, rows):
+    p = Problem(5, fmt, [rows, 7, rows], 100, 144, is_gated, k=4, whole=True, out="f32")
+    p.exact = True
+    p.src[::3] = -1
+    p.src[1::5] = p.x.shape[0] * 4
+    p.src[2::7] = 2 ** 31 - 1
+    p.d_src = _dev(p.src)
+    p.check(p.run())
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [9, 300])
+def test_infinities_and_nan_stay_in_their_rows(torch_cuda, fmt, rows):
+    # the last pieces of rows that end inside a slab: what is read in place of the rest may hold anything
+    torch = torch_cuda
+    K = 208 if fmt == "bf16" else 100
+    p = Problem(11, fmt, [rows, 40], 90, K, False, whole=True)
+    x = p.d_x.clone().abs() + 1
+    w = p.d_w.clone().abs() + 1
+    x[2, K - 1], x[rows + 5, K - 8], x[4, 0] = float("inf"), float("nan"), float("-inf")
+    w[1, 7, K - 1] = float("inf")
+    got = binding.GroupedMatmul(w)(x, p.d_off).float().cpu()
+    want = torch.full((p.M, 90), 0.0)
+    want[2], want[4], want[rows + 5] = float("inf"), float("-inf"), float("nan")
+    want[rows:, 7] = float("inf")
+    want[rows + 5] = float("nan")
+    odd = ~torch.isfinite(got)
+    assert torch.equal(odd, ~torch.isfinite(want))
+    assert torch.equal(got[odd].nan_to_num(7.0, 8.0, 9.0), want[odd].nan_to_num(7.0, 8.0, 9.0))
+
+
+def test_one_matrix_in_several_places(torch_cuda):
+    # copies of an expert share its weights
+    torch = torch_cuda
+    p = Problem(8, "i8", [30, 70, 5], 64, 256, False, out="f32")
+    one = binding.GroupedMatmul([p.d_w[0], p.d_w[0], p.d_w[2]], scales=[_dev(p.ws[0]), _dev(p.ws[0]), _dev(p.ws[2])], dtype="f32")
+    p.w[1], p.ws[1] = p.w[0], p.ws[0]
+    p.check(one(p.d_x, p.d_off, x_scale=p.d_xs, out=p.out))
+
+
+@pytest.mark.parametrize("fmt", ["i8", "bf16", "f32"])
+@pytest.mark.parametrize("is_gated", [False, True])
+def test_recorded_calls_follow_their_inputs(torch_cuda, fmt, is_gated):
+    # offsets, rows and activations change between replays; eager calls of the same handle in between
+    torch = torch_cuda
+    p = Problem(21, fmt, [200, 3, 0, 300, 40], 136, 528, is_gated, k=2, spare=9, out="bf16")
+    other = torch.empty_like(p.out)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        p.run()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.run()
+    g = np.random.default_rng(5)
+    for sizes in ([1, 1, 1, 1, 1], [0, 0, 543, 0, 0], [100, 100, 100, 100, 100], [200, 3, 0, 300, 40]):
+        p.off = np.concatenate([[0], np.cumsum(sizes)]).astype(np.int32)
+        p.src = g.integers(0, p.x.shape[0] * 2, p.M).astype(np.int32)
+        p.d_off.copy_(_dev(p.off))
+        p.d_src.copy_(_dev(p.src))
+        p.out.fill_(-7.0)
+        graph.replay()
+        p.check(p.out)
+        again = p.run(out=other.fill_(-7.0))
+        torch.cuda.synchronize()
+        assert torch.equal(again, p.out)
+
+
+def test_calls_on_a_stream_of_their_own(torch_cuda):
+    torch = torch_cuda
+    p = Problem(2, "i8", [90, 400, 11], 200, 512, True, out="bf16")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = p.run(stream=side)
+    x, xs = binding.quantize_i8(torch.ones((5, 64), device=DEV), stream=side)
+    y = binding.matmul_i8(x, xs, x, xs, dtype="f32", stream=side)
+    side.synchronize()
+    p.check(got)
+    assert torch.equal(x, torch.full_like(x, 127)) and bool((y - 64.0).abs().max() <= 64 * 6 * 2.0 ** -24)
+
+
+@pytest.mark.parametrize("T,H,I,E,k", [(40, 256, 208, 6, 2), (700, 512, 400, 5, 3)])
+def test_expert_layer_in_8_bits(torch_cuda, T, H, I, E, k):
+    """A run of the operators together: quantize, gate and up by expert, quantize, down by expert; against the same steps in
+    64 bits on the codes' values.  What separates the two: the gated product's rounding to bf16 and its own bound carry over
+    into codes, off by at most one and then by one scale."""
+    torch = torch_cuda
+    g = np.random.default_rng(T)
+    x = _dev(g.standard_normal((T, H)).astype(np.float32)).bfloat16()
+    weights = {n: binding.quantize_i8(_dev((g.standard_normal((E * r, c)) * c ** -0.5).astype(np.float32)))
+               for n, r, c in (("gate", I, H), ("up", I, H), ("down", H, I))}
+    shaped = {n: (c.view(E, -1, c.shape[1]), s.view(E, -1)) for n, (c, s) in weights.items()}
+    ids = np.stack([g.choice(E, k, replace=False) for _ in range(T)]).reshape(-1)
+    src = np.argsort(ids, kind="stable").astype(np.int32)
+    off = np.concatenate([[0], np.cumsum(np.bincount(ids, minlength=E))]).astype(np.int32)
+    first = binding.GroupedMatmul(shaped["gate"][0], scales=shaped["gate"][1], up=shaped["up"][0], up_scales=shaped["up"][1])
+    second = binding.GroupedMatmul(shaped["down"][0], scales=shaped["down"][1], dtype="f32")
+    xq, xs = binding.quantize_i8(x)
+    h = first(xq, _dev(off), x_scale=xs, src=_dev(src), k=k)
+    hq, hs = binding.quantize_i8(h)
+    y = second(hq, _dev(off), x_scale=hs).cpu().double().numpy()
+    val = {n: (c.double() * s.double()[..., None]).cpu().numpy() for n, (c, s) in shaped.items()}
+    xv = (xq.double() * xs.double()[:, None]).cpu().numpy()[src // k]
+    scale = hs.cpu().double().numpy()
+    for e in range(E):
+        r = slice(off[e], off[e + 1])
+        a, b = xv[r] @ val["gate"][e].T, xv[r] @ val["up"][e].T
+        hv = a / (1 + np.exp(-a)) * b
+        # codes: half a scale from h, h a bf16 rounding (2^-8) from hv
+        bound = (0.5 + 2.0 ** -7) * scale[r, None] + np.abs(hv) * 2.0 ** -7
+        off_by = np.abs(y[r] - hv @ val["down"][e].T)
+        assert (off_by <= bound @ np.abs(val["down"][e]).T + 1e-5 * np.abs(y[r])).all()
