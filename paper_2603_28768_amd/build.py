@@ -15,7 +15,7 @@ LIB = os.path.join(HERE, "libcraft.so")
 
 SOURCES = ["planner.cpp", "forward.cpp", "route.hip", "router.hip", "dispatch.hip", "load.hip", "ffn.hip", "ffn_packed.hip", "ffn_stream.hip", "pack.hip", "quant.hip", "probe.hip",
            "combine.hip", "kv_cache.cpp", "kv_cache.hip", "attention.hip", "attention_latent.hip",
-           "product.cpp", "product_stream.hip", "quant_i8.hip"]
+           "product.cpp", "product_stream.hip", "product_tile_i8.hip", "product_tile_bf16.hip", "product_tile_f32.hip", "quant_i8.hip"]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -32,7 +32,8 @@ def _hipcc() -> str:
 # Sources whose matrix instructions (ffn_packed.hip) or loads into LDS are written as asm
 # statements, which the compiler's hazard pass does not recognise: their emitted code is checked
 # here instead (check_matrix_operands).
-ASM_MFMA_SOURCES = {"ffn_packed.hip", "ffn.hip", "router.hip", "attention_latent.hip"}
+ASM_MFMA_SOURCES = {"ffn_packed.hip", "ffn.hip", "router.hip", "attention_latent.hip",
+                    "product_tile_i8.hip", "product_tile_bf16.hip", "product_tile_f32.hip"}
 
 
 def _registers(token: str) -> set:

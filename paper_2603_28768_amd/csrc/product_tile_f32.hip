@@ -1,0 +1,7 @@
+#include "product_tile.h"
+
+namespace craft {
+
+hipError_t launch_product_tiles_f32(const ProductArgs &a, int32_t height, hipStream_t s) { return launch_tiles<CRAFT_F32>(a, height, s); }
+
+}  // namespace craft
