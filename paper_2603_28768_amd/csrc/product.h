@@ -45,6 +45,12 @@ static __device__ __forceinline__ uint32_t product_bf16_pair(float lo, float hi)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, pair_t));
 }
 
+// silu for fp32 results, and for those rounded to bf16 right after: the hardware's exponential and reciprocal (2^-21 off
+// where silu matters), with numerator and denominator scaled down alike, since a reciprocal below 2^-126 becomes zero
+// (g < -87.3, where silu times a large second factor still is a number).
+static __device__ __forceinline__ float silu_f32(float g) { return g / (1.0f + expf(-g)); }
+static __device__ __forceinline__ float silu_bf16(float g) { return g * 0x1p-8f * __builtin_amdgcn_rcpf(fmaf(__expf(-g), 0x1p-8f, 0x1p-8f)); }
+
 // Four neighbouring columns of one row into the result, whatever its alignment: `whole` where rows and columns allow
 // one store.
 static __device__ __forceinline__ void store_columns(const ProductArgs &a, int64_t row, int32_t col, const float (&v)[4], bool whole) {

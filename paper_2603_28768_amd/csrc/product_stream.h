@@ -16,9 +16,6 @@ struct Unit {
     int64_t row0;                  // its first row among the M
 };
 
-// fp32 results: the library exponential; those rounded to bf16: the hardware one (2^-21 off where silu matters)
-static __device__ __forceinline__ float silu_of(float g, bool exact) { return g / (1.0f + (exact ? expf(-g) : __expf(-g))); }
-
 template <int FMT, bool GATED, int CF, int RF, int WAVES>
 static __device__ __forceinline__ void stream_unit(const ProductArgs &a, const Unit &u, typename Numbers<FMT>::acc_t *part) {
     typedef Numbers<FMT> T;
@@ -117,7 +114,7 @@ static __device__ __forceinline__ void stream_unit(const ProductArgs &a, const U
         }
         if constexpr (GATED)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[0][e] = silu_of(v[0][e], FMT == CRAFT_F32 || a.out_dtype == CRAFT_F32) * v[1][e];
+            for (int e = 0; e < 4; ++e) v[0][e] = (FMT == CRAFT_F32 || a.out_dtype == CRAFT_F32 ? silu_f32(v[0][e]) : silu_bf16(v[0][e])) * v[1][e];
         if (t < 0)
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[0][e] = 0.0f;

@@ -1,12 +1,13 @@
 // Products with many rows a group: tiles of up to 256 rows of x against 256 rows of the weights, one workgroup of four
-// waves per CU.
+// waves (2 x 2 over the tile) per CU.
 //
-// Rows of x go from memory straight into LDS (loads that write LDS, ffn_common.h), in slabs of 128 bytes, four
-// stages, three slabs ahead; every wave reads all of them as operand fragments.  Each wave has 64 weight rows of its own,
-// whose fragments it loads straight into registers, four slabs ahead: nobody else needs them, and LDS then carries 80
-// bytes a cycle at full speed where both operands by way of it would be 96 (of 128).  A step of 64 bytes is multiplied in
-// halves of the tile's rows, while one half is multiplied the other's fragments are fetched; every memory instruction
-// is dealt out behind a matrix instruction of its own.
+// Both operands go from memory straight into LDS (loads that write LDS, ffn_common.h) in slabs of 128 bytes a row, whole
+// lines: a CU gets 123 GB/s that way, and 38 where lanes load operand fragments of row-major weights themselves (16 rows a
+// request; the same tile 265 us so, 8192 x 4096 x 7168).  An LDS row is unpadded, its eight 16-byte pieces in the order piece ^
+// (row & 7), so that the reads of a fragment hit every bank once.  A slab is two steps of 64 bytes.  While one step is multiplied,
+// all fragments of the next are read into the other set of registers: behind the first step of a slab its stage
+// is free again, and the slab that takes its place is requested at once.  Every memory instruction is dealt out behind a matrix
+// instruction of its own.
 //
 // Groups are cut into full tiles of `height` rows and one remainder: of more than 64 rows a lower tile, of fewer units
 // of product_stream.h.  The list has all full tiles first, then remainders.
@@ -23,9 +24,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kTileColumns = 256;                  // weight rows of a tile (gated: half of them gate, half up)
-constexpr int kStages = 4;
 constexpr int kSlab = 128;                         // bytes of the contraction
-constexpr int kStageBytes = 256 * kSlab;
+constexpr int kTileLds = 2 * 512 * kSlab;
+template <int FW, int FX> constexpr int tile_stages() { return 3 * (FW + FX) * 32 * kSlab <= kTileLds + (16 << 10) ? 3 : 2; }
 constexpr int kRemCF = 2;                          // columns / 16 of a remainder's unit
 
 template <int FMT> static __device__ __forceinline__ void multiply_in_place(raw_t w, raw_t x, typename Numbers<FMT>::acc_t &c) {
@@ -47,229 +48,206 @@ struct Tile {
     int64_t row0;
 };
 
-// 32 HF rows against four waves' 16 CF weight rows each.
-template <int FMT, bool GATED, int HF, int CF>
+// FW, FX: 16-row fragments of weights and of x per wave; the tile is 32 FW columns (gated: 16 FW) x 32 FX rows.
+template <int FMT, bool GATED, int FW, int FX>
 static __device__ __forceinline__ void product_tile(const ProductArgs &a, const Tile &t, unsigned char *smem, float *row_scale, uint8_t *row_live) {
     typedef typename Numbers<FMT>::acc_t acc_t;
-    constexpr int M = HF * CF;
+    constexpr int M = FW * FX, NR = FW + FX, STAGE = NR * 32 * kSlab, S = tile_stages<FW, FX>();
+    static_assert(S * STAGE <= kTileLds + (16 << 10), "stages");
     const int lane = threadIdx.x & 63, q = lane >> 4, r16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int32_t KB = a.row_bytes, nk = (KB + kSlab - 1) / kSlab;
-    // Rows of x: chunk 4 i + wave of eight rows is this wave's i-th.
+    // Chunk 4 i + wave, eight rows of an operand, is this wave's i-th.  In front of LDS: weights, then x.
+    const uint32_t piece = (uint32_t)(((lane & 7) ^ ((lane >> 3) & 7)) * 16);
     const bool gather = a.src != nullptr;
     const ubase_t xbase = uniform_base(gather ? a.x : a.x + t.row0 * a.x_stride);
-    uint32_t aoff[HF];
+    uint32_t woff[FW], xoff[FX];
 #pragma unroll
-    for (int i = 0; i < HF; ++i) {
+    for (int i = 0; i < FX; ++i) {
         const int r = min(8 * (4 * i + wave) + (lane >> 3), t.rows - 1);
         const int64_t tok = gather ? token_of(a, t.row0 + r) : r;
-        aoff[i] = (uint32_t)((tok < 0 ? 0 : tok) * a.x_stride) + (uint32_t)(((lane & 7) ^ ((lane >> 3) & 7)) * 16);
+        xoff[i] = (uint32_t)((tok < 0 ? 0 : tok) * a.x_stride) + piece;
     }
     if ((int)threadIdx.x < t.rows) {
         const int64_t tok = token_of(a, t.row0 + threadIdx.x);
         row_live[threadIdx.x] = tok >= 0;
         if (FMT == CRAFT_I8) row_scale[threadIdx.x] = a.x_scale[tok < 0 ? 0 : tok];
     }
-    // Weight rows: fragment c of this wave is 16 columns (gated: of gate and up in turn).
-    const ubase_t w0 = uniform_base(a.off ? a.w[t.group] : a.w_one), w1 = GATED ? uniform_base(a.up[t.group]) : w0;
-    constexpr int SIDES = GATED ? 2 : 1;
-    auto column = [&](int c) { return t.n0 + (wave * (CF / SIDES) + c / SIDES) * 16; };
-    uint32_t boff[CF];
-    const ubase_t wt0 = w0 + (int64_t)t.n0 * KB, wt1 = w1 + (int64_t)t.n0 * KB;
+    // Gated: 16 rows of gate are followed by the 16 of up of the same columns; the first two waves fetch gate's.
+    const unsigned char *mat = a.off ? a.w[t.group] : a.w_one;
+    if (GATED && wave >= 2) mat = a.up[t.group];
+    const ubase_t wbase = uniform_base(mat + (int64_t)t.n0 * KB);
+    auto column = [](int r) { return GATED ? (r >> 5) * 16 + (r & 15) : r; };
 #pragma unroll
-    for (int c = 0; c < CF; ++c) boff[c] = (uint32_t)(min(column(c) + r16, a.N - 1) - t.n0) * (uint32_t)KB + (uint32_t)(q * 16);
+    for (int i = 0; i < FW; ++i) woff[i] = (uint32_t)min(column(8 * (4 * i + wave) + (lane >> 3)), a.N - 1 - t.n0) * (uint32_t)KB + piece;
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
     const uint32_t lds_wave = lds0 + (uint32_t)__builtin_amdgcn_readfirstlane(wave * 1024);
     const uint32_t fo = lds0 + (uint32_t)(r16 * 128 + ((q ^ (lane & 7)) & 7) * 16);
+    const uint32_t fw0 = fo + (uint32_t)((wave >> 1) * FW * 2048), fx0 = fo + (uint32_t)((2 * FW + (wave & 1) * FX) * 2048);
     typedef const raw_t __attribute__((address_space(3))) *frag_t;
 
-    raw_t av[2][HF], bv[4][2][CF];
-    acc_t acc[2 * HF][CF];
+    raw_t wv[2][FW], xv[2][FX];
+    acc_t acc[FW][FX];
 #pragma unroll
-    for (int f = 0; f < 2 * HF; ++f)
+    for (int f = 0; f < FW; ++f)
 #pragma unroll
-        for (int c = 0; c < CF; ++c) acc[f][c] = acc_t{};
+        for (int g = 0; g < FX; ++g) acc[f][g] = acc_t{};
 
     // where slab ks begins in a row: the last one ends with it, and what the one before has is cut away
     auto at = [&](int ks) __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_readfirstlane(min(ks * kSlab, KB - kSlab)); };
-    auto aim = [&](int i, int stage) __attribute__((always_inline)) { dma_to(lds_wave + (uint32_t)(stage * kStageBytes + 4096 * i)); };
-    auto request = [&](int i, uint32_t k) __attribute__((always_inline)) { dma_request(xbase + k, aoff[i]); };
-    auto weights = [&](int u, int step, int c, uint32_t k) __attribute__((always_inline)) {
-        bv[u][step][c] = wload<false, raw_t>(((c & (SIDES - 1)) ? wt1 : wt0) + k + step * 64, boff[c]);
+    auto aim = [&](int i, uint32_t stage) __attribute__((always_inline)) { dma_to(lds_wave + stage + (uint32_t)(4096 * i)); };
+    auto request = [&](int i, uint32_t k) __attribute__((always_inline)) {
+        if (i < FW) dma_request(wbase + k, woff[i < FW ? i : 0]);
+        else dma_request(xbase + k, xoff[i < FW ? 0 : i - FW]);
     };
-    auto fetch = [&](int half, int stage, int f) __attribute__((always_inline)) {
-        const uint32_t base = (half & 2 ? fo ^ 64u : fo) + (uint32_t)(stage * kStageBytes);
-        av[half & 1][f] = *(frag_t)(uintptr_t)(base + (uint32_t)(((half & 1) * HF + f) * 2048));
+    // x's fragments first, the next products start with those
+    auto fetch = [&](int set, int j, uint32_t stage, int step) __attribute__((always_inline)) {
+        if (j < FX) xv[set][j < FX ? j : 0] = *(frag_t)(uintptr_t)((fx0 ^ (step ? 64u : 0u)) + stage + (uint32_t)(j * 2048));
+        else wv[set][j < FX ? 0 : j - FX] = *(frag_t)(uintptr_t)((fw0 ^ (step ? 64u : 0u)) + stage + (uint32_t)((j - FX) * 2048));
     };
-    auto cut_a = [&](int half) __attribute__((always_inline)) {
-        const bool gone = (half & 2 ? 64 : 0) + q * 16 < nk * kSlab - KB;
+    // bytes of the last slab that the one before it has already; a matrix instruction may read what a vector instruction wrote
+    // two cycles later
+    auto cut = [&](int set) __attribute__((always_inline)) {
+        const bool gone = set * 64 + q * 16 < nk * kSlab - KB;
 #pragma unroll
-        for (int f = 0; f < HF; ++f) {
-            av[half & 1][f] = gone ? raw_t{} : av[half & 1][f];
-            asm volatile("s_nop 1" : "+v"(av[half & 1][f]));
+        for (int g = 0; g < FX; ++g) {
+            xv[set][g] = gone ? raw_t{} : xv[set][g];
+            asm volatile("s_nop 1" : "+v"(xv[set][g]));
+        }
+#pragma unroll
+        for (int f = 0; f < FW; ++f) {
+            wv[set][f] = gone ? raw_t{} : wv[set][f];
+            asm volatile("s_nop 1" : "+v"(wv[set][f]));
         }
     };
-    auto cut_b = [&](int u) __attribute__((always_inline)) {
-#pragma unroll
-        for (int step = 0; step < 2; ++step) {
-            const bool gone = step * 64 + q * 16 < nk * kSlab - KB;
-#pragma unroll
-            for (int c = 0; c < CF; ++c) {
-                bv[u][step][c] = gone ? raw_t{} : bv[u][step][c];
-                asm volatile("s_nop 1" : "+v"(bv[u][step][c]));
-            }
-        }
-    };
-    // Half `half` of the slab in stage u: columns outside, so that a column's weights are free behind its products.
-    // dma: rows of slab ks + 3 are requested (in halves 0 and 1); more: weights of slab ks + 4 (in half 3).
-    auto half_of = [&](auto U, auto HALF, bool dma, bool more, uint32_t kdma, uint32_t kmore) __attribute__((always_inline)) {
-        constexpr int u = U.value, half = HALF.value, next = (half + 1) & 3, next_stage = half == 3 ? (u + 1) & 3 : u;
-        constexpr int D0 = half == 0 ? 0 : (HF + 1) / 2, ND = half == 0 ? (HF + 1) / 2 : half == 1 ? HF / 2 : 0;
-        constexpr int OPS = HF + 2 * ND;
+    // One step: set STEP multiplied, the other one read from `stage`; DMA: slab `k` requested into `to` as well.
+    auto step_of = [&](auto STEP, auto DMA, uint32_t stage, uint32_t to, uint32_t k) __attribute__((always_inline)) {
+        constexpr int set = STEP.value, OPS = DMA.value ? 3 * NR : NR;
 #pragma unroll
         for (int m = 0; m < M; ++m) {
-            const int c = m / HF, f = m % HF;
-            multiply_in_place<FMT>(bv[u][half >> 1][c], av[half & 1][f], acc[(half & 1) * HF + f][c]);
+            multiply_in_place<FMT>(wv[set][m / FX], xv[set][m % FX], acc[m / FX][m % FX]);
+            // spread over three quarters of the step: what is read has to be there when the next one begins
 #pragma unroll
-            for (int o = m * OPS / M; o < (m + 1) * OPS / M; ++o) {
-                if (o < HF) fetch(next, next_stage, o);
-                else if (dma) {
-                    const int i = D0 + (o - HF) / 2;
-                    if ((o - HF) % 2 == 0) aim(i, (u + 3) & 3);
-                    else {
-                        if (o > m * OPS / M) asm volatile("s_nop 0");
-                        request(i, kdma);
-                    }
+            for (int o = min(m * OPS * 4 / (3 * M), OPS); o < min((m + 1) * OPS * 4 / (3 * M), OPS); ++o) {
+                if (!DMA.value) {
+                    fetch(set ^ 1, o, stage, set ^ 1);
+                } else if (o % 3 == 0) {
+                    dma_to(lds_wave + to + (uint32_t)(4096 * (o / 3)));
+                } else if (o % 3 == 1) {
+                    fetch(set ^ 1, o / 3, stage, set ^ 1);
+                } else {
+                    request(o / 3, k);
                 }
-            }
-            if (half == 3 && f == HF - 1 && more) {
-                weights(u, 0, c, kmore);
-                weights(u, 1, c, kmore);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    const std::integral_constant<int, 0> step0;
+    const std::integral_constant<int, 1> step1;
+    const std::true_type with;
+    const std::false_type without;
     const bool cuts = nk * kSlab != KB;
-    // AHEAD: everything that is requested exists
-    auto slab = [&](auto U, auto AHEAD, int ks) __attribute__((always_inline)) {
-        constexpr int u = U.value;
-        constexpr bool ahead = AHEAD.value;
-        const bool dma = ahead || ks + 3 < nk, more = ahead || ks + 4 < nk, last = !ahead && ks + 1 == nk;
-        const uint32_t kdma = at(ks + 3), kmore = at(ks + 4);
-        if (last && cuts) { cut_b(u); cut_a(0); }
-        half_of(U, std::integral_constant<int, 0>{}, dma, more, kdma, kmore);
-        if (last && cuts) cut_a(1);
-        half_of(U, std::integral_constant<int, 1>{}, dma, more, kdma, kmore);
-        if (last && cuts) cut_a(2);
-        half_of(U, std::integral_constant<int, 2>{}, dma, more, kdma, kmore);
-        // Slab ks + 1 has landed when at most what was requested behind it is on its way: weights and rows of two slabs
-        // (the tail: fewer).  At the barrier all of slab ks has been read by every wave.
-        if (dma) dma_wait<4 * CF + 2 * HF>();
-        else if (ks + 3 == nk) dma_wait<2 * CF + HF>();
-        else dma_wait<0>();
-        __syncthreads();
-        if (last && cuts) cut_a(3);
-        half_of(U, std::integral_constant<int, 3>{}, dma, more, kdma, kmore);
-    };
-    const std::integral_constant<int, 0> u0;
-    const std::integral_constant<int, 1> u1;
-    const std::integral_constant<int, 2> u2;
-    const std::integral_constant<int, 3> u3;
 
-    auto start_rows = [&](int j) __attribute__((always_inline)) {
-        if (j < nk) {
 #pragma unroll
-            for (int i = 0; i < HF; ++i) {
-                aim(i, j);
+    for (int j = 0; j < S; ++j)
+        if (j < nk) {
+            const uint32_t k = at(j);
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                aim(i, j * STAGE);
                 asm volatile("s_nop 0");
-                request(i, at(j));
+                request(i, k);
             }
         }
-    };
-    auto start_weights = [&](auto J) __attribute__((always_inline)) {
-        constexpr int j = J.value;
-        if (j < nk)
-#pragma unroll
-            for (int c = 0; c < CF; ++c) {
-                weights(j, 0, c, at(j));
-                weights(j, 1, c, at(j));
-            }
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    start_rows(0);
-    start_weights(u0);
-    start_rows(1);
-    start_weights(u1);
-    start_rows(2);
-    start_weights(u2);
-    start_weights(u3);
-    if (nk > 3) dma_wait<8 * CF + 2 * HF <= 63 ? 8 * CF + 2 * HF : 63>();
+    if (nk >= S) dma_wait<(S - 1) * NR>();
     else dma_wait<0>();
     __syncthreads();
 #pragma unroll
-    for (int f = 0; f < HF; ++f) fetch(0, 0, f);
+    for (int j = 0; j < NR; ++j) fetch(0, j, 0, 0);
+    uint32_t here = 0;
     int ks = 0;
-    const std::true_type ahead;
-    const std::false_type bounded;
-    for (; ks + 8 <= nk; ks += 4) {
-        slab(u0, ahead, ks);
-        slab(u1, ahead, ks + 1);
-        slab(u2, ahead, ks + 2);
-        slab(u3, ahead, ks + 3);
+    // Behind the first step all of slab ks is in registers, for every wave at the barrier, and slab ks + 1 has landed: what is
+    // on its way by then are the slabs behind it.
+    for (; ks + S < nk; ++ks) {
+        const uint32_t there = here + STAGE < S * STAGE ? here + STAGE : 0;
+        step_of(step0, without, here, 0, 0);
+        dma_wait<(S - 2) * NR>();
+        __syncthreads();
+        step_of(step1, with, there, here, at(ks + S));
+        here = there;
     }
-    for (; ks < nk; ks += 4) {
-        slab(u0, bounded, ks);
-        if (ks + 1 >= nk) break;
-        slab(u1, bounded, ks + 1);
-        if (ks + 2 >= nk) break;
-        slab(u2, bounded, ks + 2);
-        if (ks + 3 >= nk) break;
-        slab(u3, bounded, ks + 3);
+    for (; ks < nk; ++ks) {
+        const uint32_t there = here + STAGE < S * STAGE ? here + STAGE : 0;
+        const bool last = ks + 1 == nk;
+        if (last && cuts) cut(0);
+        step_of(step0, without, here, 0, 0);
+        dma_wait<0>();
+        __syncthreads();
+        if (last && cuts) cut(1);
+        step_of(step1, without, there, 0, 0);      // (behind the last slab: read and not used)
+        here = there;
     }
     // a matrix instruction's result is read: idle cycles, then every accumulator through a statement behind them
     asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
-    for (int f = 0; f < 2 * HF; ++f)
+    for (int f = 0; f < FW; ++f)
 #pragma unroll
-        for (int c = 0; c < CF; ++c) asm volatile("" : "+a"(acc[f][c]));
+        for (int g = 0; g < FX; ++g) asm volatile("" : "+a"(acc[f][g]));
 
     // element v of lane l is column 4 (l >> 4) + v and row l & 15 of its fragment
-    const bool accurate = FMT == CRAFT_F32 || a.out_dtype == CRAFT_F32;
-    const float *scales[SIDES] = {};
+    constexpr int SIDES = GATED ? 2 : 1;
+    const int32_t col0 = t.n0 + column((wave >> 1) * FW * 16) + 4 * q, row_in = (wave & 1) * FX * 16 + r16;
+    float ws[FW][4];
     if (FMT == CRAFT_I8) {
-        scales[0] = a.off ? a.w_scale[t.group] : a.w_one_scale;
-        if (GATED) scales[SIDES - 1] = a.up_scale[t.group];
+        const float *s0 = a.off ? a.w_scale[t.group] : a.w_one_scale, *s1 = GATED ? a.up_scale[t.group] : s0;
+#pragma unroll
+        for (int f = 0; f < FW; ++f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ws[f][e] = (f & (SIDES - 1) ? s1 : s0)[min(col0 + f / SIDES * 16 + e, a.N - 1)];
     }
-    float ws[CF][4];
-    if (FMT == CRAFT_I8)
+    const int32_t out_whole = a.out_whole;
+    // results of fragment g's row: BF16 and WHOLE as the whole tile has them
+    auto results = [&](auto BF16, auto WHOLE) __attribute__((always_inline)) {
+        constexpr bool bf16 = BF16.value, whole = WHOLE.value;
 #pragma unroll
-        for (int c = 0; c < CF; ++c)
+        for (int g = 0; g < FX; ++g) {
+            const int row = row_in + 16 * g;
+            if (row < t.rows) {
+                const float xs = FMT == CRAFT_I8 ? row_scale[row] : 1.0f;
+                const bool live = row_live[row];
+                unsigned char *p = static_cast<unsigned char *>(a.out) + ((t.row0 + row) * a.out_stride + col0) * (bf16 ? 2 : 4);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) ws[c][e] = scales[c & (SIDES - 1)][min(column(c) + 4 * q + e, a.N - 1)];
+                for (int f = 0; f < FW; f += SIDES) {
+                    float v[SIDES][4];
 #pragma unroll
-    for (int f = 0; f < 2 * HF; ++f) {
-        const int row = 16 * f + r16;
-        if (row < t.rows) {
-            const float xs = FMT == CRAFT_I8 ? row_scale[row] : 1.0f;
-            const bool live = row_live[row];
+                    for (int m = 0; m < SIDES; ++m)
 #pragma unroll
-            for (int c = 0; c < CF; c += SIDES) {
-                const int32_t col = column(c) + 4 * q;
-                float v[SIDES][4];
+                        for (int e = 0; e < 4; ++e) v[m][e] = FMT == CRAFT_I8 ? (float)acc[f + m][g][e] * xs * ws[f + m][e] : (float)acc[f + m][g][e];
 #pragma unroll
-                for (int m = 0; m < SIDES; ++m)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[m][e] = FMT == CRAFT_I8 ? (float)acc[f][c + m][e] * xs * ws[c + m][e] : (float)acc[f][c + m][e];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if constexpr (GATED) v[0][e] = silu_of(v[0][e], accurate) * v[1][e];
-                    v[0][e] = live ? v[0][e] : 0.0f;
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (GATED) v[0][e] = (bf16 ? silu_bf16(v[0][e]) : silu_f32(v[0][e])) * v[SIDES - 1][e];
+                        v[0][e] = live ? v[0][e] : 0.0f;
+                    }
+                    if constexpr (whole) {
+                        if (bf16) *reinterpret_cast<uint2 *>(p + f / SIDES * 32) = make_uint2(product_bf16_pair(v[0][0], v[0][1]), product_bf16_pair(v[0][2], v[0][3]));
+                        else *reinterpret_cast<float4 *>(p + f / SIDES * 64) = make_float4(v[0][0], v[0][1], v[0][2], v[0][3]);
+                    } else {
+                        const int32_t col = col0 + f / SIDES * 16;
+                        if (col < a.N) store_columns(a, t.row0 + row, col, v[0], out_whole);
+                    }
                 }
-                if (col < a.N) store_columns(a, t.row0 + row, col, v[0], a.out_whole);
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
+    };
+    const bool whole = out_whole && t.n0 + 32 * FW / SIDES <= a.N;
+    if (FMT != CRAFT_F32 && a.out_dtype == CRAFT_BF16) {
+        if (whole) results(with, with);
+        else results(with, without);
+    } else {
+        if (whole) results(without, with);
+        else results(without, without);
     }
     __syncthreads();                               // LDS may be filled again
 }
@@ -339,7 +317,7 @@ static __device__ __forceinline__ void place(int32_t i, int32_t m, int32_t nt, i
 
 template <int FMT, bool GATED>
 __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a, int32_t height) {
-    __shared__ __attribute__((aligned(16))) unsigned char smem[kStages * kStageBytes];
+    __shared__ __attribute__((aligned(16))) unsigned char smem[kTileLds + (16 << 10)];
     __shared__ Counts n;
     __shared__ float row_scale[256];
     __shared__ uint8_t row_live[256];
@@ -375,10 +353,10 @@ __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a
         t.n0 = tc * COLS;
         t.rows = __builtin_amdgcn_readfirstlane(t.rows);
         t.n0 = __builtin_amdgcn_readfirstlane(t.n0);
-        if (t.rows <= 64) product_tile<FMT, GATED, 2, 4>(a, t, smem, row_scale, row_live);
-        else if (t.rows <= 128) product_tile<FMT, GATED, 4, 4>(a, t, smem, row_scale, row_live);
-        else if (t.rows <= 192) product_tile<FMT, GATED, 6, 4>(a, t, smem, row_scale, row_live);
-        else product_tile<FMT, GATED, 8, 4>(a, t, smem, row_scale, row_live);
+        if (t.rows <= 64) product_tile<FMT, GATED, 8, 2>(a, t, smem, row_scale, row_live);
+        else if (t.rows <= 128) product_tile<FMT, GATED, 8, 4>(a, t, smem, row_scale, row_live);
+        else if (t.rows <= 192) product_tile<FMT, GATED, 8, 6>(a, t, smem, row_scale, row_live);
+        else product_tile<FMT, GATED, 8, 8>(a, t, smem, row_scale, row_live);
     }
     for (; w < all; w += gridDim.x) {
         const int64_t i = w - low;
