@@ -15,6 +15,11 @@ typedef float pf32x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 pbf16x8_t __attribute__((ext_vector_type(8)));
 typedef unsigned int raw_t __attribute__((ext_vector_type(4)));        // 16 bytes of a row
 
+// Addresses read from a table in memory: said to be global, they are else read as flat ones, which wait for LDS as well.
+typedef const unsigned char __attribute__((address_space(1))) *bytes_t;
+typedef const raw_t __attribute__((address_space(1))) *pieces_t;
+typedef const float __attribute__((address_space(1))) *scales_t;
+
 template <int FMT> struct Numbers;
 template <> struct Numbers<CRAFT_F32> {
     typedef pf32x4_t acc_t;

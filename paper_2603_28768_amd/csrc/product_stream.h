@@ -25,17 +25,17 @@ static __device__ __forceinline__ void stream_unit(const ProductArgs &a, const U
     const int lane = threadIdx.x & 63, q = lane >> 4, r16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int32_t KB = a.row_bytes, slabs = (KB + 127) >> 7;
-    const unsigned char *w[WF], *x[RF];
+    bytes_t w[WF], x[RF];
 #pragma unroll
     for (int m = 0; m < MATS; ++m) {
-        const unsigned char *mat = a.off ? (m ? +a.up : +a.w)[u.group] : a.w_one;
+        const bytes_t mat = (bytes_t)(a.off ? (m ? +a.up : +a.w)[u.group] : a.w_one);
 #pragma unroll
         for (int c = 0; c < CF; ++c) w[m * CF + c] = mat + (int64_t)min(u.n0 + 16 * c + r16, a.N - 1) * KB;
     }
 #pragma unroll
     for (int g = 0; g < RF; ++g) {
         const int64_t t = token_of(a, u.row0 + min(16 * g + r16, u.rows - 1));
-        x[g] = a.x + (t < 0 ? 0 : t) * a.x_stride;
+        x[g] = (bytes_t)a.x + (t < 0 ? 0 : t) * a.x_stride;
     }
     raw_t wv[D][2][WF], xv[D][2][RF];
     // (pieces past the rows: read from inside them, replaced by zeros below)
@@ -44,9 +44,9 @@ static __device__ __forceinline__ void stream_unit(const ProductArgs &a, const U
         for (int step = 0; step < 2; ++step) {
             const int32_t at = min(slab * 128 + step * 64 + q * 16, KB - 16);
 #pragma unroll
-            for (int c = 0; c < WF; ++c) wv[d][step][c] = *reinterpret_cast<const raw_t *>(w[c] + at);
+            for (int c = 0; c < WF; ++c) wv[d][step][c] = *(pieces_t)(w[c] + at);
 #pragma unroll
-            for (int g = 0; g < RF; ++g) xv[d][step][g] = *reinterpret_cast<const raw_t *>(x[g] + at);
+            for (int g = 0; g < RF; ++g) xv[d][step][g] = *(pieces_t)(x[g] + at);
         }
     };
     acc_t acc[WF][RF];
@@ -104,7 +104,7 @@ static __device__ __forceinline__ void stream_unit(const ProductArgs &a, const U
         for (int m = 0; m < MATS; ++m) {
             if constexpr (FMT == CRAFT_I8) {
                 const float xs = a.x_scale[t < 0 ? 0 : t];
-                const float *ws = a.off ? (m ? +a.up_scale : +a.w_scale)[u.group] : a.w_one_scale;
+                const scales_t ws = (scales_t)(a.off ? (m ? +a.up_scale : +a.w_scale)[u.group] : a.w_one_scale);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[m][e] = (float)s[m][e] * xs * ws[min(col + e, a.N - 1)];
             } else {

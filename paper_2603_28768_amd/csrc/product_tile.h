@@ -102,9 +102,15 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
         else dma_request(xbase + k, xoff[i < FW ? 0 : i - FW]);
     };
     // x's fragments first, the next products start with those
-    auto fetch = [&](int set, int j, uint32_t stage, int step) __attribute__((always_inline)) {
-        if (j < FX) xv[set][j < FX ? j : 0] = *(frag_t)(uintptr_t)((fx0 ^ (step ? 64u : 0u)) + stage + (uint32_t)(j * 2048));
-        else wv[set][j < FX ? 0 : j - FX] = *(frag_t)(uintptr_t)((fw0 ^ (step ? 64u : 0u)) + stage + (uint32_t)((j - FX) * 2048));
+    struct From { uint32_t x, w; };                // one register each, fragments at constant offsets from them
+    auto from = [&](int step, uint32_t stage) __attribute__((always_inline)) {
+        From p = {(fx0 ^ (step ? 64u : 0u)) + stage, (fw0 ^ (step ? 64u : 0u)) + stage};
+        asm volatile("" : "+v"(p.x), "+v"(p.w));
+        return p;
+    };
+    auto fetch = [&](int set, int j, const From &p) __attribute__((always_inline)) {
+        if (j < FX) xv[set][j < FX ? j : 0] = *(frag_t)(uintptr_t)(p.x + (uint32_t)(j * 2048));
+        else wv[set][j < FX ? 0 : j - FX] = *(frag_t)(uintptr_t)(p.w + (uint32_t)((j - FX) * 2048));
     };
     // bytes of the last slab that the one before it has already; a matrix instruction may read what a vector instruction wrote
     // two cycles later
@@ -124,6 +130,7 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
     // One step: set STEP multiplied, the other one read from `stage`; DMA: slab `k` requested into `to` as well.
     auto step_of = [&](auto STEP, auto DMA, uint32_t stage, uint32_t to, uint32_t k) __attribute__((always_inline)) {
         constexpr int set = STEP.value, OPS = DMA.value ? 3 * NR : NR;
+        const From p = from(set ^ 1, stage);
 #pragma unroll
         for (int m = 0; m < M; ++m) {
             multiply_in_place<FMT>(wv[set][m / FX], xv[set][m % FX], acc[m / FX][m % FX]);
@@ -131,11 +138,11 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
 #pragma unroll
             for (int o = min(m * OPS * 4 / (3 * M), OPS); o < min((m + 1) * OPS * 4 / (3 * M), OPS); ++o) {
                 if (!DMA.value) {
-                    fetch(set ^ 1, o, stage, set ^ 1);
+                    fetch(set ^ 1, o, p);
                 } else if (o % 3 == 0) {
                     dma_to(lds_wave + to + (uint32_t)(4096 * (o / 3)));
                 } else if (o % 3 == 1) {
-                    fetch(set ^ 1, o / 3, stage, set ^ 1);
+                    fetch(set ^ 1, o / 3, p);
                 } else {
                     request(o / 3, k);
                 }
@@ -164,7 +171,7 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
     else dma_wait<0>();
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < NR; ++j) fetch(0, j, 0, 0);
+    for (int j = 0; j < NR; ++j) fetch(0, j, from(0, 0));
     uint32_t here = 0;
     int ks = 0;
     // Behind the first step all of slab ks is in registers, for every wave at the barrier, and slab ks + 1 has landed: what is
@@ -197,58 +204,76 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
 
     // element v of lane l is column 4 (l >> 4) + v and row l & 15 of its fragment
     constexpr int SIDES = GATED ? 2 : 1;
-    const int32_t col0 = t.n0 + column((wave >> 1) * FW * 16) + 4 * q, row_in = (wave & 1) * FX * 16 + r16;
+    const int32_t col0 = t.n0 + column((wave >> 1) * FW * 16) + 4 * q;
     float ws[FW][4];
     if (FMT == CRAFT_I8) {
-        const float *s0 = a.off ? a.w_scale[t.group] : a.w_one_scale, *s1 = GATED ? a.up_scale[t.group] : s0;
+        const scales_t s0 = (scales_t)(a.off ? a.w_scale[t.group] : a.w_one_scale), s1 = GATED ? (scales_t)a.up_scale[t.group] : s0;
 #pragma unroll
         for (int f = 0; f < FW; ++f)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) ws[f][e] = (f & (SIDES - 1) ? s1 : s0)[min(col0 + f / SIDES * 16 + e, a.N - 1)];
+            for (int e = 0; e < 4; ++e) {
+                const int32_t c = min(col0 + f / SIDES * 16 + e, a.N - 1);
+                if (f & (SIDES - 1)) ws[f][e] = s1[c];
+                else ws[f][e] = s0[c];
+            }
     }
-    const int32_t out_whole = a.out_whole;
-    // results of fragment g's row: BF16 and WHOLE as the whole tile has them
-    auto results = [&](auto BF16, auto WHOLE) __attribute__((always_inline)) {
-        constexpr bool bf16 = BF16.value, whole = WHOLE.value;
+    // By way of LDS, 16 rows at a time and each wave for itself, so that a store covers whole lines (16 rows of 32 bytes a
+    // request: 8 us a tile where this takes 3).  Stores are of 16 bytes whatever the alignment; a lane at the matrix' edge
+    // stores its columns one by one.
+    auto results = [&](auto BF16) __attribute__((always_inline)) {
+        constexpr bool bf16 = BF16.value;
+        typedef typename std::conditional<bf16, uint16_t, float>::type out_t;
+        typedef out_t piece_t __attribute__((ext_vector_type(16 / sizeof(out_t)), aligned(sizeof(out_t))));
+        constexpr int COLS = 16 * FW / SIDES, ROWB = COLS * (int)sizeof(out_t), PITCH = ROWB + 16;     // a row of this wave
+        constexpr int PER = ROWB / 16, EACH = 16 / (int)sizeof(out_t), PASSES = 16 * PER / 64;      // pieces of a row; elements of a piece
+        static_assert(4 * 16 * PITCH <= kTileLds, "rows of results");
+        unsigned char *const mine = smem + wave * (16 * PITCH);
+        const int32_t first = t.n0 + (wave >> 1) * COLS;
+        out_t *const out = static_cast<out_t *>(a.out) + first;
 #pragma unroll
         for (int g = 0; g < FX; ++g) {
-            const int row = row_in + 16 * g;
-            if (row < t.rows) {
-                const float xs = FMT == CRAFT_I8 ? row_scale[row] : 1.0f;
-                const bool live = row_live[row];
-                unsigned char *p = static_cast<unsigned char *>(a.out) + ((t.row0 + row) * a.out_stride + col0) * (bf16 ? 2 : 4);
+            int l = lane;                          // (places are worked out here, not in front of the loop for all of it)
+            asm volatile("" : "+v"(l));
+            const int row = (wave & 1) * FX * 16 + 16 * g + (l & 15);
+            const float xs = FMT == CRAFT_I8 ? row_scale[row] : 1.0f;
+            const bool live = row_live[row];
 #pragma unroll
-                for (int f = 0; f < FW; f += SIDES) {
-                    float v[SIDES][4];
+            for (int f = 0; f < FW; f += SIDES) {
+                float v[SIDES][4];
 #pragma unroll
-                    for (int m = 0; m < SIDES; ++m)
+                for (int m = 0; m < SIDES; ++m)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) v[m][e] = FMT == CRAFT_I8 ? (float)acc[f + m][g][e] * xs * ws[f + m][e] : (float)acc[f + m][g][e];
+                    for (int e = 0; e < 4; ++e) v[m][e] = FMT == CRAFT_I8 ? (float)acc[f + m][g][e] * xs * ws[f + m][e] : (float)acc[f + m][g][e];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if constexpr (GATED) v[0][e] = (bf16 ? silu_bf16(v[0][e]) : silu_f32(v[0][e])) * v[SIDES - 1][e];
-                        v[0][e] = live ? v[0][e] : 0.0f;
-                    }
-                    if constexpr (whole) {
-                        if (bf16) *reinterpret_cast<uint2 *>(p + f / SIDES * 32) = make_uint2(product_bf16_pair(v[0][0], v[0][1]), product_bf16_pair(v[0][2], v[0][3]));
-                        else *reinterpret_cast<float4 *>(p + f / SIDES * 64) = make_float4(v[0][0], v[0][1], v[0][2], v[0][3]);
-                    } else {
-                        const int32_t col = col0 + f / SIDES * 16;
-                        if (col < a.N) store_columns(a, t.row0 + row, col, v[0], out_whole);
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (GATED) v[0][e] = (bf16 ? silu_bf16(v[0][e]) : silu_f32(v[0][e])) * v[SIDES - 1][e];
+                    v[0][e] = live ? v[0][e] : 0.0f;
+                }
+                unsigned char *p = mine + (l & 15) * PITCH + (f / SIDES * 16 + 4 * (l >> 4)) * (int)sizeof(out_t);
+                if constexpr (bf16) *reinterpret_cast<uint2 *>(p) = make_uint2(product_bf16_pair(v[0][0], v[0][1]), product_bf16_pair(v[0][2], v[0][3]));
+                else *reinterpret_cast<float4 *>(p) = make_float4(v[0][0], v[0][1], v[0][2], v[0][3]);
+            }
+            // (the wave's own rows: its reads follow its writes)
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+            for (int i = 0; i < PASSES; ++i) {
+                const int r = (i * 64 + l) / PER, c = (i * 64 + l) % PER * EACH, at = (wave & 1) * FX * 16 + 16 * g + r;
+                const unsigned char *from = mine + r * PITCH + c * (int)sizeof(out_t);
+                const raw_t v = *reinterpret_cast<const raw_t *>(from);
+                if (at < t.rows) {
+                    out_t *p = out + (t.row0 + at) * a.out_stride + c;
+                    if (first + c + EACH <= a.N) *reinterpret_cast<piece_t *>(p) = __builtin_bit_cast(piece_t, v);
+                    else
+#pragma unroll 1
+                        for (int e = 0; first + c + e < a.N; ++e) p[e] = reinterpret_cast<const out_t *>(from)[e];
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    const bool whole = out_whole && t.n0 + 32 * FW / SIDES <= a.N;
-    if (FMT != CRAFT_F32 && a.out_dtype == CRAFT_BF16) {
-        if (whole) results(with, with);
-        else results(with, without);
-    } else {
-        if (whole) results(without, with);
-        else results(without, without);
-    }
+    __syncthreads();                               // every wave has read the last slab
+    if (FMT != CRAFT_F32 && a.out_dtype == CRAFT_BF16) results(with);
+    else results(without);
     __syncthreads();                               // LDS may be filled again
 }
 
@@ -257,6 +282,17 @@ struct Counts {
     int32_t full[kMostGroups + 1], low[kMostGroups + 1], few[kMostGroups + 1];
 };
 static __device__ __forceinline__ void count_tiles(const ProductArgs &a, int32_t height, Counts &n, int32_t *scratch) {
+    if (!a.off) {                                  // one group
+        if (threadIdx.x == 0) {
+            const int32_t rest = (int32_t)(a.M % height);
+            n.full[0] = n.low[0] = n.few[0] = 0;
+            n.full[1] = (int32_t)(a.M / height);
+            n.low[1] = rest > kUnitRows;
+            n.few[1] = rest > 0 && rest <= kUnitRows;
+        }
+        __syncthreads();
+        return;
+    }
     const int32_t each = (a.G + kThreads - 1) / kThreads, first = min((int32_t)threadIdx.x * each, a.G), last = min(first + each, a.G);
     int32_t sum[3] = {0, 0, 0};
     for (int32_t g = first; g < last; ++g) {
