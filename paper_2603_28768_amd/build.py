@@ -33,7 +33,7 @@ def _hipcc() -> str:
 # statements, which the compiler's hazard pass does not recognise: their emitted code is checked
 # here instead (check_matrix_operands).
 ASM_MFMA_SOURCES = {"ffn_packed.hip", "ffn.hip", "router.hip", "attention_latent.hip",
-                    "product_tile_i8.hip", "product_tile_bf16.hip", "product_tile_f32.hip"}
+                    "product_stream.hip", "product_tile_i8.hip", "product_tile_bf16.hip", "product_tile_f32.hip"}
 
 
 def _registers(token: str) -> set:

@@ -1,9 +1,4 @@
-// Products with few rows a group: the weights are read once, straight from memory into operand registers, and the
-// contraction is shared among the waves of a workgroup.
-//
-// A unit is 16 CF columns of one group's matrix (gated: of both) against up to 64 of its rows.  Wave v of the
-// workgroup takes slabs v, v + WAVES, .. of 128 bytes along the contraction, a ring of them on their way; the waves'
-// sums meet in LDS and are added in wave order (integers: any order gives the same).
+// Products with few rows a group, as units of product_stream.h, and which kernel takes a product.
 #include <algorithm>
 
 #include "product_stream.h"
@@ -11,69 +6,81 @@
 namespace craft {
 namespace {
 
-// Units' row blocks before each group, in LDS: [G + 1].
-template <int THREADS> static __device__ __forceinline__ void count_blocks(const ProductArgs &a, int32_t *before, int32_t *scratch) {
-    // a thread's run of neighbouring groups, then a scan over threads
-    const int32_t each = (a.G + THREADS - 1) / THREADS, first = min((int32_t)threadIdx.x * each, a.G), last = min(first + each, a.G);
+constexpr int kThreads = 64 * kStreamWaves;
+
+// Row blocks of 64 before each group, in LDS: [G + 1].  Every wave works them out for itself and stores the same, so
+// that no barrier is needed: a wave reads what it has written.
+static __device__ __forceinline__ void count_blocks(const ProductArgs &a, int32_t *before) {
+    const int lane = threadIdx.x & 63;
     int32_t sum = 0;
-    for (int32_t g = first; g < last; ++g) {
-        int64_t lo, hi;
-        group_rows(a, g, lo, hi);
-        const int32_t n = (int32_t)((hi - lo + kUnitRows - 1) / kUnitRows);
-        before[g] = n;
-        sum += n;
+    for (int32_t g0 = 0; g0 < a.G; g0 += 64) {
+        const int32_t g = g0 + lane;
+        int64_t lo = 0, hi = 0;
+        if (g < a.G) group_rows(a, g, lo, hi);
+        int32_t n = (int32_t)((hi - lo + kUnitRows - 1) / kUnitRows);
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int32_t up = __shfl_up(n, d, 64);
+            n += lane >= d ? up : 0;
+        }
+        n += sum;
+        if (g < a.G) before[g + 1] = n;
+        sum = __shfl(n, 63, 64);
     }
-    scratch[threadIdx.x] = sum;
-    __syncthreads();
-    for (int d = 1; d < THREADS; d *= 2) {
-        const int32_t add = (int)threadIdx.x >= d ? scratch[threadIdx.x - d] : 0;
-        __syncthreads();
-        scratch[threadIdx.x] += add;
-        __syncthreads();
-    }
-    int32_t at = scratch[threadIdx.x] - sum;
-    for (int32_t g = first; g < last; ++g) {
-        const int32_t n = before[g];
-        before[g] = at;
-        at += n;
-    }
-    if (threadIdx.x == THREADS - 1) before[a.G] = scratch[THREADS - 1];
-    __syncthreads();
+    before[0] = 0;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
-template <int FMT, bool GATED, int CF, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void product_stream_kernel(ProductArgs a) {
+// ROWS: most 16-row fragments of a unit
+template <int FMT, bool GATED, int CF, int ROWS, int SPLIT>
+__global__ __launch_bounds__(kThreads) void product_stream_kernel(ProductArgs a) {
     typedef typename Numbers<FMT>::acc_t acc_t;
-    __shared__ acc_t part[WAVES * CF * (GATED ? 2 : 1) * 4 * 64];
-    __shared__ int32_t before[kMostGroups + 1], scratch[64 * WAVES];
+    __shared__ __attribute__((aligned(16))) unsigned char smem[kStreamWaves * kRingBytes];
+    __shared__ int32_t before[kMostGroups + 1];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int32_t cols = (a.N + 16 * CF - 1) / (16 * CF);
-    count_blocks<64 * WAVES>(a, before, scratch);
+    count_blocks(a, before);
     const int64_t units = (int64_t)before[a.G] * cols;
-    for (int64_t w = blockIdx.x; w < units; w += gridDim.x) {
-        const int32_t block = (int32_t)(w / cols);
-        int32_t lo = 0, hi = a.G;                  // before[lo] <= block < before[hi]
+    // neighbouring units (the blocks of rows of the same columns, then the next columns) on one XCD
+    const int64_t place = (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
+    const int64_t first = SPLIT > 1 ? place : place * kStreamWaves + wave, step = (int64_t)gridDim.x * (SPLIT > 1 ? 1 : kStreamWaves);
+    for (int64_t w = first; w < units; w += step) {
+        int32_t lo = 0, hi = a.G;                  // before[lo] * cols <= w < before[hi] * cols
         while (hi - lo > 1) {
             const int32_t mid = (lo + hi) >> 1;
-            if (before[mid] <= block) lo = mid; else hi = mid;
+            if ((int64_t)before[mid] * cols <= w) lo = mid; else hi = mid;
         }
-        int64_t first, last;
-        group_rows(a, lo, first, last);
+        const int32_t blocks = before[hi] - before[lo];
+        const int64_t in = w - (int64_t)before[lo] * cols;
+        int64_t r0, r1;
+        group_rows(a, lo, r0, r1);
         Unit u;
         u.group = __builtin_amdgcn_readfirstlane(lo);
-        u.n0 = __builtin_amdgcn_readfirstlane((int32_t)(w % cols) * 16 * CF);
-        u.row0 = first + (int64_t)(block - before[lo]) * kUnitRows;
-        u.rows = __builtin_amdgcn_readfirstlane((int32_t)min((int64_t)kUnitRows, last - u.row0));
-        if (u.rows <= 16) stream_unit<FMT, GATED, CF, 1, WAVES>(a, u, part);
-        else if (u.rows <= 32) stream_unit<FMT, GATED, CF, 2, WAVES>(a, u, part);
-        else stream_unit<FMT, GATED, CF, 4, WAVES>(a, u, part);
+        u.n0 = __builtin_amdgcn_readfirstlane((int32_t)(in / blocks) * 16 * CF);
+        u.row0 = r0 + (in % blocks) * kUnitRows;
+        u.rows = __builtin_amdgcn_readfirstlane((int32_t)min((int64_t)kUnitRows, r1 - u.row0));
+        unsigned char *const ring = smem + wave * kRingBytes;
+        acc_t *const part = reinterpret_cast<acc_t *>(smem);
+        if (ROWS == 1 || u.rows <= 16) stream_unit<FMT, GATED, CF, 1, SPLIT>(a, u, ring, part);
+        else if (u.rows <= 32) stream_unit<FMT, GATED, CF, 2, SPLIT>(a, u, ring, part);
+        else stream_unit<FMT, GATED, CF, 4, SPLIT>(a, u, ring, part);
     }
 }
 
-template <int FMT, bool GATED>
-hipError_t launch_stream(const ProductArgs &a, hipStream_t s) {
+template <int FMT, bool GATED, int CF, int ROWS> void launch_split(const ProductArgs &a, int64_t blocks, hipStream_t s) {
+    const int64_t units = blocks * ((a.N + 16 * CF - 1) / (16 * CF));
+    const bool alone = units >= (int64_t)a.num_cu * kStreamWaves;
+    const int64_t need = alone ? (units + kStreamWaves - 1) / kStreamWaves : units;
+    const dim3 grid((unsigned)((std::min<int64_t>(need, a.num_cu) + 7) / 8 * 8));
+    if (alone) hipLaunchKernelGGL((product_stream_kernel<FMT, GATED, CF, ROWS, 1>), grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((product_stream_kernel<FMT, GATED, CF, ROWS, kStreamWaves>), grid, dim3(kThreads), 0, s, a);
+}
+template <int FMT, bool GATED> hipError_t launch_stream(const ProductArgs &a, hipStream_t s) {
+    // most row blocks that there can be
     const int64_t blocks = a.M / kUnitRows + std::min<int64_t>(a.M, a.G);
-    const int64_t grid = std::min<int64_t>(blocks * ((a.N + 15) / 16), (int64_t)a.num_cu * 4);
-    hipLaunchKernelGGL((product_stream_kernel<FMT, GATED, 1, 4>), dim3((unsigned)grid), dim3(256), 0, s, a);
+    constexpr int WIDE = GATED ? 1 : 2;
+    if (a.M <= 16) launch_split<FMT, GATED, WIDE, 1>(a, blocks, s);
+    else launch_split<FMT, GATED, WIDE, 4>(a, blocks, s);
     return hipGetLastError();
 }
 

@@ -27,7 +27,8 @@ constexpr int kTileColumns = 256;                  // weight rows of a tile (gat
 constexpr int kSlab = 128;                         // bytes of the contraction
 constexpr int kTileLds = 2 * 512 * kSlab;
 template <int FW, int FX> constexpr int tile_stages() { return 3 * (FW + FX) * 32 * kSlab <= kTileLds + (16 << 10) ? 3 : 2; }
-constexpr int kRemCF = 2;                          // columns / 16 of a remainder's unit
+template <bool GATED> constexpr int unit_columns() { return GATED ? 16 : 32; }        // of a remainder's unit
+static_assert(kStreamWaves * 64 == kThreads && kStreamWaves * kRingBytes <= kTileLds + (16 << 10), "units in a tile's LDS");
 
 template <int FMT> static __device__ __forceinline__ void multiply_in_place(raw_t w, raw_t x, typename Numbers<FMT>::acc_t &c) {
     if constexpr (FMT == CRAFT_I8) {
@@ -358,9 +359,9 @@ __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a
     __shared__ float row_scale[256];
     __shared__ uint8_t row_live[256];
     typedef typename Numbers<FMT>::acc_t acc_t;
-    constexpr int COLS = GATED ? kTileColumns / 2 : kTileColumns;
+    constexpr int COLS = GATED ? kTileColumns / 2 : kTileColumns, REM = unit_columns<GATED>() / 16;
     count_tiles(a, height, n, reinterpret_cast<int32_t *>(smem));
-    const int32_t nt = (a.N + COLS - 1) / COLS, nu = (a.N + 16 * kRemCF - 1) / (16 * kRemCF);
+    const int32_t nt = (a.N + COLS - 1) / COLS, nu = (a.N + 16 * REM - 1) / (16 * REM);
     const int64_t full = (int64_t)n.full[a.G] * nt, low = full + (int64_t)n.low[a.G] * nt, all = low + (int64_t)n.few[a.G] * nu;
     int64_t w = blockIdx.x;
     {
@@ -400,19 +401,20 @@ __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a
         int64_t lo, hi;
         u.group = group_of(n.few, a.G, (int32_t)(i / nu));
         group_rows(a, u.group, lo, hi);
-        u.n0 = __builtin_amdgcn_readfirstlane((int32_t)(i % nu) * 16 * kRemCF);
+        u.n0 = __builtin_amdgcn_readfirstlane((int32_t)(i % nu) * 16 * REM);
         u.rows = __builtin_amdgcn_readfirstlane((int32_t)((hi - lo) % height));
         u.row0 = hi - u.rows;
         acc_t *part = reinterpret_cast<acc_t *>(smem);
-        if (u.rows <= 16) stream_unit<FMT, GATED, kRemCF, 1, 4>(a, u, part);
-        else if (u.rows <= 32) stream_unit<FMT, GATED, kRemCF, 2, 4>(a, u, part);
-        else stream_unit<FMT, GATED, kRemCF, 4, 4>(a, u, part);
+        unsigned char *const ring = smem + ((int)threadIdx.x >> 6) * kRingBytes;
+        if (u.rows <= 16) stream_unit<FMT, GATED, REM, 1, kStreamWaves>(a, u, ring, part);
+        else if (u.rows <= 32) stream_unit<FMT, GATED, REM, 2, kStreamWaves>(a, u, ring, part);
+        else stream_unit<FMT, GATED, REM, 4, kStreamWaves>(a, u, ring, part);
     }
 }
 
 template <int FMT> hipError_t launch_tiles(const ProductArgs &a, int32_t height, hipStream_t s) {
     const int cols = a.up ? kTileColumns / 2 : kTileColumns;
-    const int64_t nt = (a.N + cols - 1) / cols, nu = (a.N + 16 * kRemCF - 1) / (16 * kRemCF);
+    const int64_t nt = (a.N + cols - 1) / cols, nu = (a.N + 15) / 16;
     const int64_t bound = (a.M / height) * nt + std::min<int64_t>(a.M, a.G) * nu;
     const int64_t grid = std::max<int64_t>(8, (std::min<int64_t>(bound, a.num_cu) + 7) / 8 * 8);
     if (a.up) hipLaunchKernelGGL((product_tile_kernel<FMT, true>), dim3((unsigned)grid), dim3(kThreads), 0, s, a, height);
