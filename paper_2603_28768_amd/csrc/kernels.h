@@ -366,9 +366,10 @@ struct ProductArgs {
 };
 constexpr int32_t kMostGroups = 1024;
 hipError_t launch_product(const ProductArgs &a, hipStream_t s);
-// Many rows a group: tiles of up to `height` rows.  Rows of 128 bytes or more, and of x within 32-bit offsets.
-hipError_t launch_product_tiles_i8(const ProductArgs &a, int32_t height, hipStream_t s);
-hipError_t launch_product_tiles_bf16(const ProductArgs &a, int32_t height, hipStream_t s);
-hipError_t launch_product_tiles_f32(const ProductArgs &a, int32_t height, hipStream_t s);
+// Many rows a group: tiles of `width` rows of the weights (256 or 128: height up to 128) and up to `height` of x.  Rows of 128 bytes
+// or more, and of x within 32-bit offsets.
+hipError_t launch_product_tiles_i8(const ProductArgs &a, int32_t width, int32_t height, hipStream_t s);
+hipError_t launch_product_tiles_bf16(const ProductArgs &a, int32_t width, int32_t height, hipStream_t s);
+hipError_t launch_product_tiles_f32(const ProductArgs &a, int32_t width, int32_t height, hipStream_t s);
 
 }  // namespace craft

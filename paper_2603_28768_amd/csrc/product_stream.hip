@@ -1,5 +1,6 @@
 // Products with few rows a group, as units of product_stream.h, and which kernel takes a product.
 #include <algorithm>
+#include <cmath>
 
 #include "product_stream.h"
 
@@ -92,16 +93,37 @@ template <bool GATED> hipError_t launch_format(const ProductArgs &a, hipStream_t
 
 }  // namespace
 
+// Size of the tiles: the one whose rounds take the least.  A slab of a tile of FW x FX fragments a wave takes its matrix
+// instructions (2 FW FX of 16 cycles) or its way through LDS (12 (FW + FX) KiB at 128 bytes a cycle), whichever is longer, a tile
+// about 12000 cycles beside its slabs.  How rows are spread over groups only the GPU knows: half a tile more for each is assumed.
+void product_tile_size(const ProductArgs &a, int32_t *width, int32_t *height) {
+    const int64_t slabs = (a.row_bytes + 127) / 128, per_element = a.format == CRAFT_F32 ? 4 : 1;
+    double best = 0;
+    for (int fw = 8; fw >= 4; fw -= 4)
+        for (int fx = fw; fx >= 2; --fx) {
+            if (fx == 3) continue;
+            const int64_t columns = 32 * fw / (a.up ? 2 : 1), nt = (a.N + columns - 1) / columns;
+            const double rows = a.G == 1 ? (double)((a.M + 32 * fx - 1) / (32 * fx)) : (double)a.M / (32 * fx) + 0.5 * a.G;
+            const double rounds = rows * nt / a.num_cu;
+            const double slab = std::max(32.0 * fw * fx * per_element, 96.0 * (fw + fx));
+            const double time = (rounds < 1 ? 1 : rounds < 4 && a.G == 1 ? std::ceil(rounds) : rounds + 0.3) * (slabs * slab + 12000);
+            if (best == 0 || time < best) {
+                best = time;
+                *width = 32 * fw;
+                *height = 32 * fx;
+            }
+        }
+}
+
 hipError_t launch_product(const ProductArgs &a, hipStream_t s) {
     if (a.M <= 0) return hipSuccess;
     const bool near = a.src ? a.x_rows * a.x_stride < (int64_t)1 << 32 : a.x_stride < (int64_t)1 << 24;
     if (near && a.row_bytes >= 128 && a.M >= 128 && a.M / a.G >= 16) {
-        const int64_t nt = (a.N + (a.up ? 127 : 255)) / (a.up ? 128 : 256);
-        int32_t height = 256;
-        while (height > 64 && a.M / height * nt < a.num_cu) height -= 64;
-        if (a.format == CRAFT_I8) return launch_product_tiles_i8(a, height, s);
-        if (a.format == CRAFT_BF16) return launch_product_tiles_bf16(a, height, s);
-        return launch_product_tiles_f32(a, height, s);
+        int32_t width = 256, height = 256;
+        product_tile_size(a, &width, &height);
+        if (a.format == CRAFT_I8) return launch_product_tiles_i8(a, width, height, s);
+        if (a.format == CRAFT_BF16) return launch_product_tiles_bf16(a, width, height, s);
+        return launch_product_tiles_f32(a, width, height, s);
     }
     return a.up ? launch_format<true>(a, s) : launch_format<false>(a, s);
 }

@@ -9,8 +9,8 @@
 // is free again, and the slab that takes its place is requested at once.  Every memory instruction is dealt out behind a matrix
 // instruction of its own.
 //
-// Groups are cut into full tiles of `height` rows and one remainder: of more than 64 rows a lower tile, of fewer units
-// of product_stream.h.  The list has all full tiles first, then remainders.
+// A group's rows are shared evenly among as few tiles of at most `height` rows as hold them, in whole fragments of 32; groups of up
+// to 64 rows are units of product_stream.h.  The list has the tallest tiles first, units last.
 #pragma once
 
 #include <algorithm>
@@ -23,7 +23,6 @@ namespace craft {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTileColumns = 256;                  // weight rows of a tile (gated: half of them gate, half up)
 constexpr int kSlab = 128;                         // bytes of the contraction
 constexpr int kTileLds = 2 * 512 * kSlab;
 template <int FW, int FX> constexpr int tile_stages() { return 3 * (FW + FX) * 32 * kSlab <= kTileLds + (16 << 10) ? 3 : 2; }
@@ -69,11 +68,9 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
         const int64_t tok = gather ? token_of(a, t.row0 + r) : r;
         xoff[i] = (uint32_t)((tok < 0 ? 0 : tok) * a.x_stride) + piece;
     }
-    if ((int)threadIdx.x < t.rows) {
-        const int64_t tok = token_of(a, t.row0 + threadIdx.x);
-        row_live[threadIdx.x] = tok >= 0;
-        if (FMT == CRAFT_I8) row_scale[threadIdx.x] = a.x_scale[tok < 0 ? 0 : tok];
-    }
+    // what a thread's row of the tile is multiplied by; goes to LDS when there is time for it
+    const int64_t my_row = token_of(a, t.row0 + min((int)threadIdx.x, t.rows - 1));
+    const float my_scale = FMT == CRAFT_I8 ? a.x_scale[my_row < 0 ? 0 : my_row] : 1.0f;
     // Gated: 16 rows of gate are followed by the 16 of up of the same columns; the first two waves fetch gate's.
     const unsigned char *mat = a.off ? a.w[t.group] : a.w_one;
     if (GATED && wave >= 2) mat = a.up[t.group];
@@ -272,69 +269,61 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    row_live[threadIdx.x] = my_row >= 0;
+    if (FMT == CRAFT_I8) row_scale[threadIdx.x] = my_scale;
     __syncthreads();                               // every wave has read the last slab
     if (FMT != CRAFT_F32 && a.out_dtype == CRAFT_BF16) results(with);
     else results(without);
     __syncthreads();                               // LDS may be filled again
 }
 
-// How many full tiles, remaining tiles and remaining units the groups in front of one have: [G + 1] each, in LDS.
-struct Counts {
-    int32_t full[kMostGroups + 1], low[kMostGroups + 1], few[kMostGroups + 1];
+// How a group's rows are cut: kFew into units, else into tiles of `height` rows (the last one what is left), the classes by height.
+constexpr int kClasses = 4, kFew = 3;
+struct Cut {
+    int32_t kind, height, count;
 };
-static __device__ __forceinline__ void count_tiles(const ProductArgs &a, int32_t height, Counts &n, int32_t *scratch) {
-    if (!a.off) {                                  // one group
-        if (threadIdx.x == 0) {
-            const int32_t rest = (int32_t)(a.M % height);
-            n.full[0] = n.low[0] = n.few[0] = 0;
-            n.full[1] = (int32_t)(a.M / height);
-            n.low[1] = rest > kUnitRows;
-            n.few[1] = rest > 0 && rest <= kUnitRows;
+static __device__ __forceinline__ Cut cut_rows(int32_t rows, int32_t most) {
+    if (rows <= kUnitRows) return {kFew, kUnitRows, rows > 0};
+    const int32_t tiles = (rows + most - 1) / most, height = ((rows + tiles - 1) / tiles + 31) / 32 * 32;
+    return {height > 192 ? 0 : height > 128 ? 1 : 2, height, (rows + height - 1) / height};
+}
+// Row tiles (units: row blocks) of each class that the groups up to one have: [G + 1], in LDS.  Every wave works them out for itself
+// and stores the same, so that no barrier is needed: a wave reads what it has written.
+struct Counts {
+    int32_t of[kFew][kMostGroups + 1];
+    uint16_t few[kMostGroups + 1];                 // one a group at most
+};
+static __device__ __forceinline__ void count_tiles(const ProductArgs &a, int32_t height, Counts &n) {
+    const int lane = threadIdx.x & 63;
+    int32_t sum[kClasses] = {};
+    for (int32_t g0 = 0; g0 < a.G; g0 += 64) {
+        const int32_t g = g0 + lane;
+        int64_t lo = 0, hi = 0;
+        if (g < a.G) group_rows(a, g, lo, hi);
+        const Cut cut = cut_rows((int32_t)(hi - lo), height);
+#pragma unroll
+        for (int i = 0; i < kClasses; ++i) {
+            int32_t c = cut.kind == i ? cut.count : 0;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int32_t up = __shfl_up(c, d, 64);
+                c += lane >= d ? up : 0;
+            }
+            c += sum[i];
+            sum[i] = __shfl(c, 63, 64);
+            if (g < a.G) {
+                if (i == kFew) n.few[g + 1] = (uint16_t)c;
+                else n.of[i < kFew ? i : 0][g + 1] = c;
+            }
         }
-        __syncthreads();
-        return;
-    }
-    const int32_t each = (a.G + kThreads - 1) / kThreads, first = min((int32_t)threadIdx.x * each, a.G), last = min(first + each, a.G);
-    int32_t sum[3] = {0, 0, 0};
-    for (int32_t g = first; g < last; ++g) {
-        int64_t lo, hi;
-        group_rows(a, g, lo, hi);
-        const int32_t rows = (int32_t)(hi - lo), rest = rows % height;
-        n.full[g] = rows / height;
-        n.low[g] = rest > kUnitRows;
-        n.few[g] = rest > 0 && rest <= kUnitRows;
-        sum[0] += n.full[g];
-        sum[1] += n.low[g];
-        sum[2] += n.few[g];
     }
 #pragma unroll
-    for (int i = 0; i < 3; ++i) scratch[i * kThreads + threadIdx.x] = sum[i];
-    __syncthreads();
-    for (int d = 1; d < kThreads; d *= 2) {
-        int32_t add[3] = {0, 0, 0};
-        if ((int)threadIdx.x >= d)
-#pragma unroll
-            for (int i = 0; i < 3; ++i) add[i] = scratch[i * kThreads + threadIdx.x - d];
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 3; ++i) scratch[i * kThreads + threadIdx.x] += add[i];
-        __syncthreads();
-    }
-    int32_t *const out[3] = {n.full, n.low, n.few};
-#pragma unroll
-    for (int i = 0; i < 3; ++i) {
-        int32_t at = scratch[i * kThreads + threadIdx.x] - sum[i];
-        for (int32_t g = first; g < last; ++g) {
-            const int32_t c = out[i][g];
-            out[i][g] = at;
-            at += c;
-        }
-        if (threadIdx.x == kThreads - 1) out[i][a.G] = scratch[i * kThreads + kThreads - 1];
-    }
-    __syncthreads();
+    for (int i = 0; i < kFew; ++i) n.of[i][0] = 0;
+    n.few[0] = 0;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 // before[g] <= i < before[g + 1]
-static __device__ __forceinline__ int32_t group_of(const int32_t *before, int32_t G, int32_t i) {
+template <typename T> static __device__ __forceinline__ int32_t group_of(const T *before, int32_t G, int32_t i) {
     int32_t lo = 0, hi = G;
     while (hi - lo > 1) {
         const int32_t mid = (lo + hi) >> 1;
@@ -352,74 +341,80 @@ static __device__ __forceinline__ void place(int32_t i, int32_t m, int32_t nt, i
     col = block * 8 + rest / rj;
 }
 
-template <int FMT, bool GATED>
+template <int FMT, bool GATED, int FW>
 __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a, int32_t height) {
     __shared__ __attribute__((aligned(16))) unsigned char smem[kTileLds + (16 << 10)];
     __shared__ Counts n;
-    __shared__ float row_scale[256];
-    __shared__ uint8_t row_live[256];
+    __shared__ float row_scale[kThreads];
+    __shared__ uint8_t row_live[kThreads];
     typedef typename Numbers<FMT>::acc_t acc_t;
-    constexpr int COLS = GATED ? kTileColumns / 2 : kTileColumns, REM = unit_columns<GATED>() / 16;
-    count_tiles(a, height, n, reinterpret_cast<int32_t *>(smem));
+    constexpr int COLS = GATED ? 16 * FW : 32 * FW, REM = unit_columns<GATED>() / 16;
+    count_tiles(a, height, n);
     const int32_t nt = (a.N + COLS - 1) / COLS, nu = (a.N + 16 * REM - 1) / (16 * REM);
-    const int64_t full = (int64_t)n.full[a.G] * nt, low = full + (int64_t)n.low[a.G] * nt, all = low + (int64_t)n.few[a.G] * nu;
-    int64_t w = blockIdx.x;
-    {
-        // neighbours in the list start together on one XCD
-        const int64_t run = gridDim.x / 8;
-        w = (w % 8) * run + w / 8;
-    }
-    for (; w < low; w += gridDim.x) {
+    int64_t ends[kClasses];                        // of the classes in the list
+#pragma unroll
+    for (int i = 0; i < kClasses; ++i) ends[i] = (i ? ends[i - 1] : 0) + (i == kFew ? (int64_t)n.few[a.G] * nu : (int64_t)n.of[i < kFew ? i : 0][a.G] * nt);
+    const int64_t tiles = ends[kFew - 1], units = ends[kFew] - tiles;
+    // Neighbours in the list start together on one XCD, 32 of them, which are dealt to the XCDs in turn.  One tile a workgroup:
+    // the next one starts wherever a CU is done first.  What workgroups are left take the units in turn.
+    const int64_t at = (int64_t)(blockIdx.x / 256) * 256 + (blockIdx.x % 8) * 32 + blockIdx.x % 256 / 8;
+    for (int64_t w = at; w < tiles; w += gridDim.x) {
         Tile t;
         int64_t lo, hi;
         int32_t tr, tc;
-        const bool is_full = w < full;
-        const int32_t *before = is_full ? n.full : n.low;
-        const int64_t i = is_full ? w : w - full;
+        const int kind = w < ends[0] ? 0 : w < ends[1] ? 1 : 2;
+        const int64_t i = w - (kind == 0 ? 0 : kind == 1 ? ends[0] : ends[1]);
+        const int32_t *before = n.of[kind];
         t.group = group_of(before, a.G, (int32_t)(i / nt));
         group_rows(a, t.group, lo, hi);
-        if (is_full) {
-            place((int32_t)(i - (int64_t)before[t.group] * nt), before[t.group + 1] - before[t.group], nt, tr, tc);
-            t.rows = height;
+        const Cut cut = cut_rows((int32_t)(hi - lo), height);
+        place((int32_t)(i - (int64_t)before[t.group] * nt), cut.count, nt, tr, tc);
+        t.row0 = lo + (int64_t)tr * cut.height;
+        t.rows = __builtin_amdgcn_readfirstlane((int32_t)min((int64_t)cut.height, hi - t.row0));
+        t.n0 = __builtin_amdgcn_readfirstlane(tc * COLS);
+        if constexpr (FW == 8) {
+            if (t.rows > 224) product_tile<FMT, GATED, FW, 8>(a, t, smem, row_scale, row_live);
+            else if (t.rows > 192) product_tile<FMT, GATED, FW, 7>(a, t, smem, row_scale, row_live);
+            else if (t.rows > 160) product_tile<FMT, GATED, FW, 6>(a, t, smem, row_scale, row_live);
+            else if (t.rows > 128) product_tile<FMT, GATED, FW, 5>(a, t, smem, row_scale, row_live);
+            else if (t.rows > 64) product_tile<FMT, GATED, FW, 4>(a, t, smem, row_scale, row_live);
+            else product_tile<FMT, GATED, FW, 2>(a, t, smem, row_scale, row_live);
         } else {
-            tr = (int32_t)((hi - lo) / height);
-            tc = (int32_t)(i % nt);
-            t.rows = (int32_t)(hi - lo) - tr * height;
+            if (t.rows > 64) product_tile<FMT, GATED, FW, 4>(a, t, smem, row_scale, row_live);
+            else product_tile<FMT, GATED, FW, 2>(a, t, smem, row_scale, row_live);
         }
-        t.row0 = lo + (int64_t)tr * height;
-        t.n0 = tc * COLS;
-        t.rows = __builtin_amdgcn_readfirstlane(t.rows);
-        t.n0 = __builtin_amdgcn_readfirstlane(t.n0);
-        if (t.rows <= 64) product_tile<FMT, GATED, 8, 2>(a, t, smem, row_scale, row_live);
-        else if (t.rows <= 128) product_tile<FMT, GATED, 8, 4>(a, t, smem, row_scale, row_live);
-        else if (t.rows <= 192) product_tile<FMT, GATED, 8, 6>(a, t, smem, row_scale, row_live);
-        else product_tile<FMT, GATED, 8, 8>(a, t, smem, row_scale, row_live);
     }
-    for (; w < all; w += gridDim.x) {
-        const int64_t i = w - low;
+    const bool spare = tiles < (int64_t)gridDim.x; // (else every workgroup has had tiles)
+    if (spare && at < tiles) return;
+    for (int64_t i = spare ? at - tiles : at; i < units; i += spare ? gridDim.x - tiles : gridDim.x) {
         Unit u;
         int64_t lo, hi;
         u.group = group_of(n.few, a.G, (int32_t)(i / nu));
         group_rows(a, u.group, lo, hi);
         u.n0 = __builtin_amdgcn_readfirstlane((int32_t)(i % nu) * 16 * REM);
-        u.rows = __builtin_amdgcn_readfirstlane((int32_t)((hi - lo) % height));
-        u.row0 = hi - u.rows;
-        acc_t *part = reinterpret_cast<acc_t *>(smem);
+        u.rows = __builtin_amdgcn_readfirstlane((int32_t)(hi - lo));
+        u.row0 = lo;
         unsigned char *const ring = smem + ((int)threadIdx.x >> 6) * kRingBytes;
+        acc_t *const part = reinterpret_cast<acc_t *>(smem);
         if (u.rows <= 16) stream_unit<FMT, GATED, REM, 1, kStreamWaves>(a, u, ring, part);
         else if (u.rows <= 32) stream_unit<FMT, GATED, REM, 2, kStreamWaves>(a, u, ring, part);
         else stream_unit<FMT, GATED, REM, 4, kStreamWaves>(a, u, ring, part);
     }
 }
 
-template <int FMT> hipError_t launch_tiles(const ProductArgs &a, int32_t height, hipStream_t s) {
-    const int cols = a.up ? kTileColumns / 2 : kTileColumns;
-    const int64_t nt = (a.N + cols - 1) / cols, nu = (a.N + 15) / 16;
-    const int64_t bound = (a.M / height) * nt + std::min<int64_t>(a.M, a.G) * nu;
-    const int64_t grid = std::max<int64_t>(8, (std::min<int64_t>(bound, a.num_cu) + 7) / 8 * 8);
-    if (a.up) hipLaunchKernelGGL((product_tile_kernel<FMT, true>), dim3((unsigned)grid), dim3(kThreads), 0, s, a, height);
-    else hipLaunchKernelGGL((product_tile_kernel<FMT, false>), dim3((unsigned)grid), dim3(kThreads), 0, s, a, height);
+template <int FMT, bool GATED, int FW> hipError_t launch_width(const ProductArgs &a, int32_t height, hipStream_t s) {
+    constexpr int COLS = GATED ? 16 * FW : 32 * FW;
+    const int64_t nt = (a.N + COLS - 1) / COLS, nu = (a.N + 15) / 16;
+    // most tiles that there can be (a group's count rounds up twice: to whole tiles, and its rows to whole fragments, which leaves
+    // out tiles, never adds one), and workgroups for the units besides
+    const int64_t tiles = (a.M / height + std::min<int64_t>(a.M / (kUnitRows + 1), a.G)) * nt;
+    const int64_t grid = (tiles + std::min<int64_t>(std::min<int64_t>(a.M, a.G) * nu, a.num_cu) + 255) / 256 * 256;
+    hipLaunchKernelGGL((product_tile_kernel<FMT, GATED, FW>), dim3((unsigned)std::min<int64_t>(grid, 1 << 22)), dim3(kThreads), 0, s, a, height);
     return hipGetLastError();
+}
+template <int FMT> hipError_t launch_tiles(const ProductArgs &a, int32_t width, int32_t height, hipStream_t s) {
+    if (width == 256) return a.up ? launch_width<FMT, true, 8>(a, height, s) : launch_width<FMT, false, 8>(a, height, s);
+    return a.up ? launch_width<FMT, true, 4>(a, height, s) : launch_width<FMT, false, 4>(a, height, s);
 }
 
 }  // namespace
