@@ -9,25 +9,31 @@
 // is free again, and the slab that takes its place is requested at once.  Every memory instruction is dealt out behind a matrix
 // instruction of its own.
 //
-// A group's rows are shared evenly among as few tiles of at most `height` rows as hold them, in whole fragments of 32; groups of up
-// to 64 rows are units of product_stream.h.  The list has the tallest tiles first, units last.
+// A group's rows are shared evenly among as few tiles of at most `height` rows as hold them, in whole fragments of 32.  Groups of up
+// to 64 rows, which stream their weights through one CU at what that gets out of HBM, have tiles of 128 weight rows with up to six stages.
+// The list has the tallest tiles first.
 #pragma once
 
 #include <algorithm>
 #include <type_traits>
 
 #include "ffn_common.h"
-#include "product_stream.h"
+#include "product.h"
 
 namespace craft {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kSlab = 128;                         // bytes of the contraction
-constexpr int kTileLds = 2 * 512 * kSlab;
-template <int FW, int FX> constexpr int tile_stages() { return 3 * (FW + FX) * 32 * kSlab <= kTileLds + (16 << 10) ? 3 : 2; }
-template <bool GATED> constexpr int unit_columns() { return GATED ? 16 : 32; }        // of a remainder's unit
-static_assert(kStreamWaves * 64 == kThreads && kStreamWaves * kRingBytes <= kTileLds + (16 << 10), "units in a tile's LDS");
+constexpr int kTileLds = 160 << 10;                // all there is
+// Stages of the weights and of x: weights come from HBM the first time, x mostly from L2, so weights get one more where that
+// is what there is room for.
+template <int FW, int FX> constexpr int both_stages() { return kTileLds / ((FW + FX) * 32 * kSlab); }
+template <int FW, int FX> constexpr int x_stages() { return both_stages<FW, FX>() < 6 ? both_stages<FW, FX>() : 6; }
+template <int FW, int FX> constexpr int w_stages() {
+    return x_stages<FW, FX>() < 6 && (x_stages<FW, FX>() * (FW + FX) + FW) * 32 * kSlab <= kTileLds ? x_stages<FW, FX>() + 1 : x_stages<FW, FX>();
+}
+constexpr int kLowColumns = 4;                     // fragments of weights a wave for groups of few rows
 
 template <int FMT> static __device__ __forceinline__ void multiply_in_place(raw_t w, raw_t x, typename Numbers<FMT>::acc_t &c) {
     if constexpr (FMT == CRAFT_I8) {
@@ -50,10 +56,11 @@ struct Tile {
 
 // FW, FX: 16-row fragments of weights and of x per wave; the tile is 32 FW columns (gated: 16 FW) x 32 FX rows.
 template <int FMT, bool GATED, int FW, int FX>
-static __device__ __forceinline__ void product_tile(const ProductArgs &a, const Tile &t, unsigned char *smem, float *row_scale, uint8_t *row_live) {
+static __device__ __forceinline__ void product_tile(const ProductArgs &a, const Tile &t, unsigned char *smem) {
     typedef typename Numbers<FMT>::acc_t acc_t;
-    constexpr int M = FW * FX, NR = FW + FX, STAGE = NR * 32 * kSlab, S = tile_stages<FW, FX>();
-    static_assert(S * STAGE <= kTileLds + (16 << 10), "stages");
+    constexpr int M = FW * FX, NR = FW + FX, SW = w_stages<FW, FX>(), SX = x_stages<FW, FX>();
+    constexpr uint32_t WSTAGE = FW * 32 * kSlab, XSTAGE = FX * 32 * kSlab, XRING = SW * WSTAGE;
+    static_assert(SX >= 2 && (SW == SX || (SX == 2 && SW == 3)) && XRING + SX * XSTAGE <= kTileLds && SX * NR <= 63, "stages");
     const int lane = threadIdx.x & 63, q = lane >> 4, r16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int32_t KB = a.row_bytes, nk = (KB + kSlab - 1) / kSlab;
@@ -82,7 +89,7 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
     const uint32_t lds_wave = lds0 + (uint32_t)__builtin_amdgcn_readfirstlane(wave * 1024);
     const uint32_t fo = lds0 + (uint32_t)(r16 * 128 + ((q ^ (lane & 7)) & 7) * 16);
-    const uint32_t fw0 = fo + (uint32_t)((wave >> 1) * FW * 2048), fx0 = fo + (uint32_t)((2 * FW + (wave & 1) * FX) * 2048);
+    const uint32_t fw0 = fo + (uint32_t)((wave >> 1) * FW * 2048), fx0 = fo + XRING + (uint32_t)((wave & 1) * FX * 2048);
     typedef const raw_t __attribute__((address_space(3))) *frag_t;
 
     raw_t wv[2][FW], xv[2][FX];
@@ -94,15 +101,18 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
 
     // where slab ks begins in a row: the last one ends with it, and what the one before has is cut away
     auto at = [&](int ks) __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_readfirstlane(min(ks * kSlab, KB - kSlab)); };
-    auto aim = [&](int i, uint32_t stage) __attribute__((always_inline)) { dma_to(lds_wave + stage + (uint32_t)(4096 * i)); };
-    auto request = [&](int i, uint32_t k) __attribute__((always_inline)) {
-        if (i < FW) dma_request(wbase + k, woff[i < FW ? i : 0]);
-        else dma_request(xbase + k, xoff[i < FW ? 0 : i - FW]);
+    // Request j of a slab: x's chunks, then the weights' (their order is what the waits count on); w, x: stages
+    auto aim = [&](int j, uint32_t w, uint32_t x) __attribute__((always_inline)) {
+        dma_to(lds_wave + (j < FX ? XRING + x + (uint32_t)(4096 * j) : w + (uint32_t)(4096 * (j - FX))));
+    };
+    auto request = [&](int j, uint32_t kw, uint32_t kx) __attribute__((always_inline)) {
+        if (j < FX) dma_request(xbase + kx, xoff[j < FX ? j : 0]);
+        else dma_request(wbase + kw, woff[j < FX ? 0 : j - FX]);
     };
     // x's fragments first, the next products start with those
     struct From { uint32_t x, w; };                // one register each, fragments at constant offsets from them
-    auto from = [&](int step, uint32_t stage) __attribute__((always_inline)) {
-        From p = {(fx0 ^ (step ? 64u : 0u)) + stage, (fw0 ^ (step ? 64u : 0u)) + stage};
+    auto from = [&](int step, uint32_t w, uint32_t x) __attribute__((always_inline)) {
+        From p = {(fx0 ^ (step ? 64u : 0u)) + x, (fw0 ^ (step ? 64u : 0u)) + w};
         asm volatile("" : "+v"(p.x), "+v"(p.w));
         return p;
     };
@@ -125,24 +135,25 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
             asm volatile("s_nop 1" : "+v"(wv[set][f]));
         }
     };
-    // One step: set STEP multiplied, the other one read from `stage`; DMA: slab `k` requested into `to` as well.
-    auto step_of = [&](auto STEP, auto DMA, uint32_t stage, uint32_t to, uint32_t k) __attribute__((always_inline)) {
-        constexpr int set = STEP.value, OPS = DMA.value ? 3 * NR : NR;
-        const From p = from(set ^ 1, stage);
+    // One step: set STEP multiplied, the other one read from stages w and x; the first REQ requests of slabs at kw and kx into
+    // stages tw and tx as well.
+    auto step_of = [&](auto STEP, auto REQ, uint32_t w, uint32_t x, uint32_t tw, uint32_t tx, uint32_t kw, uint32_t kx) __attribute__((always_inline)) {
+        constexpr int set = STEP.value, R = REQ.value, OPS = NR + 2 * R;
+        const From p = from(set ^ 1, w, x);
 #pragma unroll
         for (int m = 0; m < M; ++m) {
             multiply_in_place<FMT>(wv[set][m / FX], xv[set][m % FX], acc[m / FX][m % FX]);
             // spread over three quarters of the step: what is read has to be there when the next one begins
 #pragma unroll
             for (int o = min(m * OPS * 4 / (3 * M), OPS); o < min((m + 1) * OPS * 4 / (3 * M), OPS); ++o) {
-                if (!DMA.value) {
-                    fetch(set ^ 1, o, p);
-                } else if (o % 3 == 0) {
-                    dma_to(lds_wave + to + (uint32_t)(4096 * (o / 3)));
-                } else if (o % 3 == 1) {
-                    fetch(set ^ 1, o / 3, p);
+                // a request's address, a fragment, the request: a load may not follow its M0 at once
+                const int i = o / 3;
+                if (i < R) {
+                    if (o % 3 == 0) aim(i, tw, tx);
+                    else if (o % 3 == 1) fetch(set ^ 1, i, p);
+                    else request(i, kw, kx);
                 } else {
-                    request(o / 3, k);
+                    fetch(set ^ 1, o - 2 * R, p);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -150,48 +161,68 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
     };
     const std::integral_constant<int, 0> step0;
     const std::integral_constant<int, 1> step1;
+    const std::integral_constant<int, 0> nothing;
+    const std::integral_constant<int, FX> rows_only;
+    const std::integral_constant<int, NR> all;
     const std::true_type with;
     const std::false_type without;
     const bool cuts = nk * kSlab != KB;
 
+    __syncthreads();                               // nobody reads what LDS held
 #pragma unroll
-    for (int j = 0; j < S; ++j)
+    for (int j = 0; j < SW; ++j)
         if (j < nk) {
             const uint32_t k = at(j);
 #pragma unroll
-            for (int i = 0; i < NR; ++i) {
-                aim(i, j * STAGE);
+            for (int i = j < SX ? 0 : FX; i < NR; ++i) {
+                aim(i, j * WSTAGE, j * XSTAGE);
                 asm volatile("s_nop 0");
-                request(i, k);
+                request(i, k, k);
             }
         }
-    if (nk >= S) dma_wait<(S - 1) * NR>();
+    if (nk >= SW) dma_wait<(SX - 1) * NR + (SW - SX) * FW>();
     else dma_wait<0>();
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < NR; ++j) fetch(0, j, from(0, 0));
-    uint32_t here = 0;
+    for (int j = 0; j < NR; ++j) fetch(0, j, from(0, 0, 0));
+    uint32_t hw = 0, hx = 0;                       // stages of slab ks
     int ks = 0;
-    // Behind the first step all of slab ks is in registers, for every wave at the barrier, and slab ks + 1 has landed: what is
-    // on its way by then are the slabs behind it.
-    for (; ks + S < nk; ++ks) {
-        const uint32_t there = here + STAGE < S * STAGE ? here + STAGE : 0;
-        step_of(step0, without, here, 0, 0);
-        dma_wait<(S - 2) * NR>();
+    auto next_w = [&](uint32_t v) { return v + WSTAGE < SW * WSTAGE ? v + WSTAGE : 0; };
+    auto next_x = [&](uint32_t v) { return v + XSTAGE < SX * XSTAGE ? v + XSTAGE : 0; };
+    // Behind the first step all of slab ks is in registers, for every wave at the barrier, and slab ks + 1 has landed: what
+    // was requested behind its x may be on its way, and behind its weights, which are a slab older where they have a stage more.
+    constexpr int BEHIND = (SX - 2) * NR + (SW > SX ? FW : 0);
+    for (; ks + SW < nk; ++ks) {
+        const uint32_t tw = next_w(hw), tx = next_x(hx);
+        step_of(step0, nothing, hw, hx, 0, 0, 0, 0);
+        dma_wait<BEHIND>();
         __syncthreads();
-        step_of(step1, with, there, here, at(ks + S));
-        here = there;
+        step_of(step1, all, tw, tx, hw, hx, at(ks + SW), at(ks + SX));
+        hw = tw;
+        hx = tx;
+    }
+    if (SW > SX && ks + SX < nk) {                 // the last rows of x that are still to be requested
+        const uint32_t tw = next_w(hw), tx = next_x(hx);
+        step_of(step0, nothing, hw, hx, 0, 0, 0, 0);
+        dma_wait<BEHIND>();
+        __syncthreads();
+        step_of(step1, rows_only, tw, tx, hw, hx, 0, at(ks + SX));
+        hw = tw;
+        hx = tx;
+        ++ks;
     }
     for (; ks < nk; ++ks) {
-        const uint32_t there = here + STAGE < S * STAGE ? here + STAGE : 0;
+        const uint32_t tw = next_w(hw), tx = next_x(hx);
         const bool last = ks + 1 == nk;
         if (last && cuts) cut(0);
-        step_of(step0, without, here, 0, 0);
-        dma_wait<0>();
+        step_of(step0, nothing, hw, hx, 0, 0, 0, 0);
+        if (SW == SX && ks + 2 < nk) dma_wait<NR>();      // one slab or more behind the next
+        else dma_wait<0>();
         __syncthreads();
         if (last && cuts) cut(1);
-        step_of(step1, without, there, 0, 0);      // (behind the last slab: read and not used)
-        here = there;
+        step_of(step1, nothing, tw, tx, 0, 0, 0, 0);      // (behind the last slab: read and not used)
+        hw = tw;
+        hx = tx;
     }
     // a matrix instruction's result is read: idle cycles, then every accumulator through a statement behind them
     asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
@@ -215,6 +246,8 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
                 else ws[f][e] = s0[c];
             }
     }
+    float *const row_scale = reinterpret_cast<float *>(smem + kTileLds - 4096);
+    uint8_t *const row_live = smem + kTileLds - 2048;
     // By way of LDS, 16 rows at a time and each wave for itself, so that a store covers whole lines (16 rows of 32 bytes a
     // request: 8 us a tile where this takes 3).  Stores are of 16 bytes whatever the alignment; a lane at the matrix' edge
     // stores its columns one by one.
@@ -224,7 +257,7 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
         typedef out_t piece_t __attribute__((ext_vector_type(16 / sizeof(out_t)), aligned(sizeof(out_t))));
         constexpr int COLS = 16 * FW / SIDES, ROWB = COLS * (int)sizeof(out_t), PITCH = ROWB + 16;     // a row of this wave
         constexpr int PER = ROWB / 16, EACH = 16 / (int)sizeof(out_t), PASSES = 16 * PER / 64;      // pieces of a row; elements of a piece
-        static_assert(4 * 16 * PITCH <= kTileLds, "rows of results");
+        static_assert(4 * 16 * PITCH <= kTileLds - 4096, "rows of results");
         unsigned char *const mine = smem + wave * (16 * PITCH);
         const int32_t first = t.n0 + (wave >> 1) * COLS;
         out_t *const out = static_cast<out_t *>(a.out) + first;
@@ -269,29 +302,28 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    __syncthreads();                               // every wave has read the last slab
     row_live[threadIdx.x] = my_row >= 0;
     if (FMT == CRAFT_I8) row_scale[threadIdx.x] = my_scale;
-    __syncthreads();                               // every wave has read the last slab
+    __syncthreads();
     if (FMT != CRAFT_F32 && a.out_dtype == CRAFT_BF16) results(with);
     else results(without);
-    __syncthreads();                               // LDS may be filled again
 }
 
-// How a group's rows are cut: kFew into units, else into tiles of `height` rows (the last one what is left), the classes by height.
-constexpr int kClasses = 4, kFew = 3;
+// How a group's rows are cut: kFew into one low tile, else into tiles of `height` rows (the last one what is left), the classes by height.
+constexpr int kClasses = 4, kFew = 3, kFewRows = 64;
 struct Cut {
     int32_t kind, height, count;
 };
 static __device__ __forceinline__ Cut cut_rows(int32_t rows, int32_t most) {
-    if (rows <= kUnitRows) return {kFew, kUnitRows, rows > 0};
+    if (rows <= kFewRows) return {kFew, kFewRows, rows > 0};
     const int32_t tiles = (rows + most - 1) / most, height = ((rows + tiles - 1) / tiles + 31) / 32 * 32;
     return {height > 192 ? 0 : height > 128 ? 1 : 2, height, (rows + height - 1) / height};
 }
-// Row tiles (units: row blocks) of each class that the groups up to one have: [G + 1], in LDS.  Every wave works them out for itself
+// Row tiles of each class that the groups up to one have: [G + 1], in LDS.  Every wave works them out for itself
 // and stores the same, so that no barrier is needed: a wave reads what it has written.
 struct Counts {
-    int32_t of[kFew][kMostGroups + 1];
-    uint16_t few[kMostGroups + 1];                 // one a group at most
+    int32_t of[kClasses][kMostGroups + 1];
 };
 static __device__ __forceinline__ void count_tiles(const ProductArgs &a, int32_t height, Counts &n) {
     const int lane = threadIdx.x & 63;
@@ -311,19 +343,15 @@ static __device__ __forceinline__ void count_tiles(const ProductArgs &a, int32_t
             }
             c += sum[i];
             sum[i] = __shfl(c, 63, 64);
-            if (g < a.G) {
-                if (i == kFew) n.few[g + 1] = (uint16_t)c;
-                else n.of[i < kFew ? i : 0][g + 1] = c;
-            }
+            if (g < a.G) n.of[i][g + 1] = c;
         }
     }
 #pragma unroll
-    for (int i = 0; i < kFew; ++i) n.of[i][0] = 0;
-    n.few[0] = 0;
+    for (int i = 0; i < kClasses; ++i) n.of[i][0] = 0;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 // before[g] <= i < before[g + 1]
-template <typename T> static __device__ __forceinline__ int32_t group_of(const T *before, int32_t G, int32_t i) {
+static __device__ __forceinline__ int32_t group_of(const int32_t *before, int32_t G, int32_t i) {
     int32_t lo = 0, hi = G;
     while (hi - lo > 1) {
         const int32_t mid = (lo + hi) >> 1;
@@ -343,72 +371,61 @@ static __device__ __forceinline__ void place(int32_t i, int32_t m, int32_t nt, i
 
 template <int FMT, bool GATED, int FW>
 __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a, int32_t height) {
-    __shared__ __attribute__((aligned(16))) unsigned char smem[kTileLds + (16 << 10)];
-    __shared__ Counts n;
-    __shared__ float row_scale[kThreads];
-    __shared__ uint8_t row_live[kThreads];
-    typedef typename Numbers<FMT>::acc_t acc_t;
-    constexpr int COLS = GATED ? 16 * FW : 32 * FW, REM = unit_columns<GATED>() / 16;
-    count_tiles(a, height, n);
-    const int32_t nt = (a.N + COLS - 1) / COLS, nu = (a.N + 16 * REM - 1) / (16 * REM);
-    int64_t ends[kClasses];                        // of the classes in the list
-#pragma unroll
-    for (int i = 0; i < kClasses; ++i) ends[i] = (i ? ends[i - 1] : 0) + (i == kFew ? (int64_t)n.few[a.G] * nu : (int64_t)n.of[i < kFew ? i : 0][a.G] * nt);
-    const int64_t tiles = ends[kFew - 1], units = ends[kFew] - tiles;
+    __shared__ __attribute__((aligned(16))) unsigned char smem[kTileLds];
+    Counts &n = *reinterpret_cast<Counts *>(smem); // until a tile's rows take its place
+    constexpr int SIDES = GATED ? 2 : 1, COLS = 32 * FW / SIDES, LOW = 32 * kLowColumns / SIDES;
+    static_assert(FW >= kLowColumns && sizeof(Counts) <= kTileLds, "columns of a low tile");
+    const int32_t nt = (a.N + COLS - 1) / COLS, nlow = (a.N + LOW - 1) / LOW;
     // Neighbours in the list start together on one XCD, 32 of them, which are dealt to the XCDs in turn.  One tile a workgroup:
-    // the next one starts wherever a CU is done first.  What workgroups are left take the units in turn.
-    const int64_t at = (int64_t)(blockIdx.x / 256) * 256 + (blockIdx.x % 8) * 32 + blockIdx.x % 256 / 8;
-    for (int64_t w = at; w < tiles; w += gridDim.x) {
+    // the next one starts wherever a CU is done first.  (The grid is short of the list only where that has millions of tiles.)
+    for (int64_t w = (int64_t)(blockIdx.x / 256) * 256 + (blockIdx.x % 8) * 32 + blockIdx.x % 256 / 8;; w += gridDim.x) {
+        count_tiles(a, height, n);
+        int64_t begin = 0;
+        int kind = 0;
+        for (; kind < kClasses; ++kind) {
+            const int64_t tiles = (int64_t)n.of[kind][a.G] * (kind == kFew ? nlow : nt);
+            if (w < begin + tiles) break;
+            begin += tiles;
+        }
+        kind = __builtin_amdgcn_readfirstlane(kind);
+        if (kind == kClasses) return;
+        const int32_t columns = kind == kFew ? nlow : nt;
+        const int64_t i = w - begin;
+        const int32_t *before = n.of[kind];
         Tile t;
         int64_t lo, hi;
         int32_t tr, tc;
-        const int kind = w < ends[0] ? 0 : w < ends[1] ? 1 : 2;
-        const int64_t i = w - (kind == 0 ? 0 : kind == 1 ? ends[0] : ends[1]);
-        const int32_t *before = n.of[kind];
-        t.group = group_of(before, a.G, (int32_t)(i / nt));
+        t.group = group_of(before, a.G, (int32_t)(i / columns));
         group_rows(a, t.group, lo, hi);
         const Cut cut = cut_rows((int32_t)(hi - lo), height);
-        place((int32_t)(i - (int64_t)before[t.group] * nt), cut.count, nt, tr, tc);
+        place((int32_t)(i - (int64_t)before[t.group] * columns), cut.count, columns, tr, tc);
         t.row0 = lo + (int64_t)tr * cut.height;
         t.rows = __builtin_amdgcn_readfirstlane((int32_t)min((int64_t)cut.height, hi - t.row0));
-        t.n0 = __builtin_amdgcn_readfirstlane(tc * COLS);
-        if constexpr (FW == 8) {
-            if (t.rows > 224) product_tile<FMT, GATED, FW, 8>(a, t, smem, row_scale, row_live);
-            else if (t.rows > 192) product_tile<FMT, GATED, FW, 7>(a, t, smem, row_scale, row_live);
-            else if (t.rows > 160) product_tile<FMT, GATED, FW, 6>(a, t, smem, row_scale, row_live);
-            else if (t.rows > 128) product_tile<FMT, GATED, FW, 5>(a, t, smem, row_scale, row_live);
-            else if (t.rows > 64) product_tile<FMT, GATED, FW, 4>(a, t, smem, row_scale, row_live);
-            else product_tile<FMT, GATED, FW, 2>(a, t, smem, row_scale, row_live);
+        t.n0 = __builtin_amdgcn_readfirstlane(tc * (kind == kFew ? LOW : COLS));
+        if (kind == kFew) {
+            if (t.rows > 32) product_tile<FMT, GATED, kLowColumns, 2>(a, t, smem);
+            else product_tile<FMT, GATED, kLowColumns, 1>(a, t, smem);
+        } else if constexpr (FW == 8) {
+            if (t.rows > 224) product_tile<FMT, GATED, FW, 8>(a, t, smem);
+            else if (t.rows > 192) product_tile<FMT, GATED, FW, 7>(a, t, smem);
+            else if (t.rows > 160) product_tile<FMT, GATED, FW, 6>(a, t, smem);
+            else if (t.rows > 128) product_tile<FMT, GATED, FW, 5>(a, t, smem);
+            else if (t.rows > 64) product_tile<FMT, GATED, FW, 4>(a, t, smem);
+            else product_tile<FMT, GATED, FW, 2>(a, t, smem);
         } else {
-            if (t.rows > 64) product_tile<FMT, GATED, FW, 4>(a, t, smem, row_scale, row_live);
-            else product_tile<FMT, GATED, FW, 2>(a, t, smem, row_scale, row_live);
+            if (t.rows > 64) product_tile<FMT, GATED, FW, 4>(a, t, smem);
+            else product_tile<FMT, GATED, FW, 2>(a, t, smem);
         }
-    }
-    const bool spare = tiles < (int64_t)gridDim.x; // (else every workgroup has had tiles)
-    if (spare && at < tiles) return;
-    for (int64_t i = spare ? at - tiles : at; i < units; i += spare ? gridDim.x - tiles : gridDim.x) {
-        Unit u;
-        int64_t lo, hi;
-        u.group = group_of(n.few, a.G, (int32_t)(i / nu));
-        group_rows(a, u.group, lo, hi);
-        u.n0 = __builtin_amdgcn_readfirstlane((int32_t)(i % nu) * 16 * REM);
-        u.rows = __builtin_amdgcn_readfirstlane((int32_t)(hi - lo));
-        u.row0 = lo;
-        unsigned char *const ring = smem + ((int)threadIdx.x >> 6) * kRingBytes;
-        acc_t *const part = reinterpret_cast<acc_t *>(smem);
-        if (u.rows <= 16) stream_unit<FMT, GATED, REM, 1, kStreamWaves>(a, u, ring, part);
-        else if (u.rows <= 32) stream_unit<FMT, GATED, REM, 2, kStreamWaves>(a, u, ring, part);
-        else stream_unit<FMT, GATED, REM, 4, kStreamWaves>(a, u, ring, part);
+        __syncthreads();                           // LDS may be filled again
     }
 }
 
 template <int FMT, bool GATED, int FW> hipError_t launch_width(const ProductArgs &a, int32_t height, hipStream_t s) {
-    constexpr int COLS = GATED ? 16 * FW : 32 * FW;
-    const int64_t nt = (a.N + COLS - 1) / COLS, nu = (a.N + 15) / 16;
-    // most tiles that there can be (a group's count rounds up twice: to whole tiles, and its rows to whole fragments, which leaves
-    // out tiles, never adds one), and workgroups for the units besides
-    const int64_t tiles = (a.M / height + std::min<int64_t>(a.M / (kUnitRows + 1), a.G)) * nt;
-    const int64_t grid = (tiles + std::min<int64_t>(std::min<int64_t>(a.M, a.G) * nu, a.num_cu) + 255) / 256 * 256;
+    constexpr int SIDES = GATED ? 2 : 1, COLS = 32 * FW / SIDES, LOW = 32 * kLowColumns / SIDES;
+    const int64_t nt = (a.N + COLS - 1) / COLS, nlow = (a.N + LOW - 1) / LOW;
+    // Most tiles that there can be.  (Heights round up to whole fragments: that leaves out tiles, never adds one.)
+    const int64_t tiles = (a.M / height + std::min<int64_t>(a.M / (kFewRows + 1), a.G)) * nt + std::min<int64_t>(a.M, a.G) * nlow;
+    const int64_t grid = (tiles + 255) / 256 * 256;
     hipLaunchKernelGGL((product_tile_kernel<FMT, GATED, FW>), dim3((unsigned)std::min<int64_t>(grid, 1 << 22)), dim3(kThreads), 0, s, a, height);
     return hipGetLastError();
 }
