@@ -26,13 +26,12 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kSlab = 128;                         // bytes of the contraction
 constexpr int kTileLds = 160 << 10;                // all there is
-// Stages of the weights and of x: weights come from HBM the first time, x mostly from L2, so weights get one more where that
-// is what there is room for.
+// Stages of the weights and of x.  Weights come from HBM the first time, x mostly from L2: where what is left holds a stage of
+// weights besides, they have one more.
 template <int FW, int FX> constexpr int both_stages() { return kTileLds / ((FW + FX) * 32 * kSlab); }
+template <int FW, int FX> constexpr bool more_weights() { return both_stages<FW, FX>() == 2 && (3 * FW + 2 * FX) * 32 * kSlab <= kTileLds; }
 template <int FW, int FX> constexpr int x_stages() { return both_stages<FW, FX>() < 6 ? both_stages<FW, FX>() : 6; }
-template <int FW, int FX> constexpr int w_stages() {
-    return x_stages<FW, FX>() < 6 && (x_stages<FW, FX>() * (FW + FX) + FW) * 32 * kSlab <= kTileLds ? x_stages<FW, FX>() + 1 : x_stages<FW, FX>();
-}
+template <int FW, int FX> constexpr int w_stages() { return more_weights<FW, FX>() ? 3 : x_stages<FW, FX>(); }
 constexpr int kLowColumns = 4;                     // fragments of weights a wave for groups of few rows
 
 template <int FMT> static __device__ __forceinline__ void multiply_in_place(raw_t w, raw_t x, typename Numbers<FMT>::acc_t &c) {
@@ -60,7 +59,7 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
     typedef typename Numbers<FMT>::acc_t acc_t;
     constexpr int M = FW * FX, NR = FW + FX, SW = w_stages<FW, FX>(), SX = x_stages<FW, FX>();
     constexpr uint32_t WSTAGE = FW * 32 * kSlab, XSTAGE = FX * 32 * kSlab, XRING = SW * WSTAGE;
-    static_assert(SX >= 2 && (SW == SX || (SX == 2 && SW == 3)) && XRING + SX * XSTAGE <= kTileLds && SX * NR <= 63, "stages");
+    static_assert(((SW == SX && SX >= 3) || (SX == 2 && SW == 3)) && XRING + SX * XSTAGE <= kTileLds && SX * NR <= 63, "stages");
     const int lane = threadIdx.x & 63, q = lane >> 4, r16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int32_t KB = a.row_bytes, nk = (KB + kSlab - 1) / kSlab;
@@ -101,13 +100,13 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
 
     // where slab ks begins in a row: the last one ends with it, and what the one before has is cut away
     auto at = [&](int ks) __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_readfirstlane(min(ks * kSlab, KB - kSlab)); };
-    // Request j of a slab: x's chunks, then the weights' (their order is what the waits count on); w, x: stages
-    auto aim = [&](int j, uint32_t w, uint32_t x) __attribute__((always_inline)) {
-        dma_to(lds_wave + (j < FX ? XRING + x + (uint32_t)(4096 * j) : w + (uint32_t)(4096 * (j - FX))));
+    // request i of a slab's x, or of its weights, into a stage of theirs
+    auto aim = [&](auto X, int i, uint32_t stage) __attribute__((always_inline)) {
+        dma_to(lds_wave + (X.value ? XRING : 0u) + stage + (uint32_t)(4096 * i));
     };
-    auto request = [&](int j, uint32_t kw, uint32_t kx) __attribute__((always_inline)) {
-        if (j < FX) dma_request(xbase + kx, xoff[j < FX ? j : 0]);
-        else dma_request(wbase + kw, woff[j < FX ? 0 : j - FX]);
+    auto request = [&](auto X, int i, uint32_t k) __attribute__((always_inline)) {
+        if constexpr (X.value) dma_request(xbase + k, xoff[i < FX ? i : 0]);
+        else dma_request(wbase + k, woff[i < FW ? i : 0]);
     };
     // x's fragments first, the next products start with those
     struct From { uint32_t x, w; };                // one register each, fragments at constant offsets from them
@@ -135,23 +134,25 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
             asm volatile("s_nop 1" : "+v"(wv[set][f]));
         }
     };
-    // One step: set STEP multiplied, the other one read from stages w and x; the first REQ requests of slabs at kw and kx into
-    // stages tw and tx as well.
-    auto step_of = [&](auto STEP, auto REQ, uint32_t w, uint32_t x, uint32_t tw, uint32_t tx, uint32_t kw, uint32_t kx) __attribute__((always_inline)) {
-        constexpr int set = STEP.value, R = REQ.value, OPS = NR + 2 * R;
+    // One step: set STEP multiplied, the other one read from stages w and x; and, if REQ, this slab's requests at k into
+    // stage `to`: weights in the first step, x in the second, so that they are as far apart as they can be (all of them in one step:
+    // 8192 x 4096 x 14336 in zeros 304 us).
+    auto step_of = [&](auto STEP, auto REQ, uint32_t w, uint32_t x, uint32_t to, uint32_t k) __attribute__((always_inline)) {
+        constexpr int set = STEP.value, R = !REQ.value ? 0 : set ? FX : FW, OPS = NR + 2 * R;
+        const std::integral_constant<bool, set == 1> of_x;
         const From p = from(set ^ 1, w, x);
 #pragma unroll
         for (int m = 0; m < M; ++m) {
             multiply_in_place<FMT>(wv[set][m / FX], xv[set][m % FX], acc[m / FX][m % FX]);
-            // spread over three quarters of the step: what is read has to be there when the next one begins
+            // spread over seven eighths of the step: what is read has to be there when the next one begins
 #pragma unroll
-            for (int o = min(m * OPS * 4 / (3 * M), OPS); o < min((m + 1) * OPS * 4 / (3 * M), OPS); ++o) {
+            for (int o = min(m * OPS * 8 / (7 * M), OPS); o < min((m + 1) * OPS * 8 / (7 * M), OPS); ++o) {
                 // a request's address, a fragment, the request: a load may not follow its M0 at once
                 const int i = o / 3;
                 if (i < R) {
-                    if (o % 3 == 0) aim(i, tw, tx);
+                    if (o % 3 == 0) aim(of_x, i, to);
                     else if (o % 3 == 1) fetch(set ^ 1, i, p);
-                    else request(i, kw, kx);
+                    else request(of_x, i, k);
                 } else {
                     fetch(set ^ 1, o - 2 * R, p);
                 }
@@ -161,26 +162,28 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
     };
     const std::integral_constant<int, 0> step0;
     const std::integral_constant<int, 1> step1;
-    const std::integral_constant<int, 0> nothing;
-    const std::integral_constant<int, FX> rows_only;
-    const std::integral_constant<int, NR> all;
     const std::true_type with;
     const std::false_type without;
     const bool cuts = nk * kSlab != KB;
 
     __syncthreads();                               // nobody reads what LDS held
-#pragma unroll
-    for (int j = 0; j < SW; ++j)
+    auto start = [&](auto X, int j) __attribute__((always_inline)) {
         if (j < nk) {
             const uint32_t k = at(j);
 #pragma unroll
-            for (int i = j < SX ? 0 : FX; i < NR; ++i) {
-                aim(i, j * WSTAGE, j * XSTAGE);
+            for (int i = 0; i < (X.value ? FX : FW); ++i) {
+                aim(X, i, j * (X.value ? XSTAGE : WSTAGE));
                 asm volatile("s_nop 0");
-                request(i, k, k);
+                request(X, i, k);
             }
         }
-    if (nk >= SW) dma_wait<(SX - 1) * NR + (SW - SX) * FW>();
+    };
+#pragma unroll
+    for (int j = 0; j < SX; ++j) {
+        start(with, j);
+        if (j < SW - 1) start(without, j);
+    }
+    if (nk >= SX) dma_wait<(SX - 1) * FX + (SW - 2) * FW>();
     else dma_wait<0>();
     __syncthreads();
 #pragma unroll
@@ -189,24 +192,27 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
     int ks = 0;
     auto next_w = [&](uint32_t v) { return v + WSTAGE < SW * WSTAGE ? v + WSTAGE : 0; };
     auto next_x = [&](uint32_t v) { return v + XSTAGE < SX * XSTAGE ? v + XSTAGE : 0; };
-    // Behind the first step all of slab ks is in registers, for every wave at the barrier, and slab ks + 1 has landed: what
-    // was requested behind its x may be on its way, and behind its weights, which are a slab older where they have a stage more.
-    constexpr int BEHIND = (SX - 2) * NR + (SW > SX ? FW : 0);
-    for (; ks + SW < nk; ++ks) {
+    auto last_w = [&](uint32_t v) { return v > 0 ? v - WSTAGE : (SW - 1) * WSTAGE; };
+    // In slab ks, weights of slab ks + SW - 1 are requested into the stage of slab ks - 1, behind the barrier x of slab ks + SX into
+    // that of slab ks.  At the barrier, behind the first step, all of slab ks is in registers of every wave and slab ks + 1 has landed:
+    // what was requested behind its x and its weights may be on its way.
+    constexpr int BEHIND_X = (SX - 1) * FW + (SX - 2) * FX, BEHIND_W = (SW - 2) * NR;
+    constexpr int BEHIND = BEHIND_X < BEHIND_W ? BEHIND_X : BEHIND_W;
+    for (; ks + SX < nk; ++ks) {
         const uint32_t tw = next_w(hw), tx = next_x(hx);
-        step_of(step0, nothing, hw, hx, 0, 0, 0, 0);
+        step_of(step0, with, hw, hx, last_w(hw), at(ks + SW - 1));
         dma_wait<BEHIND>();
         __syncthreads();
-        step_of(step1, all, tw, tx, hw, hx, at(ks + SW), at(ks + SX));
+        step_of(step1, with, tw, tx, hx, at(ks + SX));
         hw = tw;
         hx = tx;
     }
-    if (SW > SX && ks + SX < nk) {                 // the last rows of x that are still to be requested
+    if (SW == SX && ks + SX == nk) {               // the last weights are still to be requested
         const uint32_t tw = next_w(hw), tx = next_x(hx);
-        step_of(step0, nothing, hw, hx, 0, 0, 0, 0);
+        step_of(step0, with, hw, hx, last_w(hw), at(ks + SW - 1));
         dma_wait<BEHIND>();
         __syncthreads();
-        step_of(step1, rows_only, tw, tx, hw, hx, 0, at(ks + SX));
+        step_of(step1, without, tw, tx, 0, 0);
         hw = tw;
         hx = tx;
         ++ks;
@@ -215,12 +221,12 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
         const uint32_t tw = next_w(hw), tx = next_x(hx);
         const bool last = ks + 1 == nk;
         if (last && cuts) cut(0);
-        step_of(step0, nothing, hw, hx, 0, 0, 0, 0);
-        if (SW == SX && ks + 2 < nk) dma_wait<NR>();      // one slab or more behind the next
+        step_of(step0, without, hw, hx, 0, 0);
+        if (ks + 2 < nk) dma_wait<FW>();           // the last weights were requested behind what is needed now
         else dma_wait<0>();
         __syncthreads();
         if (last && cuts) cut(1);
-        step_of(step1, nothing, tw, tx, 0, 0, 0, 0);      // (behind the last slab: read and not used)
+        step_of(step1, without, tw, tx, 0, 0);     // (behind the last slab: read and not used)
         hw = tw;
         hx = tx;
     }
