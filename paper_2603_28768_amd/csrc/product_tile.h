@@ -55,13 +55,13 @@ struct Tile {
 
 // FW, FX: 16-row fragments of weights and of x per wave; the tile is 32 FW columns (gated: 16 FW) x 32 FX rows.
 template <int FMT, bool GATED, int FW, int FX>
-static __device__ __forceinline__ void product_tile(const ProductArgs &a, const Tile &t, unsigned char *smem) {
+static __device__ __forceinline__ void product_tile(const ProductArgs &a, const Tile &t, unsigned char *smem, int tid) {
     typedef typename Numbers<FMT>::acc_t acc_t;
     constexpr int M = FW * FX, NR = FW + FX, SW = w_stages<FW, FX>(), SX = x_stages<FW, FX>();
     constexpr uint32_t WSTAGE = FW * 32 * kSlab, XSTAGE = FX * 32 * kSlab, XRING = SW * WSTAGE;
     static_assert(((SW == SX && SX >= 3) || (SX == 2 && SW == 3)) && XRING + SX * XSTAGE <= kTileLds && SX * NR <= 63, "stages");
-    const int lane = threadIdx.x & 63, q = lane >> 4, r16 = lane & 15;
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int lane = tid & 63, q = lane >> 4, r16 = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int32_t KB = a.row_bytes, nk = (KB + kSlab - 1) / kSlab;
     // Chunk 4 i + wave, eight rows of an operand, is this wave's i-th.  In front of LDS: weights, then x.
     const uint32_t piece = (uint32_t)(((lane & 7) ^ ((lane >> 3) & 7)) * 16);
@@ -75,7 +75,7 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
         xoff[i] = (uint32_t)((tok < 0 ? 0 : tok) * a.x_stride) + piece;
     }
     // what a thread's row of the tile is multiplied by; goes to LDS when there is time for it
-    const int64_t my_row = token_of(a, t.row0 + min((int)threadIdx.x, t.rows - 1));
+    const int64_t my_row = token_of(a, t.row0 + min(tid, t.rows - 1));
     const float my_scale = FMT == CRAFT_I8 ? a.x_scale[my_row < 0 ? 0 : my_row] : 1.0f;
     // Gated: 16 rows of gate are followed by the 16 of up of the same columns; the first two waves fetch gate's.
     const unsigned char *mat = a.off ? a.w[t.group] : a.w_one;
@@ -255,62 +255,80 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
     float *const row_scale = reinterpret_cast<float *>(smem + kTileLds - 4096);
     uint8_t *const row_live = smem + kTileLds - 2048;
     // By way of LDS, 16 rows at a time and each wave for itself, so that a store covers whole lines (16 rows of 32 bytes a
-    // request: 8 us a tile where this takes 3).  Stores are of 16 bytes whatever the alignment; a lane at the matrix' edge
-    // stores its columns one by one.
+    // request: 8 us a tile).  While 16 rows come back from there the next are worked out.  Stores are of 16 bytes whatever the
+    // alignment; a lane at the matrix' edge stores its columns one by one.
     auto results = [&](auto BF16) __attribute__((always_inline)) {
         constexpr bool bf16 = BF16.value;
         typedef typename std::conditional<bf16, uint16_t, float>::type out_t;
         typedef out_t piece_t __attribute__((ext_vector_type(16 / sizeof(out_t)), aligned(sizeof(out_t))));
-        constexpr int COLS = 16 * FW / SIDES, ROWB = COLS * (int)sizeof(out_t), PITCH = ROWB + 16;     // a row of this wave
-        constexpr int PER = ROWB / 16, EACH = 16 / (int)sizeof(out_t), PASSES = 16 * PER / 64;      // pieces of a row; elements of a piece
-        static_assert(4 * 16 * PITCH <= kTileLds - 4096, "rows of results");
-        unsigned char *const mine = smem + wave * (16 * PITCH);
-        const int32_t first = t.n0 + (wave >> 1) * COLS;
-        out_t *const out = static_cast<out_t *>(a.out) + first;
-#pragma unroll
-        for (int g = 0; g < FX; ++g) {
-            int l = lane;                          // (places are worked out here, not in front of the loop for all of it)
+        constexpr int ES = (int)sizeof(out_t), COLS = 16 * FW / SIDES, ROWB = COLS * ES, PITCH = ROWB + 16, BUFFER = 16 * PITCH;
+        constexpr int PER = ROWB / 16, EACH = 16 / ES, PASSES = 16 * PER / 64, ROWS = 64 / PER;     // pieces of a row; elements of a piece; rows of a pass
+        static_assert(4 * 2 * BUFFER <= kTileLds - 4096 && PER <= 64, "rows of results");
+        unsigned char *const mine = smem + wave * (2 * BUFFER);
+        const int32_t first = t.n0 + (wave >> 1) * COLS, row0 = (wave & 1) * FX * 16;
+        int l0 = lane;
+        asm volatile("" : "+v"(l0));
+        const int r = l0 / PER, c = l0 % PER * EACH;
+        const bool full = t.rows == 32 * FX && t.n0 + 2 * COLS <= a.N;      // the whole tile is there
+        out_t *p = static_cast<out_t *>(a.out) + first + c + (t.row0 + row0 + r) * a.out_stride;
+        const int64_t pass = ROWS * a.out_stride;
+        raw_t v[PASSES];
+        auto put = [&](int g) __attribute__((always_inline)) {
+            int l = lane;                          // (places are worked out here, not in front of everything for all of it)
             asm volatile("" : "+v"(l));
-            const int row = (wave & 1) * FX * 16 + 16 * g + (l & 15);
+            unsigned char *const to = mine + (g & 1) * BUFFER + (l & 15) * PITCH + (l >> 4) * 4 * ES;
+            const int row = row0 + 16 * g + (l & 15);
             const float xs = FMT == CRAFT_I8 ? row_scale[row] : 1.0f;
-            const bool live = row_live[row];
 #pragma unroll
             for (int f = 0; f < FW; f += SIDES) {
-                float v[SIDES][4];
+                float y[SIDES][4];
 #pragma unroll
                 for (int m = 0; m < SIDES; ++m)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[m][e] = FMT == CRAFT_I8 ? (float)acc[f + m][g][e] * xs * ws[f + m][e] : (float)acc[f + m][g][e];
+                    for (int e = 0; e < 4; ++e) y[m][e] = FMT == CRAFT_I8 ? (float)acc[f + m][g][e] * xs * ws[f + m][e] : (float)acc[f + m][g][e];
+                if constexpr (GATED)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if constexpr (GATED) v[0][e] = (bf16 ? silu_bf16(v[0][e]) : silu_f32(v[0][e])) * v[SIDES - 1][e];
-                    v[0][e] = live ? v[0][e] : 0.0f;
-                }
-                unsigned char *p = mine + (l & 15) * PITCH + (f / SIDES * 16 + 4 * (l >> 4)) * (int)sizeof(out_t);
-                if constexpr (bf16) *reinterpret_cast<uint2 *>(p) = make_uint2(product_bf16_pair(v[0][0], v[0][1]), product_bf16_pair(v[0][2], v[0][3]));
-                else *reinterpret_cast<float4 *>(p) = make_float4(v[0][0], v[0][1], v[0][2], v[0][3]);
+                    for (int e = 0; e < 4; ++e) y[0][e] = (bf16 ? silu_bf16(y[0][e]) : silu_f32(y[0][e])) * y[SIDES - 1][e];
+                if constexpr (bf16) *reinterpret_cast<uint2 *>(to + f / SIDES * 32) = make_uint2(product_bf16_pair(y[0][0], y[0][1]), product_bf16_pair(y[0][2], y[0][3]));
+                else *reinterpret_cast<float4 *>(to + f / SIDES * 64) = make_float4(y[0][0], y[0][1], y[0][2], y[0][3]);
             }
+            if (gather && !row_live[row])          // (seldom)
+#pragma unroll 1
+                for (int f = 0; f < FW / SIDES; ++f)
+                    for (int e = 0; e < 4; ++e) reinterpret_cast<out_t *>(to + f * 16 * ES)[e] = 0;
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        put(0);
+#pragma unroll
+        for (int g = 0; g < FX; ++g) {
             // (the wave's own rows: its reads follow its writes)
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            const unsigned char *from = mine + (g & 1) * BUFFER + r * PITCH + c * ES;
 #pragma unroll
-            for (int i = 0; i < PASSES; ++i) {
-                const int r = (i * 64 + l) / PER, c = (i * 64 + l) % PER * EACH, at = (wave & 1) * FX * 16 + 16 * g + r;
-                const unsigned char *from = mine + r * PITCH + c * (int)sizeof(out_t);
-                const raw_t v = *reinterpret_cast<const raw_t *>(from);
-                if (at < t.rows) {
-                    out_t *p = out + (t.row0 + at) * a.out_stride + c;
-                    if (first + c + EACH <= a.N) *reinterpret_cast<piece_t *>(p) = __builtin_bit_cast(piece_t, v);
-                    else
+            for (int i = 0; i < PASSES; ++i) v[i] = *reinterpret_cast<const raw_t *>(from + i * ROWS * PITCH);
+            __builtin_amdgcn_sched_barrier(0);
+            if (g + 1 < FX) put(g + 1);
+            if (full) {
+#pragma unroll
+                for (int i = 0; i < PASSES; ++i) *reinterpret_cast<piece_t *>(p + i * pass) = __builtin_bit_cast(piece_t, v[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < PASSES; ++i)
+                    if (row0 + 16 * g + i * ROWS + r < t.rows) {
+                        out_t *to = p + i * pass;
+                        if (first + c + EACH <= a.N) *reinterpret_cast<piece_t *>(to) = __builtin_bit_cast(piece_t, v[i]);
+                        else
 #pragma unroll 1
-                        for (int e = 0; first + c + e < a.N; ++e) p[e] = reinterpret_cast<const out_t *>(from)[e];
-                }
+                            for (int e = 0; first + c + e < a.N; ++e) to[e] = reinterpret_cast<const out_t *>(from + i * ROWS * PITCH)[e];
+                    }
             }
+            p += PASSES * pass;
             __builtin_amdgcn_sched_barrier(0);
         }
     };
     __syncthreads();                               // every wave has read the last slab
-    row_live[threadIdx.x] = my_row >= 0;
-    if (FMT == CRAFT_I8) row_scale[threadIdx.x] = my_scale;
+    row_live[tid] = my_row >= 0;
+    if (FMT == CRAFT_I8) row_scale[tid] = my_scale;
     __syncthreads();
     if (FMT != CRAFT_F32 && a.out_dtype == CRAFT_BF16) results(with);
     else results(without);
@@ -331,8 +349,8 @@ static __device__ __forceinline__ Cut cut_rows(int32_t rows, int32_t most) {
 struct Counts {
     int32_t of[kClasses][kMostGroups + 1];
 };
-static __device__ __forceinline__ void count_tiles(const ProductArgs &a, int32_t height, Counts &n) {
-    const int lane = threadIdx.x & 63;
+static __device__ __forceinline__ void count_tiles(const ProductArgs &a, int32_t height, Counts &n, int tid) {
+    const int lane = tid & 63;
     int32_t sum[kClasses] = {};
     for (int32_t g0 = 0; g0 < a.G; g0 += 64) {
         const int32_t g = g0 + lane;
@@ -385,7 +403,9 @@ __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a
     // Neighbours in the list start together on one XCD, 32 of them, which are dealt to the XCDs in turn.  One tile a workgroup:
     // the next one starts wherever a CU is done first.  (The grid is short of the list only where that has millions of tiles.)
     for (int64_t w = (int64_t)(blockIdx.x / 256) * 256 + (blockIdx.x % 8) * 32 + blockIdx.x % 256 / 8;; w += gridDim.x) {
-        count_tiles(a, height, n);
+        int tid = threadIdx.x;                     // (what depends on it is worked out for this tile, not kept for all)
+        asm volatile("" : "+v"(tid));
+        count_tiles(a, height, n, tid);
         int64_t begin = 0;
         int kind = 0;
         for (; kind < kClasses; ++kind) {
@@ -409,18 +429,18 @@ __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a
         t.rows = __builtin_amdgcn_readfirstlane((int32_t)min((int64_t)cut.height, hi - t.row0));
         t.n0 = __builtin_amdgcn_readfirstlane(tc * (kind == kFew ? LOW : COLS));
         if (kind == kFew) {
-            if (t.rows > 32) product_tile<FMT, GATED, kLowColumns, 2>(a, t, smem);
-            else product_tile<FMT, GATED, kLowColumns, 1>(a, t, smem);
+            if (t.rows > 32) product_tile<FMT, GATED, kLowColumns, 2>(a, t, smem, tid);
+            else product_tile<FMT, GATED, kLowColumns, 1>(a, t, smem, tid);
         } else if constexpr (FW == 8) {
-            if (t.rows > 224) product_tile<FMT, GATED, FW, 8>(a, t, smem);
-            else if (t.rows > 192) product_tile<FMT, GATED, FW, 7>(a, t, smem);
-            else if (t.rows > 160) product_tile<FMT, GATED, FW, 6>(a, t, smem);
-            else if (t.rows > 128) product_tile<FMT, GATED, FW, 5>(a, t, smem);
-            else if (t.rows > 64) product_tile<FMT, GATED, FW, 4>(a, t, smem);
-            else product_tile<FMT, GATED, FW, 2>(a, t, smem);
+            if (t.rows > 224) product_tile<FMT, GATED, FW, 8>(a, t, smem, tid);
+            else if (t.rows > 192) product_tile<FMT, GATED, FW, 7>(a, t, smem, tid);
+            else if (t.rows > 160) product_tile<FMT, GATED, FW, 6>(a, t, smem, tid);
+            else if (t.rows > 128) product_tile<FMT, GATED, FW, 5>(a, t, smem, tid);
+            else if (t.rows > 64) product_tile<FMT, GATED, FW, 4>(a, t, smem, tid);
+            else product_tile<FMT, GATED, FW, 2>(a, t, smem, tid);
         } else {
-            if (t.rows > 64) product_tile<FMT, GATED, FW, 4>(a, t, smem);
-            else product_tile<FMT, GATED, FW, 2>(a, t, smem);
+            if (t.rows > 64) product_tile<FMT, GATED, FW, 4>(a, t, smem, tid);
+            else product_tile<FMT, GATED, FW, 2>(a, t, smem, tid);
         }
         __syncthreads();                           // LDS may be filled again
     }
