@@ -394,55 +394,53 @@ static __device__ __forceinline__ void place(int32_t i, int32_t m, int32_t nt, i
 }
 
 template <int FMT, bool GATED, int FW>
-__global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a, int32_t height) {
+__global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a, int32_t height, int64_t first) {
     __shared__ __attribute__((aligned(16))) unsigned char smem[kTileLds];
     Counts &n = *reinterpret_cast<Counts *>(smem); // until a tile's rows take its place
     constexpr int SIDES = GATED ? 2 : 1, COLS = 32 * FW / SIDES, LOW = 32 * kLowColumns / SIDES;
     static_assert(FW >= kLowColumns && sizeof(Counts) <= kTileLds, "columns of a low tile");
     const int32_t nt = (a.N + COLS - 1) / COLS, nlow = (a.N + LOW - 1) / LOW;
-    // Neighbours in the list start together on one XCD, 32 of them, which are dealt to the XCDs in turn.  One tile a workgroup:
-    // the next one starts wherever a CU is done first.  (The grid is short of the list only where that has millions of tiles.)
-    for (int64_t w = (int64_t)(blockIdx.x / 256) * 256 + (blockIdx.x % 8) * 32 + blockIdx.x % 256 / 8;; w += gridDim.x) {
-        int tid = threadIdx.x;                     // (what depends on it is worked out for this tile, not kept for all)
-        asm volatile("" : "+v"(tid));
-        count_tiles(a, height, n, tid);
-        int64_t begin = 0;
-        int kind = 0;
-        for (; kind < kClasses; ++kind) {
-            const int64_t tiles = (int64_t)n.of[kind][a.G] * (kind == kFew ? nlow : nt);
-            if (w < begin + tiles) break;
-            begin += tiles;
-        }
-        kind = __builtin_amdgcn_readfirstlane(kind);
-        if (kind == kClasses) return;
-        const int32_t columns = kind == kFew ? nlow : nt;
-        const int64_t i = w - begin;
-        const int32_t *before = n.of[kind];
-        Tile t;
-        int64_t lo, hi;
-        int32_t tr, tc;
-        t.group = group_of(before, a.G, (int32_t)(i / columns));
-        group_rows(a, t.group, lo, hi);
-        const Cut cut = cut_rows((int32_t)(hi - lo), height);
-        place((int32_t)(i - (int64_t)before[t.group] * columns), cut.count, columns, tr, tc);
-        t.row0 = lo + (int64_t)tr * cut.height;
-        t.rows = __builtin_amdgcn_readfirstlane((int32_t)min((int64_t)cut.height, hi - t.row0));
-        t.n0 = __builtin_amdgcn_readfirstlane(tc * (kind == kFew ? LOW : COLS));
-        if (kind == kFew) {
-            if (t.rows > 32) product_tile<FMT, GATED, kLowColumns, 2>(a, t, smem, tid);
-            else product_tile<FMT, GATED, kLowColumns, 1>(a, t, smem, tid);
-        } else if constexpr (FW == 8) {
-            if (t.rows > 224) product_tile<FMT, GATED, FW, 8>(a, t, smem, tid);
-            else if (t.rows > 192) product_tile<FMT, GATED, FW, 7>(a, t, smem, tid);
-            else if (t.rows > 160) product_tile<FMT, GATED, FW, 6>(a, t, smem, tid);
-            else if (t.rows > 128) product_tile<FMT, GATED, FW, 5>(a, t, smem, tid);
-            else if (t.rows > 64) product_tile<FMT, GATED, FW, 4>(a, t, smem, tid);
-            else product_tile<FMT, GATED, FW, 2>(a, t, smem, tid);
-        } else {
-            if (t.rows > 64) product_tile<FMT, GATED, FW, 4>(a, t, smem, tid);
-            else product_tile<FMT, GATED, FW, 2>(a, t, smem, tid);
-        }
-        __syncthreads();                           // LDS may be filled again
+    // Neighbours in the list start together on one XCD, 32 of them, which are dealt to the XCDs in turn.  One tile a workgroup: the next
+    // one starts wherever a CU is done first.  (No loop over tiles: what the compiler keeps across one costs registers that a
+    // tile needs, and memory to spill them to costs every workgroup its start: 8192 x 4096 x 7168 178 us, without 173.)
+    const int64_t w = first + (int64_t)(blockIdx.x / 256) * 256 + (blockIdx.x % 8) * 32 + blockIdx.x % 256 / 8;
+    const int tid = threadIdx.x;
+    count_tiles(a, height, n, tid);
+    int64_t begin = 0;
+    int kind = 0;
+    for (; kind < kClasses; ++kind) {
+        const int64_t tiles = (int64_t)n.of[kind][a.G] * (kind == kFew ? nlow : nt);
+        if (w < begin + tiles) break;
+        begin += tiles;
+    }
+    kind = __builtin_amdgcn_readfirstlane(kind);
+    if (kind == kClasses) return;
+    const int32_t columns = kind == kFew ? nlow : nt;
+    const int64_t i = w - begin;
+    const int32_t *before = n.of[kind];
+    Tile t;
+    int64_t lo, hi;
+    int32_t tr, tc;
+    t.group = group_of(before, a.G, (int32_t)(i / columns));
+    group_rows(a, t.group, lo, hi);
+    const Cut cut = cut_rows((int32_t)(hi - lo), height);
+    place((int32_t)(i - (int64_t)before[t.group] * columns), cut.count, columns, tr, tc);
+    t.row0 = lo + (int64_t)tr * cut.height;
+    t.rows = __builtin_amdgcn_readfirstlane((int32_t)min((int64_t)cut.height, hi - t.row0));
+    t.n0 = __builtin_amdgcn_readfirstlane(tc * (kind == kFew ? LOW : COLS));
+    if (kind == kFew) {
+        if (t.rows > 32) product_tile<FMT, GATED, kLowColumns, 2>(a, t, smem, tid);
+        else product_tile<FMT, GATED, kLowColumns, 1>(a, t, smem, tid);
+    } else if constexpr (FW == 8) {
+        if (t.rows > 224) product_tile<FMT, GATED, FW, 8>(a, t, smem, tid);
+        else if (t.rows > 192) product_tile<FMT, GATED, FW, 7>(a, t, smem, tid);
+        else if (t.rows > 160) product_tile<FMT, GATED, FW, 6>(a, t, smem, tid);
+        else if (t.rows > 128) product_tile<FMT, GATED, FW, 5>(a, t, smem, tid);
+        else if (t.rows > 64) product_tile<FMT, GATED, FW, 4>(a, t, smem, tid);
+        else product_tile<FMT, GATED, FW, 2>(a, t, smem, tid);
+    } else {
+        if (t.rows > 64) product_tile<FMT, GATED, FW, 4>(a, t, smem, tid);
+        else product_tile<FMT, GATED, FW, 2>(a, t, smem, tid);
     }
 }
 
@@ -451,8 +449,11 @@ template <int FMT, bool GATED, int FW> hipError_t launch_width(const ProductArgs
     const int64_t nt = (a.N + COLS - 1) / COLS, nlow = (a.N + LOW - 1) / LOW;
     // Most tiles that there can be.  (Heights round up to whole fragments: that leaves out tiles, never adds one.)
     const int64_t tiles = (a.M / height + std::min<int64_t>(a.M / (kFewRows + 1), a.G)) * nt + std::min<int64_t>(a.M, a.G) * nlow;
-    const int64_t grid = (tiles + 255) / 256 * 256;
-    hipLaunchKernelGGL((product_tile_kernel<FMT, GATED, FW>), dim3((unsigned)std::min<int64_t>(grid, 1 << 22)), dim3(kThreads), 0, s, a, height);
+    constexpr int64_t MOST = 1 << 22;              // workgroups of a launch, which has fewer than 2^32 threads
+    for (int64_t first = 0; first < tiles; first += MOST) {
+        const int64_t grid = (std::min(tiles - first, MOST) + 255) / 256 * 256;
+        hipLaunchKernelGGL((product_tile_kernel<FMT, GATED, FW>), dim3((unsigned)grid), dim3(kThreads), 0, s, a, height, first);
+    }
     return hipGetLastError();
 }
 template <int FMT> hipError_t launch_tiles(const ProductArgs &a, int32_t width, int32_t height, hipStream_t s) {
