@@ -348,7 +348,8 @@ struct ProductArgs {
     int32_t format, out_dtype;     // CRAFT_F32, _BF16, _I8 of x and w; CRAFT_F32 or _BF16
     int32_t G, N;
     int32_t row_bytes;             // of the contraction
-    int32_t k;
+    int32_t k;                     // src counts assignments, k to a row of x
+    uint32_t k_magic, k_shift;     // k > 1: the quotient by k is the upper half of the product with magic, shifted
     int64_t M, x_rows;
     int64_t x_stride;              // bytes
     int64_t out_stride;            // elements

@@ -109,6 +109,12 @@ craft_status craft_grouped_matmul(const craft_grouped_matmul_args *g, void *stre
     }
     a.G = g->G;
     a.k = g->src ? g->k : 1;
+    if (a.k > 1) {
+        int bits = 1;                              // ceil(log2 k)
+        while (((int64_t)1 << bits) < a.k) ++bits;
+        a.k_magic = (uint32_t)((((uint64_t)1 << (31 + bits)) + (uint32_t)a.k - 1) / (uint32_t)a.k);
+        a.k_shift = (uint32_t)(bits - 1);
+    }
     a.src = g->src;
     a.off = g->off;
     a.w = reinterpret_cast<const unsigned char *const *>(g->w);

@@ -82,12 +82,12 @@ static __device__ __forceinline__ void store_columns(const ProductArgs &a, int64
     }
 }
 
-// Row p of the products is row `token` of x; -1: the permutation names no row of x, and the result is zeros.
-static __device__ __forceinline__ int64_t token_of(const ProductArgs &a, int64_t p) {
-    if (!a.src) return p;
+// Row p of the products is this row of x; -1: the permutation names none, and the result is zeros.  Only where there is one.
+static __device__ __forceinline__ int32_t token_of(const ProductArgs &a, int64_t p) {
     const int32_t s = a.src[p];
-    const int64_t t = s >= 0 ? s / a.k : -1;
-    return t < a.x_rows ? t : -1;
+    // s / k: the product with 2^(31 + l) / k rounded up, l = ceil(log2 k), is exact for 31 bits
+    const int32_t t = a.k == 1 ? s : (int32_t)(__umulhi((uint32_t)s, a.k_magic) >> a.k_shift);
+    return s >= 0 && t < a.x_rows ? t : -1;
 }
 
 // Rows of group g, inside [0, M) whatever the offsets are.
@@ -100,6 +100,20 @@ static __device__ __forceinline__ void group_rows(const ProductArgs &a, int32_t 
     const int64_t l = a.off[g], h = a.off[g + 1];
     lo = l < 0 ? 0 : l < a.M ? l : a.M;
     hi = h < lo ? lo : h < a.M ? h : a.M;
+}
+
+// Inclusive sums over the lanes of a wave.
+template <int DPP, int ROWS> static __device__ __forceinline__ int32_t lane_before(int32_t x) {
+    return __builtin_amdgcn_update_dpp(0, x, DPP, ROWS, 0xf, false);
+}
+static __device__ __forceinline__ int32_t wave_sums(int32_t x) {
+    x += lane_before<0x111, 0xf>(x);               // one, two, four, eight lanes up a row of 16
+    x += lane_before<0x112, 0xf>(x);
+    x += lane_before<0x114, 0xf>(x);
+    x += lane_before<0x118, 0xf>(x);
+    x += lane_before<0x142, 0xa>(x);               // a row's last lane into the next row, the second one's into the upper half
+    x += lane_before<0x143, 0xc>(x);
+    return x;
 }
 
 }  // namespace craft

@@ -44,7 +44,7 @@ static __device__ __forceinline__ void stream_unit(const ProductArgs &a, const U
     for (int j = 0; j < 2 * CF; ++j) woff[j] = (uint32_t)min(8 * j + (lane >> 3), a.N - 1 - u.n0) * (uint32_t)KB + piece;
 #pragma unroll
     for (int j = 0; j < 2 * RF; ++j) {
-        const int64_t t = token_of(a, u.row0 + min(8 * j + (lane >> 3), u.rows - 1));
+        const int64_t p = u.row0 + min(8 * j + (lane >> 3), u.rows - 1), t = a.src ? token_of(a, p) : p;
         x[j] = a.x + (t < 0 ? 0 : t) * a.x_stride + piece;
     }
     const uint32_t lds0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)ring);
@@ -139,7 +139,7 @@ static __device__ __forceinline__ void stream_unit(const ProductArgs &a, const U
             }
             const int32_t row = 16 * g + r16, col = u.n0 + 16 * c + 4 * q;
             if (row >= u.rows || col >= a.N) continue;
-            const int64_t p = u.row0 + row, t = token_of(a, p);
+            const int64_t p = u.row0 + row, t = a.src ? token_of(a, p) : p;
             float v[MATS][4];
 #pragma unroll
             for (int m = 0; m < MATS; ++m) {

@@ -19,14 +19,9 @@ static __device__ __forceinline__ void count_blocks(const ProductArgs &a, int32_
         int64_t lo = 0, hi = 0;
         if (g < a.G) group_rows(a, g, lo, hi);
         int32_t n = (int32_t)((hi - lo + kUnitRows - 1) / kUnitRows);
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int32_t up = __shfl_up(n, d, 64);
-            n += lane >= d ? up : 0;
-        }
-        n += sum;
+        n = sum + wave_sums(n);
         if (g < a.G) before[g + 1] = n;
-        sum = __shfl(n, 63, 64);
+        sum = __builtin_amdgcn_readlane(n, 63);
     }
     before[0] = 0;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");

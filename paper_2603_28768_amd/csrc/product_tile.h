@@ -71,15 +71,21 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
 #pragma unroll
     for (int i = 0; i < FX; ++i) {
         const int r = min(8 * (4 * i + wave) + (lane >> 3), t.rows - 1);
-        const int64_t tok = gather ? token_of(a, t.row0 + r) : r;
-        xoff[i] = (uint32_t)((tok < 0 ? 0 : tok) * a.x_stride) + piece;
+        const int32_t tok = gather ? token_of(a, t.row0 + r) : r;
+        xoff[i] = (uint32_t)max(tok, 0) * (uint32_t)a.x_stride + piece;
     }
     // what a thread's row of the tile is multiplied by; goes to LDS when there is time for it
-    const int64_t my_row = token_of(a, t.row0 + min(tid, t.rows - 1));
+    const int64_t my_row = gather ? token_of(a, t.row0 + min(tid, t.rows - 1)) : t.row0 + min(tid, t.rows - 1);
     const float my_scale = FMT == CRAFT_I8 ? a.x_scale[my_row < 0 ? 0 : my_row] : 1.0f;
     // Gated: 16 rows of gate are followed by the 16 of up of the same columns; the first two waves fetch gate's.
-    const unsigned char *mat = a.off ? a.w[t.group] : a.w_one;
-    if (GATED && wave >= 2) mat = a.up[t.group];
+    const unsigned char *mat;
+    if constexpr (GATED) {
+        const unsigned char *const *side = a.w;
+        if (wave >= 2) side = a.up;
+        mat = side[t.group];
+    } else {
+        mat = a.off ? a.w[t.group] : a.w_one;
+    }
     const ubase_t wbase = uniform_base(mat + (int64_t)t.n0 * KB);
     auto column = [](int r) { return GATED ? (r >> 5) * 16 + (r & 15) : r; };
 #pragma unroll
@@ -166,7 +172,6 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
     const std::false_type without;
     const bool cuts = nk * kSlab != KB;
 
-    __syncthreads();                               // nobody reads what LDS held
     auto start = [&](auto X, int j) __attribute__((always_inline)) {
         if (j < nk) {
             const uint32_t k = at(j);
@@ -344,44 +349,19 @@ static __device__ __forceinline__ Cut cut_rows(int32_t rows, int32_t most) {
     const int32_t tiles = (rows + most - 1) / most, height = ((rows + tiles - 1) / tiles + 31) / 32 * 32;
     return {height > 192 ? 0 : height > 128 ? 1 : 2, height, (rows + height - 1) / height};
 }
-// Row tiles of each class that the groups up to one have: [G + 1], in LDS.  Every wave works them out for itself
-// and stores the same, so that no barrier is needed: a wave reads what it has written.
-struct Counts {
-    int32_t of[kClasses][kMostGroups + 1];
+// 64 groups, one a lane: their rows and how they are cut.
+struct Groups {
+    int64_t lo, hi;
+    Cut cut;
 };
-static __device__ __forceinline__ void count_tiles(const ProductArgs &a, int32_t height, Counts &n, int tid) {
-    const int lane = tid & 63;
-    int32_t sum[kClasses] = {};
-    for (int32_t g0 = 0; g0 < a.G; g0 += 64) {
-        const int32_t g = g0 + lane;
-        int64_t lo = 0, hi = 0;
-        if (g < a.G) group_rows(a, g, lo, hi);
-        const Cut cut = cut_rows((int32_t)(hi - lo), height);
-#pragma unroll
-        for (int i = 0; i < kClasses; ++i) {
-            int32_t c = cut.kind == i ? cut.count : 0;
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const int32_t up = __shfl_up(c, d, 64);
-                c += lane >= d ? up : 0;
-            }
-            c += sum[i];
-            sum[i] = __shfl(c, 63, 64);
-            if (g < a.G) n.of[i][g + 1] = c;
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < kClasses; ++i) n.of[i][0] = 0;
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+static __device__ __forceinline__ Groups groups_at(const ProductArgs &a, int32_t g, int32_t height) {
+    Groups r = {0, 0, {}};
+    if (g < a.G) group_rows(a, g, r.lo, r.hi);
+    r.cut = cut_rows((int32_t)(r.hi - r.lo), height);
+    return r;
 }
-// before[g] <= i < before[g + 1]
-static __device__ __forceinline__ int32_t group_of(const int32_t *before, int32_t G, int32_t i) {
-    int32_t lo = 0, hi = G;
-    while (hi - lo > 1) {
-        const int32_t mid = (lo + hi) >> 1;
-        if (before[mid] <= i) lo = mid; else hi = mid;
-    }
-    return __builtin_amdgcn_readfirstlane(lo);
+static __device__ __forceinline__ int64_t lane_value(int64_t v, int lane) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane));
 }
 
 // Item i of a group's m x nt tiles: blocks of 8 x 8, column by column inside a block, so that the tiles that run at one
@@ -396,38 +376,57 @@ static __device__ __forceinline__ void place(int32_t i, int32_t m, int32_t nt, i
 template <int FMT, bool GATED, int FW>
 __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a, int32_t height, int64_t first) {
     __shared__ __attribute__((aligned(16))) unsigned char smem[kTileLds];
-    Counts &n = *reinterpret_cast<Counts *>(smem); // until a tile's rows take its place
     constexpr int SIDES = GATED ? 2 : 1, COLS = 32 * FW / SIDES, LOW = 32 * kLowColumns / SIDES;
-    static_assert(FW >= kLowColumns && sizeof(Counts) <= kTileLds, "columns of a low tile");
+    static_assert(FW >= kLowColumns, "columns of a low tile");
     const int32_t nt = (a.N + COLS - 1) / COLS, nlow = (a.N + LOW - 1) / LOW;
     // Neighbours in the list start together on one XCD, 32 of them, which are dealt to the XCDs in turn.  One tile a workgroup: the next
     // one starts wherever a CU is done first.  (No loop over tiles: what the compiler keeps across one costs registers that a
     // tile needs, and memory to spill them to costs every workgroup its start: 8192 x 4096 x 7168 178 us, without 173.)
     const int64_t w = first + (int64_t)(blockIdx.x / 256) * 256 + (blockIdx.x % 8) * 32 + blockIdx.x % 256 / 8;
-    const int tid = threadIdx.x;
-    count_tiles(a, height, n, tid);
-    int64_t begin = 0;
-    int kind = 0;
-    for (; kind < kClasses; ++kind) {
-        const int64_t tiles = (int64_t)n.of[kind][a.G] * (kind == kFew ? nlow : nt);
-        if (w < begin + tiles) break;
-        begin += tiles;
+    const int tid = threadIdx.x, lane = tid & 63;
+    // Every wave finds the tile for itself, in registers: how many row tiles of each class there are, then the group.
+    Groups own = groups_at(a, lane, height);
+    int32_t total[kClasses] = {};
+    for (int32_t g0 = 0; g0 < a.G; g0 += 64) {
+        const Groups at = a.G <= 64 ? own : groups_at(a, g0 + lane, height);
+#pragma unroll
+        for (int i = 0; i < kClasses; ++i) total[i] += __builtin_amdgcn_readlane(wave_sums(at.cut.kind == i ? at.cut.count : 0), 63);
     }
-    kind = __builtin_amdgcn_readfirstlane(kind);
+    int64_t begin = 0;
+    int kind = kClasses;
+#pragma unroll
+    for (int i = 0; i < kClasses; ++i)
+        if (kind == kClasses) {
+            const int64_t tiles = (int64_t)total[i] * (i == kFew ? nlow : nt);
+            if (w < begin + tiles) kind = i;
+            else begin += tiles;
+        }
     if (kind == kClasses) return;
-    const int32_t columns = kind == kFew ? nlow : nt;
-    const int64_t i = w - begin;
-    const int32_t *before = n.of[kind];
-    Tile t;
-    int64_t lo, hi;
+    const int32_t columns = kind == kFew ? nlow : nt, place_in = (int32_t)((w - begin) / columns);
+    Tile t = {};
+    int32_t before = 0, height_in = 0, count_in = 0;
+    int64_t lo = 0, hi = 0;
+    for (int32_t g0 = 0, run = 0;; g0 += 64) {
+        if (a.G > 64) own = groups_at(a, g0 + lane, height);
+        const int32_t mine = own.cut.kind == kind ? own.cut.count : 0, upto = run + wave_sums(mine);
+        const uint64_t behind = __ballot(upto > place_in);
+        if (behind) {
+            const int at = __builtin_ctzll(behind);
+            t.group = g0 + at;
+            before = __builtin_amdgcn_readlane(upto - mine, at);
+            height_in = __builtin_amdgcn_readlane(own.cut.height, at);
+            count_in = __builtin_amdgcn_readlane(own.cut.count, at);
+            lo = lane_value(own.lo, at);
+            hi = lane_value(own.hi, at);
+            break;
+        }
+        run = __builtin_amdgcn_readlane(upto, 63);
+    }
     int32_t tr, tc;
-    t.group = group_of(before, a.G, (int32_t)(i / columns));
-    group_rows(a, t.group, lo, hi);
-    const Cut cut = cut_rows((int32_t)(hi - lo), height);
-    place((int32_t)(i - (int64_t)before[t.group] * columns), cut.count, columns, tr, tc);
-    t.row0 = lo + (int64_t)tr * cut.height;
-    t.rows = __builtin_amdgcn_readfirstlane((int32_t)min((int64_t)cut.height, hi - t.row0));
-    t.n0 = __builtin_amdgcn_readfirstlane(tc * (kind == kFew ? LOW : COLS));
+    place((int32_t)(w - begin - (int64_t)before * columns), count_in, columns, tr, tc);
+    t.row0 = lo + (int64_t)tr * height_in;
+    t.rows = (int32_t)min((int64_t)height_in, hi - t.row0);
+    t.n0 = tc * (kind == kFew ? LOW : COLS);
     if (kind == kFew) {
         if (t.rows > 32) product_tile<FMT, GATED, kLowColumns, 2>(a, t, smem, tid);
         else product_tile<FMT, GATED, kLowColumns, 1>(a, t, smem, tid);
