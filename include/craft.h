@@ -587,7 +587,7 @@ craft_status craft_matmul_i8(int64_t M, int32_t N, int32_t K, const int8_t *x, i
  * Which rows a group has is read on the GPU: a recorded call follows the offsets of each replay.  The
  * result depends on the arguments only, never on scheduling.
  * Limits: G <= 1024;  rows of x and w are whole multiples of 16 bytes, shorter than 8 MiB;
- * K < 131072 for CRAFT_I8;  N <= 2^30;  M, x_rows < 2^31, M may be 0. */
+ * K < 131072 for CRAFT_I8;  N <= 2^30;  M <= 2^26, may be 0;  x_rows < 2^31. */
 typedef struct {
     int32_t format, out_dtype;
     int32_t G, N, K, k;

@@ -9,6 +9,7 @@ inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_
 
 constexpr int64_t kInts = (int64_t)1 << 31;       // 32-bit indices stay below this
 constexpr int64_t kFarthest = (int64_t)1 << 46;   // bytes from a matrix' start to its end
+constexpr int64_t kMostRows = (int64_t)1 << 26;    // of a grouped product: tiles of groups that overlap stay countable
 constexpr int32_t kMostCodes = 131071;            // of a contraction: products of two codes are at most 2^14, sums below 2^31
 constexpr int64_t kLongestRow = (int64_t)1 << 23; // bytes of the contraction: 256 rows stay inside a 32-bit offset
 
@@ -98,7 +99,7 @@ craft_status craft_grouped_matmul(const craft_grouped_matmul_args *g, void *stre
     ProductArgs a{};
     const craft_status st = sizes(g->format, g->out_dtype, g->M, g->N, g->K, g->src ? g->x_rows : g->M, g->x_stride, g->out_stride, &a);
     if (st != CRAFT_OK) return st;
-    if (g->G <= 0 || g->G > kMostGroups) return CRAFT_EINVAL;
+    if (g->G <= 0 || g->G > kMostGroups || g->M > kMostRows) return CRAFT_EINVAL;
     if (g->src && (g->k <= 0 || !aligned(g->src, 4))) return CRAFT_EINVAL;
     if (g->M == 0) return CRAFT_OK;
     if (g->src && g->x_rows == 0) return CRAFT_EINVAL;         // places whose row is not there are read from row 0

@@ -1,6 +1,6 @@
 // Few rows of a group against its weights, which are read once.
 //
-// A unit is 16 CF columns of one group's matrix (gated: of both) against up to 64 of its rows.  One wave has it by itself,
+// A unit is 16 CF columns of one group's matrix (gated: of both) against up to 16 RF of its rows.  One wave has it by itself,
 // or SPLIT waves of a workgroup share it along the contraction: wave v takes slabs v, v + SPLIT, .. of 128 bytes a row, and
 // the waves' sums meet in LDS and are added in wave order (integers: any order gives the same).
 // Weights and rows travel straight into LDS, whole lines of eight rows a request, into a ring of slabs that is the wave's own:
@@ -13,22 +13,20 @@
 
 namespace craft {
 
-constexpr int kUnitRows = 64;
-constexpr int kStreamWaves = 4;
-constexpr int kRingBytes = 36 << 10;               // of a wave
+constexpr int kStreamLds = 144 << 10;              // of a workgroup, shared among its waves
 
 struct Unit {
-    int32_t group, n0, rows;       // rows of this unit, 1 .. 64
+    int32_t group, n0, rows;       // rows of this unit, 1 .. 16 RF
     int64_t row0;                  // its first row among the M
 };
 
 // ring: this wave's part of LDS;  part: room for the sums of SPLIT waves, LDS that nobody reads any more once all are here
-template <int FMT, bool GATED, int CF, int RF, int SPLIT>
+template <int FMT, bool GATED, int CF, int RF, int SPLIT, int RING>
 static __device__ __forceinline__ void stream_unit(const ProductArgs &a, const Unit &u, unsigned char *ring, typename Numbers<FMT>::acc_t *part) {
     typedef Numbers<FMT> T;
     typedef typename T::acc_t acc_t;
     constexpr int MATS = GATED ? 2 : 1, WF = CF * MATS, NR = WF + RF, SLAB = NR * 2048, REQ = 2 * NR;
-    constexpr int D0 = kRingBytes / SLAB, D = D0 < 8 ? D0 : 8;
+    constexpr int D0 = RING / SLAB, D = D0 < 8 ? D0 : 8;
     static_assert(D >= 2 && D * REQ <= 63, "slabs on their way");
     const int lane = threadIdx.x & 63, q = lane >> 4, r16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), mine = SPLIT > 1 ? wave : 0;

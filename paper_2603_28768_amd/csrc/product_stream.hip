@@ -7,19 +7,20 @@
 namespace craft {
 namespace {
 
-constexpr int kThreads = 64 * kStreamWaves;
+// Eight waves of half the ring each, with blocks of 32 rows, take the same time within 3 % but for 250 rows on 32 experts in bf16,
+// which they read in 78 us in place of 72.
+constexpr int kStreamWaves = 4;
 
-// Row blocks of 64 before each group, in LDS: [G + 1].  Every wave works them out for itself and stores the same, so
+// Blocks of ROWS rows before each group, in LDS: [G + 1].  Every wave works them out for itself and stores the same, so
 // that no barrier is needed: a wave reads what it has written.
-static __device__ __forceinline__ void count_blocks(const ProductArgs &a, int32_t *before) {
+template <int ROWS> static __device__ __forceinline__ void count_blocks(const ProductArgs &a, int32_t *before) {
     const int lane = threadIdx.x & 63;
     int32_t sum = 0;
     for (int32_t g0 = 0; g0 < a.G; g0 += 64) {
         const int32_t g = g0 + lane;
         int64_t lo = 0, hi = 0;
         if (g < a.G) group_rows(a, g, lo, hi);
-        int32_t n = (int32_t)((hi - lo + kUnitRows - 1) / kUnitRows);
-        n = sum + wave_sums(n);
+        const int32_t n = sum + wave_sums((int32_t)((hi - lo + ROWS - 1) / ROWS));
         if (g < a.G) before[g + 1] = n;
         sum = __builtin_amdgcn_readlane(n, 63);
     }
@@ -27,19 +28,20 @@ static __device__ __forceinline__ void count_blocks(const ProductArgs &a, int32_
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
-// ROWS: most 16-row fragments of a unit
-template <int FMT, bool GATED, int CF, int ROWS, int SPLIT>
-__global__ __launch_bounds__(kThreads) void product_stream_kernel(ProductArgs a) {
+// MOST: 16-row fragments of a block; SPLIT: 1 or WAVES
+template <int FMT, bool GATED, int CF, int MOST, int WAVES, int SPLIT>
+__global__ __launch_bounds__(64 * WAVES) void product_stream_kernel(ProductArgs a) {
     typedef typename Numbers<FMT>::acc_t acc_t;
-    __shared__ __attribute__((aligned(16))) unsigned char smem[kStreamWaves * kRingBytes];
+    constexpr int RING = kStreamLds / WAVES, ROWS = 16 * MOST;
+    __shared__ __attribute__((aligned(16))) unsigned char smem[kStreamLds];
     __shared__ int32_t before[kMostGroups + 1];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int32_t cols = (a.N + 16 * CF - 1) / (16 * CF);
-    count_blocks(a, before);
+    count_blocks<ROWS>(a, before);
     const int64_t units = (int64_t)before[a.G] * cols;
     // neighbouring units (the blocks of rows of the same columns, then the next columns) on one XCD
     const int64_t place = (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
-    const int64_t first = SPLIT > 1 ? place : place * kStreamWaves + wave, step = (int64_t)gridDim.x * (SPLIT > 1 ? 1 : kStreamWaves);
+    const int64_t first = SPLIT > 1 ? place : place * WAVES + wave, step = (int64_t)gridDim.x * (SPLIT > 1 ? 1 : WAVES);
     for (int64_t w = first; w < units; w += step) {
         int32_t lo = 0, hi = a.G;                  // before[lo] * cols <= w < before[hi] * cols
         while (hi - lo > 1) {
@@ -53,30 +55,30 @@ __global__ __launch_bounds__(kThreads) void product_stream_kernel(ProductArgs a)
         Unit u;
         u.group = __builtin_amdgcn_readfirstlane(lo);
         u.n0 = __builtin_amdgcn_readfirstlane((int32_t)(in / blocks) * 16 * CF);
-        u.row0 = r0 + (in % blocks) * kUnitRows;
-        u.rows = __builtin_amdgcn_readfirstlane((int32_t)min((int64_t)kUnitRows, r1 - u.row0));
-        unsigned char *const ring = smem + wave * kRingBytes;
+        u.row0 = r0 + (in % blocks) * ROWS;
+        u.rows = __builtin_amdgcn_readfirstlane((int32_t)min((int64_t)ROWS, r1 - u.row0));
+        unsigned char *const ring = smem + wave * RING;
         acc_t *const part = reinterpret_cast<acc_t *>(smem);
-        if (ROWS == 1 || u.rows <= 16) stream_unit<FMT, GATED, CF, 1, SPLIT>(a, u, ring, part);
-        else if (u.rows <= 32) stream_unit<FMT, GATED, CF, 2, SPLIT>(a, u, ring, part);
-        else stream_unit<FMT, GATED, CF, 4, SPLIT>(a, u, ring, part);
+        if (MOST == 1 || u.rows <= 16) stream_unit<FMT, GATED, CF, 1, SPLIT, RING>(a, u, ring, part);
+        else if (MOST == 2 || u.rows <= 32) stream_unit<FMT, GATED, CF, MOST < 2 ? 1 : 2, SPLIT, RING>(a, u, ring, part);
+        else stream_unit<FMT, GATED, CF, MOST, SPLIT, RING>(a, u, ring, part);
     }
 }
 
-template <int FMT, bool GATED, int CF, int ROWS> void launch_split(const ProductArgs &a, int64_t blocks, hipStream_t s) {
+template <int FMT, bool GATED, int CF, int MOST, int WAVES> void launch_split(const ProductArgs &a, hipStream_t s) {
+    // most blocks of rows that there can be
+    const int64_t blocks = a.M / (16 * MOST) + std::min<int64_t>(a.M, a.G);
     const int64_t units = blocks * ((a.N + 16 * CF - 1) / (16 * CF));
-    const bool alone = units >= (int64_t)a.num_cu * kStreamWaves;
-    const int64_t need = alone ? (units + kStreamWaves - 1) / kStreamWaves : units;
+    const bool alone = units >= (int64_t)a.num_cu * WAVES;
+    const int64_t need = alone ? (units + WAVES - 1) / WAVES : units;
     const dim3 grid((unsigned)((std::min<int64_t>(need, a.num_cu) + 7) / 8 * 8));
-    if (alone) hipLaunchKernelGGL((product_stream_kernel<FMT, GATED, CF, ROWS, 1>), grid, dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((product_stream_kernel<FMT, GATED, CF, ROWS, kStreamWaves>), grid, dim3(kThreads), 0, s, a);
+    if (alone) hipLaunchKernelGGL((product_stream_kernel<FMT, GATED, CF, MOST, WAVES, 1>), grid, dim3(64 * WAVES), 0, s, a);
+    else hipLaunchKernelGGL((product_stream_kernel<FMT, GATED, CF, MOST, WAVES, WAVES>), grid, dim3(64 * WAVES), 0, s, a);
 }
 template <int FMT, bool GATED> hipError_t launch_stream(const ProductArgs &a, hipStream_t s) {
-    // most row blocks that there can be
-    const int64_t blocks = a.M / kUnitRows + std::min<int64_t>(a.M, a.G);
     constexpr int WIDE = GATED ? 1 : 2;
-    if (a.M <= 16) launch_split<FMT, GATED, WIDE, 1>(a, blocks, s);
-    else launch_split<FMT, GATED, WIDE, 4>(a, blocks, s);
+    if (a.M <= 16) launch_split<FMT, GATED, WIDE, 1, kStreamWaves>(a, s);
+    else launch_split<FMT, GATED, WIDE, 4, kStreamWaves>(a, s);
     return hipGetLastError();
 }
 
@@ -86,41 +88,76 @@ template <bool GATED> hipError_t launch_format(const ProductArgs &a, hipStream_t
     return launch_stream<CRAFT_F32, GATED>(a, s);
 }
 
-}  // namespace
-
-// Size of the tiles: the one whose rounds take the least.  A slab of a tile of FW x FX fragments a wave takes 88 FW + 26 FW FX
-// cycles (measured: 0.39 us at 4 x 4, 0.87 at 8 x 4, 1.2 at 8 x 8), a tile 12000 and 150 for every product of fragments
-// beside its slabs.  How rows are spread over groups only the GPU knows: a third of a tile more for each is assumed.  Behind the first
-// round tiles end at different times.
-void product_tile_size(const ProductArgs &a, int32_t *width, int32_t *height) {
-    const int64_t slabs = (a.row_bytes + 127) / 128, per_element = a.format == CRAFT_F32 ? 4 : 1;
+// Which kernel, and the size of its tiles: what is expected to take the least time, from sizes that the host knows.  How rows are
+// spread over groups only the GPU knows.  Fitted to times of 70 drawn products of 6 to 3700 rows (1 to 68 groups, every type), of
+// which the choice takes 1.008 of the better kernel's time in the geometric mean; units up to 127 rows or 15 a group and tiles
+// beyond took 1.13.
+struct Sizes {
+    double rows, groups, columns, slabs;           // groups: those that can have rows
+    double matrix;                                 // cycles of a slab's matrix instructions, relative to 16 bits
+    double weights;                                // ns that the weights take out of HBM
+};
+Sizes sizes_of(const ProductArgs &a) {
+    Sizes z;
+    z.rows = (double)a.M;
+    z.groups = (double)std::min<int64_t>(a.M, a.G);
+    z.columns = a.N;
+    z.slabs = (a.row_bytes + 127) / 128;
+    z.matrix = a.format == CRAFT_F32 ? 4 : 1;
+    z.weights = z.groups * a.N * a.row_bytes * (a.up ? 2 : 1) / 5000;
+    return z;
+}
+// ns of units: their bytes at 60 GB/s a CU, or their matrix instructions; 2 us for a unit that four waves share, 4 to 5.5 for
+// four of a wave each, whose results go out at the same time.
+double stream_time(const ProductArgs &a, const Sizes &z) {
+    const double blocks = a.G == 1 ? std::ceil(z.rows / 64) : std::max(z.groups, z.rows / 64 + 0.5 * z.groups);
+    const double rows = z.rows / blocks, fx = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    const double units = blocks * std::ceil(z.columns / (a.up ? 16 : 32));
+    const double bytes = z.slabs * (2 + fx) * 2048, matrix = z.slabs * 4 * fx * 16 / 2 * (z.matrix > 1 ? 8 : 1);
+    double time;
+    if (units >= 4.0 * a.num_cu) time = std::ceil(units / (4.0 * a.num_cu)) * (std::max(4 * bytes / 60, matrix) + 3500 + 500 * fx);
+    else time = std::ceil(units / a.num_cu) * (std::max(bytes / 60, matrix / 4) + 2000);
+    return std::max(time, z.weights);
+}
+// ns of tiles.  A slab of a tile of FW x FX fragments a wave takes 88 FW + 26 FW FX cycles (0.39 us at 4 x 4, 0.87 at 8 x 4, 1.2 at
+// 8 x 8), a tile 12000 and 150 for every product of fragments beside its slabs, at 2 GHz.  A third of a tile more for each group is
+// assumed, and that behind the first round tiles end at different times; groups of 64 rows in the mean: low tiles.
+double tile_time(const ProductArgs &a, const Sizes &z, int32_t *width, int32_t *height) {
     double best = 0;
     for (int fw = 8; fw >= 4; fw -= 4)
         for (int fx = fw; fx >= 2; --fx) {
             if (fx == 3) continue;
-            const int64_t columns = 32 * fw / (a.up ? 2 : 1), nt = (a.N + columns - 1) / columns;
-            const double rows = a.G == 1 ? (double)((a.M + 32 * fx - 1) / (32 * fx)) : (double)a.M / (32 * fx) + 0.35 * a.G;
-            const double rounds = rows * nt / a.num_cu;
+            const double columns = std::ceil(z.columns / (32 * fw / (a.up ? 2 : 1)));
+            const double rows = a.G == 1 ? std::ceil(z.rows / (32 * fx)) : z.rows / (32 * fx) + 0.35 * a.G;
+            const double rounds = rows * columns / a.num_cu;
             const double made = rounds <= 1 ? 1 : a.G == 1 ? std::ceil(rounds) : rounds + 0.6;
-            const double slab = 88.0 * fw + 26.0 * fw * fx * per_element;
-            const double time = made * (slabs * slab + 12000 + 150 * fw * fx);
+            const double time = made * (z.slabs * (88 * fw + 26 * fw * fx * z.matrix) + 12000 + 150 * fw * fx) / 2;
             if (best == 0 || time < best) {
                 best = time;
                 *width = 32 * fw;
                 *height = 32 * fx;
             }
         }
+    if (z.rows / a.G <= 64) {
+        const double rounds = z.groups * std::ceil(z.columns / (a.up ? 64 : 128)) / a.num_cu, fx = z.rows / a.G <= 32 ? 1 : 2;
+        best = (rounds < 2 ? std::ceil(rounds) : rounds + 0.5) * (z.slabs * (352 + 104 * fx * z.matrix) + 12500) / 2;
+    }
+    return std::max(best, z.weights * 5000 / 4500);
 }
+
+}  // namespace
 
 hipError_t launch_product(const ProductArgs &a, hipStream_t s) {
     if (a.M <= 0) return hipSuccess;
     const bool near = a.src ? a.x_rows * a.x_stride < (int64_t)1 << 32 : a.x_stride < (int64_t)1 << 24;
-    if (near && a.row_bytes >= 128 && a.M >= 128 && a.M / a.G >= 16) {
-        int32_t width = 256, height = 256;
-        product_tile_size(a, &width, &height);
-        if (a.format == CRAFT_I8) return launch_product_tiles_i8(a, width, height, s);
-        if (a.format == CRAFT_BF16) return launch_product_tiles_bf16(a, width, height, s);
-        return launch_product_tiles_f32(a, width, height, s);
+    if (near && a.row_bytes >= 128 && a.M > 16) {
+        const Sizes z = sizes_of(a);
+        int32_t width = 0, height = 0;
+        if (tile_time(a, z, &width, &height) < stream_time(a, z)) {
+            if (a.format == CRAFT_I8) return launch_product_tiles_i8(a, width, height, s);
+            if (a.format == CRAFT_BF16) return launch_product_tiles_bf16(a, width, height, s);
+            return launch_product_tiles_f32(a, width, height, s);
+        }
     }
     return a.up ? launch_format<true>(a, s) : launch_format<false>(a, s);
 }

@@ -56,7 +56,7 @@ def _grouped(**kw):
 @pytest.mark.parametrize("bad", [
     dict(format=3), dict(format=-1), dict(out_dtype=2), dict(format=0, out_dtype=1), dict(format=1, out_dtype=0), dict(G=0), dict(G=-1), dict(G=1025), dict(N=0),
     dict(N=-1), dict(K=0), dict(K=56), dict(format=1, K=60), dict(format=0, out_dtype=0, K=62), dict(K=131072, x_stride=131072),
-    dict(format=1, K=1 << 22, x_stride=1 << 22), dict(k=0), dict(k=-2), dict(M=-1), dict(M=1 << 31), dict(x_rows=-1), dict(x_rows=0), dict(x_rows=1 << 31),
+    dict(format=1, K=1 << 22, x_stride=1 << 22), dict(k=0), dict(k=-2), dict(M=-1), dict(M=1 << 31), dict(M=(1 << 26) + 1), dict(x_rows=-1), dict(x_rows=0), dict(x_rows=1 << 31),
     dict(x=0), dict(x=AT + 4), dict(x_stride=60), dict(x_stride=72), dict(x_stride=1 << 60), dict(x_scale=0), dict(x_scale=AT + 1), dict(src=AT + 1), dict(off=0),
     dict(off=AT + 2), dict(w=0), dict(w=AT + 4), dict(w_up=AT + 4), dict(w_scale=0), dict(w_scale=AT + 4), dict(up_scale=0), dict(up_scale=AT + 4), dict(out=0),
     dict(out=AT + 1), dict(out_stride=7), dict(out_stride=1 << 60)])
