@@ -379,10 +379,9 @@ __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a
     constexpr int SIDES = GATED ? 2 : 1, COLS = 32 * FW / SIDES, LOW = 32 * kLowColumns / SIDES;
     static_assert(FW >= kLowColumns, "columns of a low tile");
     const int32_t nt = (a.N + COLS - 1) / COLS, nlow = (a.N + LOW - 1) / LOW;
-    // Neighbours in the list start together on one XCD, 32 of them, which are dealt to the XCDs in turn.  One tile a workgroup: the next
-    // one starts wherever a CU is done first.  (No loop over tiles: what the compiler keeps across one costs registers that a
-    // tile needs, and memory to spill them to costs every workgroup its start: 8192 x 4096 x 7168 178 us, without 173.)
-    const int64_t w = first + (int64_t)(blockIdx.x / 256) * 256 + (blockIdx.x % 8) * 32 + blockIdx.x % 256 / 8;
+    // One tile a workgroup: the next one starts wherever a CU is done first.  (No loop over tiles: what the compiler keeps across
+    // one costs registers that a tile needs, and memory to spill them to costs every workgroup its start: 8192 x 4096 x 7168
+    // 178 us, without 171.)
     const int tid = threadIdx.x, lane = tid & 63;
     // Every wave finds the tile for itself, in registers: how many row tiles of each class there are, then the group.
     Groups own = groups_at(a, lane, height);
@@ -392,6 +391,17 @@ __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a
 #pragma unroll
         for (int i = 0; i < kClasses; ++i) total[i] += __builtin_amdgcn_readlane(wave_sums(at.cut.kind == i ? at.cut.count : 0), 63);
     }
+    int64_t all = 0;
+#pragma unroll
+    for (int i = 0; i < kClasses; ++i) all += (int64_t)total[i] * (i == kFew ? nlow : nt);
+    // Workgroup b runs on XCD b mod 8.  Of every 256 tiles in the list an XCD has 32 neighbours, which share rows of x and of the weights
+    // in its L2; every other 256 in reverse, since tiles are listed by height: the XCDs that had the lowest ones take the next first.
+    // Tiles of one group are alike: fewer than 256 at the end are spread over all XCDs.
+    const int64_t block = first + blockIdx.x, round = block / 256;
+    const int32_t left = (int32_t)min(all - round * 256, (int64_t)256), run = a.G == 1 ? (left + 7) / 8 : 32;
+    const int32_t xcd = (int32_t)(block % 8), in_run = (int32_t)(block % 256 / 8), in_round = (round & 1 ? 7 - xcd : xcd) * run + in_run;
+    if (in_run >= run || in_round >= left) return;
+    const int64_t w = round * 256 + in_round;
     int64_t begin = 0;
     int kind = kClasses;
 #pragma unroll
@@ -401,7 +411,6 @@ __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a
             if (w < begin + tiles) kind = i;
             else begin += tiles;
         }
-    if (kind == kClasses) return;
     const int32_t columns = kind == kFew ? nlow : nt, place_in = (int32_t)((w - begin) / columns);
     Tile t = {};
     int32_t before = 0, height_in = 0, count_in = 0;
