@@ -106,14 +106,20 @@ static __device__ __forceinline__ void group_rows(const ProductArgs &a, int32_t 
 template <int DPP, int ROWS> static __device__ __forceinline__ int32_t lane_before(int32_t x) {
     return __builtin_amdgcn_update_dpp(0, x, DPP, ROWS, 0xf, false);
 }
-static __device__ __forceinline__ int32_t wave_sums(int32_t x) {
-    x += lane_before<0x111, 0xf>(x);               // one, two, four, eight lanes up a row of 16
-    x += lane_before<0x112, 0xf>(x);
-    x += lane_before<0x114, 0xf>(x);
-    x += lane_before<0x118, 0xf>(x);
-    x += lane_before<0x142, 0xa>(x);               // a row's last lane into the next row, the second one's into the upper half
-    x += lane_before<0x143, 0xc>(x);
-    return x;
+// Several at a time: an instruction across lanes reads what was written two instructions earlier at the soonest.
+template <int N> static __device__ __forceinline__ void wave_sums(int32_t (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += lane_before<0x111, 0xf>(x[i]);     // one, two, four, eight lanes up a row of 16
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += lane_before<0x112, 0xf>(x[i]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += lane_before<0x114, 0xf>(x[i]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += lane_before<0x118, 0xf>(x[i]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += lane_before<0x142, 0xa>(x[i]);     // a row's last lane into the next row, the second one's
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += lane_before<0x143, 0xc>(x[i]);     // into the upper half
 }
 
 }  // namespace craft

@@ -20,9 +20,10 @@ template <int ROWS> static __device__ __forceinline__ void count_blocks(const Pr
         const int32_t g = g0 + lane;
         int64_t lo = 0, hi = 0;
         if (g < a.G) group_rows(a, g, lo, hi);
-        const int32_t n = sum + wave_sums((int32_t)((hi - lo + ROWS - 1) / ROWS));
-        if (g < a.G) before[g + 1] = n;
-        sum = __builtin_amdgcn_readlane(n, 63);
+        int32_t n[1] = {(int32_t)((hi - lo + ROWS - 1) / ROWS)};
+        wave_sums(n);
+        if (g < a.G) before[g + 1] = sum + n[0];
+        sum += __builtin_amdgcn_readlane(n[0], 63);
     }
     before[0] = 0;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");

@@ -346,8 +346,8 @@ struct Cut {
 };
 static __device__ __forceinline__ Cut cut_rows(int32_t rows, int32_t most) {
     if (rows <= kFewRows) return {kFew, kFewRows, rows > 0};
-    const int32_t tiles = (rows + most - 1) / most, height = ((rows + tiles - 1) / tiles + 31) / 32 * 32;
-    return {height > 192 ? 0 : height > 128 ? 1 : 2, height, (rows + height - 1) / height};
+    const uint32_t r = (uint32_t)rows, m = (uint32_t)most, tiles = (r + m - 1) / m, height = ((r + tiles - 1) / tiles + 31) / 32 * 32;
+    return {height > 192 ? 0 : height > 128 ? 1 : 2, (int32_t)height, (int32_t)((r + height - 1) / height)};
 }
 // 64 groups, one a lane: their rows and how they are cut.
 struct Groups {
@@ -366,11 +366,11 @@ static __device__ __forceinline__ int64_t lane_value(int64_t v, int lane) {
 
 // Item i of a group's m x nt tiles: blocks of 8 x 8, column by column inside a block, so that the tiles that run at one
 // time need few rows of either operand between them.
-static __device__ __forceinline__ void place(int32_t i, int32_t m, int32_t nt, int32_t &row, int32_t &col) {
-    const int32_t band = i / (8 * nt), r0 = band * 8, rj = min(8, m - r0), in = i - r0 * nt;
-    const int32_t block = in / (rj * 8), rest = in - block * rj * 8;
-    row = r0 + rest % rj;
-    col = block * 8 + rest / rj;
+static __device__ __forceinline__ void place(uint32_t i, uint32_t m, uint32_t nt, int32_t &row, int32_t &col) {
+    const uint32_t band = i / (8 * nt), r0 = band * 8, rj = min(8u, m - r0), in = i - r0 * nt;
+    const uint32_t block = in / (rj * 8), rest = in - block * rj * 8, across = rest / rj;
+    row = (int32_t)(r0 + rest - across * rj);
+    col = (int32_t)(block * 8 + across);
 }
 
 template <int FMT, bool GATED, int FW>
@@ -384,12 +384,15 @@ __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a
     // 178 us, without 171.)
     const int tid = threadIdx.x, lane = tid & 63;
     // Every wave finds the tile for itself, in registers: how many row tiles of each class there are, then the group.
-    Groups own = groups_at(a, lane, height);
-    int32_t total[kClasses] = {};
+    Groups own = {};
+    int32_t sums[kClasses] = {}, total[kClasses] = {};
     for (int32_t g0 = 0; g0 < a.G; g0 += 64) {
-        const Groups at = a.G <= 64 ? own : groups_at(a, g0 + lane, height);
+        own = groups_at(a, g0 + lane, height);
 #pragma unroll
-        for (int i = 0; i < kClasses; ++i) total[i] += __builtin_amdgcn_readlane(wave_sums(at.cut.kind == i ? at.cut.count : 0), 63);
+        for (int i = 0; i < kClasses; ++i) sums[i] = own.cut.kind == i ? own.cut.count : 0;
+        wave_sums(sums);
+#pragma unroll
+        for (int i = 0; i < kClasses; ++i) total[i] += __builtin_amdgcn_readlane(sums[i], 63);
     }
     int64_t all = 0;
 #pragma unroll
@@ -411,28 +414,40 @@ __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a
             if (w < begin + tiles) kind = i;
             else begin += tiles;
         }
-    const int32_t columns = kind == kFew ? nlow : nt, place_in = (int32_t)((w - begin) / columns);
+    const uint32_t columns = (uint32_t)(kind == kFew ? nlow : nt);
+    const int64_t in_class = w - begin;
+    // (a list of 2^32 tiles and more is one that nobody waits for)
+    const int32_t place_in = in_class >> 32 ? (int32_t)(in_class / columns) : (int32_t)((uint32_t)in_class / columns);
     Tile t = {};
     int32_t before = 0, height_in = 0, count_in = 0;
     int64_t lo = 0, hi = 0;
-    for (int32_t g0 = 0, run = 0;; g0 += 64) {
-        if (a.G > 64) own = groups_at(a, g0 + lane, height);
-        const int32_t mine = own.cut.kind == kind ? own.cut.count : 0, upto = run + wave_sums(mine);
-        const uint64_t behind = __ballot(upto > place_in);
+    for (int32_t g0 = 0, run_up = 0;; g0 += 64) {
+        int32_t upto[1] = {0};
+        if (a.G > 64) {
+            own = groups_at(a, g0 + lane, height);
+            upto[0] = own.cut.kind == kind ? own.cut.count : 0;
+            wave_sums(upto);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kClasses; ++i)
+                if (kind == i) upto[0] = sums[i];
+        }
+        upto[0] += run_up;
+        const uint64_t behind = __ballot(upto[0] > place_in);
         if (behind) {
             const int at = __builtin_ctzll(behind);
             t.group = g0 + at;
-            before = __builtin_amdgcn_readlane(upto - mine, at);
             height_in = __builtin_amdgcn_readlane(own.cut.height, at);
             count_in = __builtin_amdgcn_readlane(own.cut.count, at);
+            before = __builtin_amdgcn_readlane(upto[0], at) - count_in;
             lo = lane_value(own.lo, at);
             hi = lane_value(own.hi, at);
             break;
         }
-        run = __builtin_amdgcn_readlane(upto, 63);
+        run_up = __builtin_amdgcn_readlane(upto[0], 63);
     }
     int32_t tr, tc;
-    place((int32_t)(w - begin - (int64_t)before * columns), count_in, columns, tr, tc);
+    place((uint32_t)(in_class - (int64_t)before * columns), (uint32_t)count_in, columns, tr, tc);
     t.row0 = lo + (int64_t)tr * height_in;
     t.rows = (int32_t)min((int64_t)height_in, hi - t.row0);
     t.n0 = tc * (kind == kFew ? LOW : COLS);
