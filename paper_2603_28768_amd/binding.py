@@ -773,7 +773,7 @@ class GroupedMatmul:
         a.G, a.N, a.K = self.G, self.N, self.K
         a.w, a.w_up = pointers(weights, first.shape, first.dtype), pointers(up, first.shape, first.dtype)
         a.w_scale, a.up_scale = scale_pointers(scales), scale_pointers(up_scales)
-        self.args, self._ref, self._call = a, ctypes.byref(a), lib().craft_grouped_matmul
+        self._args, self._call = a, lib().craft_grouped_matmul
         self._int32, self._float32 = torch.int32, torch.float32
 
     def __call__(self, x, off, x_scale=None, src=None, k: int = 1, out=None, stream=None):
@@ -781,7 +781,8 @@ class GroupedMatmul:
         g's products are rows off[g] .. off[g + 1]; src: int32 [M], product p then takes row src[p] // k of x.  Returns
         [M][N], new or written into `out`; rows of no group are left as they were (a new result: anything)."""
         import torch
-        a, gpu = self.args, self._gpu
+        # a copy: calls of several threads do not share their arguments
+        a, gpu = GroupedMatmulArgs.from_buffer_copy(self._args), self._gpu
         assert x.dim() == 2 and off.dtype == self._int32 and off.get_device() == gpu and off.shape == (self.G + 1,) and off.is_contiguous()
         rows = x.shape[0]
         stride = _matrix(x, rows, self.K, gpu, self.dtype)
@@ -799,7 +800,7 @@ class GroupedMatmul:
         a.x_scale = None if x_scale is None else x_scale.data_ptr()
         a.src = None if src is None else src.data_ptr()
         a.out, a.out_stride = out.data_ptr(), _matrix(out, M, self.N, gpu, self.out_dtype)
-        rc = self._call(self._ref, _stream_on(gpu, stream))
+        rc = self._call(ctypes.byref(a), _stream_on(gpu, stream))
         if rc:
             _check(rc, "craft_grouped_matmul")
         return out

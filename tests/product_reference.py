@@ -38,7 +38,8 @@ def _rounded(x: np.ndarray, dtype) -> torch.Tensor:
 def product(x, w, xs=None, ws=None):
     """One group's product.  int8: (fp32 result, None); otherwise (float64 result, bound of its fp32 sums)."""
     if x.dtype == np.int8:
-        acc = x.astype(np.int64) @ w.astype(np.int64).T
+        # whole numbers below 2^53: exact in float64, whatever the order
+        acc = (x.astype(np.float64) @ w.astype(np.float64).T).astype(np.int64)
         with np.errstate(over="ignore", invalid="ignore"):
             return acc.astype(np.float32) * xs[:, None] * ws[None, :], None
     x, w = x.astype(np.float64), w.astype(np.float64)

@@ -233,6 +233,71 @@ def test_grouped_drawn_values(torch_cuda, fmt, out, is_gated, sizes, N, K, pad, 
     p.check(p.run())
 
 
+# a tile of every height, the lowest ones of groups with few rows among them; the sum is about one round of tiles
+HEIGHTS = [256, 200, 180, 150, 100, 70, 64, 33, 20, 5, 0, 512, 700, 900, 110]
+
+
+@pytest.mark.parametrize("fmt,out", [("i8", "bf16"), ("i8", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("is_gated,N", [(False, 4096 + 5), (True, 2048 - 3)])
+@pytest.mark.parametrize("K", [128, 592])
+def test_tiles_of_every_height(torch_cuda, fmt, out, is_gated, N, K):
+    print(f"heights {fmt} {out} gated={is_gated} N={N} K={K}", flush=True)
+    p = Problem(N + K, fmt, HEIGHTS, N, K, is_gated, out=out, k=2, front=3, spare=7, whole=not is_gated, pad=16, out_pad=3)
+    p.exact = True
+    p.src[5::37] = -1
+    p.src[6::41] = p.x.shape[0] * 2
+    p.d_src = _dev(p.src)
+    p.check(p.run())
+
+
+@pytest.mark.parametrize("M,N,K", [(5121, 2048, 256), (2689, 4000, 144), (777, 4096, 1040), (1345, 1100, 2048), (641, 8192, 400), (400, 2500, 3000 // 16 * 16)])
+def test_matmul_in_tiles(torch_cuda, M, N, K):
+    # last tiles of one row, of half a fragment; rows that end inside a slab
+    torch = torch_cuda
+    print(f"matmul tiles {M}x{N}x{K}", flush=True)
+    g = np.random.default_rng(M)
+    (x, xs), (w, ws) = _codes(g, M, K), _codes(g, N, K)
+    got = binding.matmul_i8(_dev(x), _dev(xs), _dev(w), _dev(ws), dtype="bf16")
+    assert torch.equal(got, _dev(ref.product(x, w, xs, ws)[0]).bfloat16())
+
+
+@pytest.mark.parametrize("fmt", ["i8", "bf16", "f32"])
+@pytest.mark.parametrize("G,most", [(70, 90), (200, 30), (1024, 9), (130, 300)])
+def test_many_groups(torch_cuda, fmt, G, most):
+    # more groups than a wave has lanes, in tiles and in units
+    g = np.random.default_rng(G)
+    sizes = g.integers(0, most, G).tolist()
+    K = 64 if fmt == "f32" else 128
+    for N in (40, 520 if G < 1000 else 72):
+        print(f"many groups {fmt} G={G} most={most} N={N}", flush=True)
+        p = Problem(G, fmt, sizes, N, K, False, out="bf16", whole=True, spare=1)
+        p.exact = True
+        p.check(p.run())
+
+
+@pytest.mark.parametrize("fmt", ["i8", "bf16"])
+def test_rows_behind_an_offset_of_32_bits(torch_cuda, fmt):
+    """Rows of x further from its start than 32 bits of bytes, in order and through a permutation: strides far beyond the rows."""
+    torch = torch_cuda
+    K, rows, N = 256, 300, 48
+    kind = torch.int8 if fmt == "i8" else torch.bfloat16
+    stride = (16 << 20) + 256 if fmt == "i8" else (8 << 20) + 128          # elements: a row every 16 MiB
+    room = torch.empty(rows * stride, dtype=kind, device=DEV)
+    x = room.as_strided((rows, K), (stride, 1))
+    g = np.random.default_rng(1)
+    x.copy_(_dev(g.integers(-8, 9, (rows, K)).astype(np.float32)).to(kind))
+    w = _dev(g.integers(-8, 9, (2, N, K)).astype(np.float32)).to(kind)
+    one = lambda *s: torch.ones(s, device=DEV) if fmt == "i8" else None  # noqa: E731
+    op = binding.GroupedMatmul(w, scales=one(2, N))
+    off = torch.tensor([0, 200, 300], dtype=torch.int32, device=DEV)
+    want = torch.cat([x[:200].float() @ w[0].float().T, x[200:].float() @ w[1].float().T]).bfloat16()
+    assert torch.equal(op(x, off, x_scale=one(rows)), want)
+    src = torch.arange(rows - 1, -1, -1, dtype=torch.int32, device=DEV)
+    back = x.flip(0).float()
+    want = torch.cat([back[:200] @ w[0].float().T, back[200:] @ w[1].float().T]).bfloat16()
+    assert torch.equal(op(x, off, x_scale=one(rows), src=src), want)
+
+
 @pytest.mark.parametrize("fmt", ["i8", "bf16", "f32"])
 @pytest.mark.parametrize("off", [[5, 2, 9, 9], [-4, 30, 20, 1000], [40, 60, 80, 33], [90, 95, 95, 2000000000], [-2000000000, 0, 0, 0]])
 def test_offsets_that_are_none_stay_inside(torch_cuda, fmt, off):
@@ -261,18 +326,18 @@ def test_places_that_name_no_row_are_zeros(torch_cuda, fmt, is_gated, rows):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "f32"])
-@pytest.mark.parametrize("rows", [9, 300])
-def test_infinities_and_nan_stay_in_their_rows(torch_cuda, fmt, rows):
+@pytest.mark.parametrize("rows,N", [(9, 90), (300, 90), (1500, 2100)])
+def test_infinities_and_nan_stay_in_their_rows(torch_cuda, fmt, rows, N):
     # the last pieces of rows that end inside a slab: what is read in place of the rest may hold anything
     torch = torch_cuda
     K = 208 if fmt == "bf16" else 100
-    p = Problem(11, fmt, [rows, 40], 90, K, False, whole=True)
+    p = Problem(11, fmt, [rows, 40 + rows // 2], N, K, False, whole=True)
     x = p.d_x.clone().abs() + 1
     w = p.d_w.clone().abs() + 1
     x[2, K - 1], x[rows + 5, K - 8], x[4, 0] = float("inf"), float("nan"), float("-inf")
     w[1, 7, K - 1] = float("inf")
     got = binding.GroupedMatmul(w)(x, p.d_off).float().cpu()
-    want = torch.full((p.M, 90), 0.0)
+    want = torch.full((p.M, N), 0.0)
     want[2], want[4], want[rows + 5] = float("inf"), float("-inf"), float("nan")
     want[rows:, 7] = float("inf")
     want[rows + 5] = float("nan")
