@@ -743,36 +743,27 @@ class GroupedMatmul:
         assert dtype is None or eight or dtype == natural, "only 8-bit products have a choice of result"
         self.dtype, self.out_dtype = first.dtype, _torch_dtype(dtype or natural)
         assert (scales is not None) == eight and (up_scales is not None) == (eight and up is not None)
-        self._keep = []
-
-        def pointers(items, shape, kind):
-            if items is None:
-                return None
-            items = list(items)
-            assert len(items) == self.G
-            for t in items:
-                assert t.dtype == kind and t.get_device() == self._gpu and t.shape == shape and t.is_contiguous() and t.data_ptr() % 16 == 0
-            table = torch.tensor([t.data_ptr() for t in items], dtype=torch.int64, device=dev)
-            self._keep += [items, table]
-            return table.data_ptr()
-
-        def scale_pointers(items):
-            # (a row of an odd [G][N] need not be 16-byte aligned)
-            if items is None:
-                return None
-            items = list(items)
-            assert len(items) == self.G
-            for t in items:
-                assert t.dtype == torch.float32 and t.get_device() == self._gpu and t.shape == (self.N,) and t.is_contiguous()
-            table = torch.tensor([t.data_ptr() for t in items], dtype=torch.int64, device=dev)
-            self._keep += [items, table]
-            return table.data_ptr()
+        # four tables of addresses in one tensor; a scale row of an odd [G][N] need not be 16-byte aligned
+        kinds = ((weights, first.shape, first.dtype, 16), (up, first.shape, first.dtype, 16),
+                 (scales, (self.N,), torch.float32, 4), (up_scales, (self.N,), torch.float32, 4))
+        self._keep, addresses = [], []
+        for items, shape, kind, alignment in kinds:
+            items = None if items is None else list(items)
+            assert items is None or len(items) == self.G
+            for t in items or ():
+                assert t.dtype == kind and t.get_device() == self._gpu and t.shape == shape and t.is_contiguous() and t.data_ptr() % alignment == 0
+            self._keep.append(items)
+            addresses += [t.data_ptr() for t in items] if items else []
+        self._table = torch.tensor(addresses, dtype=torch.int64, device=dev)
+        places, at = [], self._table.data_ptr()
+        for items in self._keep:
+            places.append(at if items else None)
+            at += 8 * self.G if items else 0
 
         a = GroupedMatmulArgs()
         a.format, a.out_dtype = formats[first.dtype], CRAFT_BF16 if self.out_dtype == torch.bfloat16 else CRAFT_F32
         a.G, a.N, a.K = self.G, self.N, self.K
-        a.w, a.w_up = pointers(weights, first.shape, first.dtype), pointers(up, first.shape, first.dtype)
-        a.w_scale, a.up_scale = scale_pointers(scales), scale_pointers(up_scales)
+        a.w, a.w_up, a.w_scale, a.up_scale = places
         self._args, self._call = a, lib().craft_grouped_matmul
         self._int32, self._float32 = torch.int32, torch.float32
 
