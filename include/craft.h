@@ -574,7 +574,7 @@ craft_status craft_matmul_i8(int64_t M, int32_t N, int32_t K, const int8_t *x, i
  *   M          places of out (and of x or src): off[G] <= M.  Places behind off[G] are left as they
  *              were, and so are those in front of off[0].  Offsets outside [0, M] count as the nearer
  *              end, a group that ends before it begins has no rows; groups that overlap leave any of
- *              their results
+ *              their results in the rows they share
  *   x          DEVICE [M][K], or [x_rows][K] with src; a row every x_stride elements, rows 16-byte
  *              aligned
  *   src        DEVICE [M] int32, optional; a place whose row is outside [0, x_rows) gets zeros.
@@ -585,7 +585,9 @@ craft_status craft_matmul_i8(int64_t M, int32_t N, int32_t K, const int8_t *x, i
  *   w_scale, up_scale  DEVICE arrays of G device pointers to [N] fp32, CRAFT_I8 only
  *   out        DEVICE [M][N], a row every out_stride elements; must not overlap x
  * Which rows a group has is read on the GPU: a recorded call follows the offsets of each replay.  The
- * result depends on the arguments only, never on scheduling.
+ * result depends on the arguments and the GPU's number of compute units only, never on scheduling.  Sums
+ * in fp32 are added in an order that follows the sizes: a row's result can differ in its last bits
+ * between calls of other M or G.
  * Limits: G <= 1024;  rows of x and w are whole multiples of 16 bytes, shorter than 8 MiB;
  * K < 131072 for CRAFT_I8;  N <= 2^30;  M <= 2^26, may be 0;  x_rows < 2^31. */
 typedef struct {

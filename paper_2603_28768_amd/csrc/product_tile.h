@@ -5,9 +5,9 @@
 // lines: a CU gets 123 GB/s that way, and 38 where lanes load operand fragments of row-major weights themselves (16 rows a
 // request; the same tile 265 us so, 8192 x 4096 x 7168).  An LDS row is unpadded, its eight 16-byte pieces in the order piece ^
 // (row & 7), so that the reads of a fragment hit every bank once.  A slab is two steps of 64 bytes.  While one step is multiplied,
-// all fragments of the next are read into the other set of registers: behind the first step of a slab its stage
-// is free again, and the slab that takes its place is requested at once.  Every memory instruction is dealt out behind a matrix
-// instruction of its own.
+// all fragments of the next are read into the other set of registers: behind the first step of a slab its stages are free
+// again.  x of the slab that takes its place is requested in the second step, its weights in the first step of the next slab.
+// Every memory instruction is dealt out behind a matrix instruction of its own.
 //
 // A group's rows are shared evenly among as few tiles of at most `height` rows as hold them, in whole fragments of 32.  Groups of up
 // to 64 rows, which stream their weights through one CU at what that gets out of HBM, have tiles of 128 weight rows with up to six stages.
