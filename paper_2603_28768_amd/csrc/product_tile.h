@@ -373,8 +373,50 @@ static __device__ __forceinline__ void place(uint32_t i, uint32_t m, uint32_t nt
     col = (int32_t)(block * 8 + across);
 }
 
+// Every step-th tile from `first` on, of a list without classes: 64 rows, 32 kLowColumns columns.  A loop costs little with the
+// registers that such tiles need, and what they take is not what counts here.  The arguments, the kernel's first, are read
+// anew for every tile: kept, they would take scalar registers from the other tiles' path too.
+template <int FMT, bool GATED>
+static __device__ __forceinline__ void overlapping_tiles(unsigned char *smem, int tid, int64_t first, int64_t step) {
+    constexpr int LOW = 32 * kLowColumns / (GATED ? 2 : 1);
+    for (int64_t w = first;; w += step) {
+        auto args = __builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(args));
+        const ProductArgs a = *(const ProductArgs *)args;
+        const int32_t nlow = (a.N + LOW - 1) / LOW, lane = tid & 63;
+        const int64_t place_in = w / nlow;
+        Tile t = {};
+        int64_t behind_last = 0;
+        int32_t run_up = 0;
+        bool found = false;
+        for (int32_t g0 = 0; g0 < a.G && !found; g0 += 64) {
+            const int32_t g = g0 + lane;
+            int64_t lo = 0, hi = 0;
+            if (g < a.G) group_rows(a, g, lo, hi);
+            const int32_t count = (int32_t)((hi - lo + kFewRows - 1) / kFewRows);
+            int32_t upto[1] = {count};
+            wave_sums(upto);
+            upto[0] += run_up;
+            const uint64_t behind = __ballot(upto[0] > place_in);
+            if (behind) {
+                const int at = __builtin_ctzll(behind);
+                t.group = g0 + at;
+                t.row0 = lane_value(lo, at) + (place_in - __builtin_amdgcn_readlane(upto[0] - count, at)) * kFewRows;
+                behind_last = lane_value(hi, at);
+                found = true;
+            }
+            run_up = __builtin_amdgcn_readlane(upto[0], 63);
+        }
+        if (!found) return;
+        t.rows = (int32_t)min(behind_last - t.row0, (int64_t)kFewRows);
+        t.n0 = (int32_t)(w % nlow) * LOW;
+        product_tile<FMT, GATED, kLowColumns, kFewRows / 32>(a, t, smem, tid);
+        __syncthreads();                           // every wave's results have left LDS
+    }
+}
+
 template <int FMT, bool GATED, int FW>
-__global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a, int32_t height, int64_t first) {
+__global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a, int32_t height, int64_t first, int64_t launched) {
     __shared__ __attribute__((aligned(16))) unsigned char smem[kTileLds];
     constexpr int SIDES = GATED ? 2 : 1, COLS = 32 * FW / SIDES, LOW = 32 * kLowColumns / SIDES;
     static_assert(FW >= kLowColumns, "columns of a low tile");
@@ -401,6 +443,11 @@ __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a
     // in its L2; every other 256 in reverse, since tiles are listed by height: the XCDs that had the lowest ones take the next first.
     // Tiles of one group are alike: fewer than 256 at the end are spread over all XCDs.
     const int64_t block = first + blockIdx.x, round = block / 256;
+    // Only groups that overlap, where offsets fall, can have more tiles than there are workgroups in all launches.
+    if (__builtin_expect(all > launched, 0)) {
+        overlapping_tiles<FMT, GATED>(smem, tid, block, launched);
+        return;
+    }
     const int32_t left = (int32_t)min(all - round * 256, (int64_t)256), run = a.G == 1 ? (left + 7) / 8 : 32;
     const int32_t xcd = (int32_t)(block % 8), in_run = (int32_t)(block % 256 / 8), in_round = (round & 1 ? 7 - xcd : xcd) * run + in_run;
     if (in_run >= run || in_round >= left) return;
@@ -470,12 +517,13 @@ __global__ __launch_bounds__(kThreads, 1) void product_tile_kernel(ProductArgs a
 template <int FMT, bool GATED, int FW> hipError_t launch_width(const ProductArgs &a, int32_t height, hipStream_t s) {
     constexpr int SIDES = GATED ? 2 : 1, COLS = 32 * FW / SIDES, LOW = 32 * kLowColumns / SIDES;
     const int64_t nt = (a.N + COLS - 1) / COLS, nlow = (a.N + LOW - 1) / LOW;
-    // Most tiles that there can be.  (Heights round up to whole fragments: that leaves out tiles, never adds one.)
+    // Most tiles that groups without common rows can have.  (Heights round up to whole fragments: that leaves out tiles, never adds one.)
     const int64_t tiles = (a.M / height + std::min<int64_t>(a.M / (kFewRows + 1), a.G)) * nt + std::min<int64_t>(a.M, a.G) * nlow;
+    const int64_t launched = (tiles + 255) / 256 * 256;
     constexpr int64_t MOST = 1 << 22;              // workgroups of a launch, which has fewer than 2^32 threads
     for (int64_t first = 0; first < tiles; first += MOST) {
         const int64_t grid = (std::min(tiles - first, MOST) + 255) / 256 * 256;
-        hipLaunchKernelGGL((product_tile_kernel<FMT, GATED, FW>), dim3((unsigned)grid), dim3(kThreads), 0, s, a, height, first);
+        hipLaunchKernelGGL((product_tile_kernel<FMT, GATED, FW>), dim3((unsigned)grid), dim3(kThreads), 0, s, a, height, first, launched);
     }
     return hipGetLastError();
 }

@@ -312,6 +312,38 @@ def test_offsets_that_are_none_stay_inside(torch_cuda, fmt, off):
         p.check(got, off)
 
 
+# (rows, columns, offsets): far more rows in all the groups than there are places, tall tiles, few rows and more groups than a
+# wave has lanes among them; every last group has rows of its own
+FALLING = [(8192, 2048, [0, 4096] * 7 + [0, 8192]), (5000, 2050, [500, 4900] * 4 + [0, 40]), (9000, 1030, [300, 8800] * 50 + [0, 9000])]
+
+
+@pytest.mark.parametrize("fmt", ["i8", "bf16", "f32"])
+@pytest.mark.parametrize("is_gated", [False, True])
+@pytest.mark.parametrize("which", range(len(FALLING)))
+def test_groups_that_overlap_lose_no_rows(torch_cuda, fmt, is_gated, which):
+    """Rows that several groups have get any of their results, rows of one group its own."""
+    torch = torch_cuda
+    M, N, off = FALLING[which]
+    G = len(off) - 1
+    print(f"overlap {fmt} gated={is_gated} M={M} N={N} G={G}", flush=True)
+    p = Problem(31, fmt, [0] * (G - 1) + [M], N, 64 if fmt == "f32" else 256, is_gated, whole=True, out="bf16")
+    p.exact = True
+    off = np.asarray(off, np.int32)
+    got = p.handle(p.d_x, _dev(off), x_scale=p.d_xs, out=p.out).clone()
+    fits = torch.zeros((M, N), dtype=torch.bool, device=DEV)
+    covered = np.zeros(M, bool)
+    for g, lo, hi in ref.rows_of(None, off, M):
+        covered[lo:hi] = True
+        alone = np.asarray([lo] * (g + 1) + [hi] * (G - g), np.int32)
+        one = p.handle(p.d_x, _dev(alone), x_scale=p.d_xs, out=p.out.fill_(-7.0))
+        fits[lo:hi] |= one[lo:hi] == got[lo:hi]
+    p.check(one, alone)                            # the last group
+    rows = torch.from_numpy(covered).to(DEV)
+    lost = (rows & ~fits.all(dim=1)).nonzero().flatten().tolist()
+    assert not lost, (len(lost), lost[0], lost[-1])
+    assert bool((got[~rows] == -7.0).all())
+
+
 @pytest.mark.parametrize("fmt", ["i8", "bf16", "f32"])
 @pytest.mark.parametrize("is_gated", [False, True])
 @pytest.mark.parametrize("rows", [20, 300])
