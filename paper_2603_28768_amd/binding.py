@@ -673,6 +673,9 @@ class DecodeAttention:
 
 # ---------------------------------------------- 8-bit integers, products by expert
 
+_INTS = 1 << 31            # ctypes passes the lower half of a larger number on
+
+
 def _matrix(t, rows, row_elements, gpu, dtype):
     """Checks a cuda matrix with contiguous rows; the elements between its rows."""
     assert t.dtype == dtype and t.get_device() == gpu and t.shape == (rows, row_elements)
@@ -687,6 +690,7 @@ def quantize_i8(x, codes=None, scale=None, stream=None):
     import torch
     assert x.is_cuda and x.dim() == 2 and x.dtype in (torch.float32, torch.bfloat16)
     rows, K = x.shape
+    assert K < _INTS, "sizes beyond 32 bits"
     gpu = x.get_device()
     stride = _matrix(x, rows, K, gpu, x.dtype)
     if codes is None:
@@ -708,6 +712,7 @@ def matmul_i8(x, x_scale, w, w_scale, dtype: str = "bf16", out=None, stream=None
     import torch
     assert x.is_cuda and x.dim() == 2 and w.dim() == 2
     (M, K), N, gpu = x.shape, w.shape[0], x.get_device()
+    assert N < _INTS and K < _INTS, "sizes beyond 32 bits"
     stride = _matrix(x, M, K, gpu, torch.int8)
     assert w.dtype == torch.int8 and w.get_device() == gpu and w.shape == (N, K) and w.is_contiguous()
     for t, n in ((x_scale, M), (w_scale, N)):
@@ -738,6 +743,7 @@ class GroupedMatmul:
         formats = {torch.float32: CRAFT_F32, torch.bfloat16: CRAFT_BF16, torch.int8: CRAFT_I8}
         assert first.is_cuda and first.dim() == 2 and first.dtype in formats
         self.G, (self.N, self.K), self._gpu, dev = len(weights), first.shape, first.get_device(), first.device
+        assert self.N < _INTS and self.K < _INTS, "sizes beyond 32 bits"
         eight = first.dtype == torch.int8
         natural = {torch.float32: "f32", torch.bfloat16: "bf16", torch.int8: "bf16"}[first.dtype]
         assert dtype is None or eight or dtype == natural, "only 8-bit products have a choice of result"
@@ -781,6 +787,7 @@ class GroupedMatmul:
         if src is not None:
             M = src.shape[0]
             assert src.dtype == self._int32 and src.get_device() == gpu and src.shape == (M,) and src.is_contiguous()
+        assert -_INTS <= k < _INTS, "sizes beyond 32 bits"
         assert (x_scale is not None) == (a.format == CRAFT_I8)
         if x_scale is not None:
             assert x_scale.dtype == self._float32 and x_scale.get_device() == gpu and x_scale.shape == (rows,) and x_scale.is_contiguous()

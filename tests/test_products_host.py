@@ -120,3 +120,29 @@ def test_quantize_refuses_other_outputs(codes, scale):
     own = dict(codes=codes or Placed((4, 64), torch.int8), scale=scale or Placed((4,), torch.float32))
     with pytest.raises(AssertionError):
         binding.quantize_i8(Placed((4, 64), torch.float32), **own)
+
+
+class Wide(Placed):
+    device = torch.device("cpu")
+
+
+def _beyond_32_bits():
+    i8, f32, bf16 = torch.int8, torch.float32, torch.bfloat16
+    far = (1 << 32) + 64                           # 64 in the lower half
+    s = Wide((4,), f32)
+    yield "quantize K", lambda: binding.quantize_i8(Wide((4, far), f32), codes=Wide((4, far), i8), scale=s)
+    yield "matmul K", lambda: binding.matmul_i8(Wide((4, far), i8), s, Wide((4, far), i8), s, out=Wide((4, 4), bf16))
+    yield "matmul N", lambda: binding.matmul_i8(Wide((4, 64), i8), s, Wide((far, 64), i8), Wide((far,), f32), out=Wide((4, far), bf16))
+    yield "grouped K", lambda: binding.GroupedMatmul([Wide((8, far), bf16)])
+    yield "grouped N", lambda: binding.GroupedMatmul([Wide((far, 64), bf16)])
+    one = binding.GroupedMatmul([Wide((8, 64), bf16)])
+    for k in ((1 << 32) + 2, (1 << 31), -(1 << 32) + 2):
+        yield f"grouped k {k}", lambda k=k: one(Wide((4, 64), bf16), Wide((2,), torch.int32), src=Wide((4,), torch.int32), k=k, out=Wide((4, 8), bf16))
+
+
+@pytest.mark.parametrize("which", range(8))
+def test_sizes_beyond_32_bits_are_refused(which):
+    # the library's sizes are 32-bit integers: a larger one would arrive as its lower half
+    name, call = list(_beyond_32_bits())[which]
+    with pytest.raises(AssertionError, match="32 bits"):
+        call()
