@@ -6,6 +6,7 @@ import pytest
 from paper_2603_28768_amd import binding
 
 import product_reference as ref
+import product_shapes as shapes
 
 pytestmark = pytest.mark.gpu
 
@@ -460,3 +461,114 @@ def test_expert_layer_in_8_bits(torch_cuda, T, H, I, E, k):
         bound = (0.5 + 2.0 ** -7) * scale[r, None] + np.abs(hv) * 2.0 ** -7
         off_by = np.abs(y[r] - hv @ val["down"][e].T)
         assert (off_by <= bound @ np.abs(val["down"][e]).T + 1e-5 * np.abs(y[r])).all()
+
+
+# ------------------------------------------------------- products in tiles (test_product_choice.py: that they are)
+
+@pytest.mark.parametrize("fmt,out", [("i8", "bf16"), ("i8", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("is_gated,which", [(gated, i) for gated in (False, True) for i in range(len(shapes.SHAPES[gated]))])
+def test_every_tile(torch_cuda, fmt, out, is_gated, which):
+    s = shapes.SHAPES[is_gated][which]
+    K = shapes.elements(fmt, s.row_bytes)
+    print(f"tiles {fmt} {out} gated={is_gated} {s.width}x{s.height} N={s.N} K={K}", flush=True)
+    p = Problem(which + K, fmt, s.sizes, s.N, K, is_gated, out=out, k=2, front=shapes.FRONT, spare=shapes.SPARE, whole=not is_gated,
+                pad=shapes.elements(fmt, 32), out_pad=which % 2)
+    p.exact = True
+    p.check(p.run())
+
+
+@pytest.mark.parametrize("fmt", ["i8", "bf16", "f32"])
+@pytest.mark.parametrize("is_gated", [False, True])
+def test_recorded_calls_in_tiles(torch_cuda, fmt, is_gated):
+    # what a replay has to find by itself: rows of each group, other rows of x, groups that overlap and do not any more
+    torch = torch_cuda
+    G, M, N, row_bytes = shapes.CHANGING
+    p = Problem(23, fmt, [700, 3, 0, 1300, 190], N, shapes.elements(fmt, row_bytes), is_gated, k=2, spare=M - 2193, out="bf16", whole=not is_gated)
+    assert p.M == M and p.G == G
+    p.exact = True
+    other = torch.empty_like(p.out)
+    p.run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.run()
+    g = np.random.default_rng(6)
+    for off in ([0, 1, 2, 3, 4, 5], [0, 0, 0, 2193, 2193, 2200], [300, 300, 740, 1180, 1620, 2060], [0, 2200, 0, 2200, 0, 2200], [0, 700, 703, 703, 2003, 2193]):
+        p.off = np.asarray(off, np.int32)
+        p.src = g.integers(0, p.x.shape[0] * 2, M).astype(np.int32)
+        p.src[::50] = -1
+        p.d_off.copy_(_dev(p.off))
+        p.d_src.copy_(_dev(p.src))
+        fill = -7.0 if off[2] >= off[1] else float("nan")
+        p.out.fill_(fill)
+        graph.replay()
+        again = p.run(out=other.fill_(fill))
+        torch.cuda.synchronize()
+        if off[2] >= off[1]:
+            p.check(p.out)
+            assert torch.equal(again, p.out)
+        else:
+            # every place is in three groups
+            assert not bool(p.out.isnan().any()) and not bool(again.isnan().any())
+
+
+@pytest.mark.parametrize("fmt", ["i8", "bf16", "f32"])
+@pytest.mark.parametrize("is_gated", [False, True])
+@pytest.mark.parametrize("off", [[5, 2, 1500, 1500, 2150, 2150], [-4, 700, 700, 1500, 2000, 2 ** 31 - 1], [1500, 1900, 20, 800, 800, 33],
+                                 [2190, 2195, 2195, 2 ** 31 - 1, 2 ** 31 - 1, 0], [-2 ** 31, 0, 0, 0, -1, 0], [-2 ** 31, 2 ** 31 - 1, 2 ** 31 - 1, -2 ** 31, -5, -5]])
+def test_offsets_that_are_none_in_tiles(torch_cuda, fmt, is_gated, off):
+    G, M, N, row_bytes = shapes.CHANGING
+    print(f"offsets in tiles {fmt} gated={is_gated} {off}", flush=True)
+    p = Problem(9, fmt, [0] * (G - 1) + [M], N, shapes.elements(fmt, row_bytes), is_gated, out="bf16", whole=not is_gated)
+    p.exact = True
+    off = np.asarray(off, np.int32)
+    p.check(p.handle(p.d_x, _dev(off), x_scale=p.d_xs, out=p.out), off)
+
+
+@pytest.mark.parametrize("fmt", ["i8", "bf16", "f32"])
+@pytest.mark.parametrize("gathered", [False, True])
+def test_tiles_of_rows_up_to_32_bits_apart(torch_cuda, fmt, gathered):
+    """Offsets of rows, from the start of x or of a tile, between 2^31 and 2^32."""
+    torch = torch_cuda
+    rows, stride, places, N = shapes.FAR_GATHERED if gathered else shapes.FAR_IN_ORDER
+    K, step = shapes.elements(fmt, shapes.FAR_BYTES), shapes.elements(fmt, stride)
+    print(f"far rows {fmt} gathered={gathered} {rows} x {stride}", flush=True)
+    kind = {"i8": torch.int8, "bf16": torch.bfloat16, "f32": torch.float32}[fmt]
+    x = torch.empty((rows - 1) * step + K, dtype=kind, device=DEV).as_strided((rows, K), (step, 1))
+    g = np.random.default_rng(12)
+    x.copy_(_dev(g.integers(-8, 9, (rows, K)).astype(np.float32)).to(kind))
+    G = 2 if gathered else 1
+    w = _dev(g.integers(-8, 9, (G, N, K)).astype(np.float32)).to(kind)
+    one = lambda *s: torch.ones(s, device=DEV) if fmt == "i8" else None  # noqa: E731
+    cuts = [0, 301, places] if gathered else [0, places]
+    at = np.concatenate([g.integers(0, rows, places - 2), [rows - 1, rows - 2]]).astype(np.int64) if gathered else np.arange(places)
+    got = binding.GroupedMatmul(w, scales=one(G, N), dtype="f32" if fmt == "i8" else None)(
+        x, _dev(np.asarray(cuts, np.int32)), x_scale=one(rows), src=_dev(at.astype(np.int32)) if gathered else None)
+    near = x[_dev(at)].float()
+    for e, (lo, hi) in enumerate(zip(cuts, cuts[1:])):
+        # sums of 256 products of at most 64: exact in fp32
+        assert torch.equal(got[lo:hi], (near[lo:hi] @ w[e].float().T).to(got.dtype)), e
+
+
+# ------------------------------------------------------- quantisation: a width for every number of units and lanes a row
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,K,pad", [(8200, 272, 16), (8200, 512, 0), (8195, 528, 0), (8193, 768, 0), (8193, 1040, 32), (8193, 1536, 0), (9000, 800, 0), (9, 1552, 0),
+                                        (9, 2560, 0), (9, 5120, 64), (9, 6144, 0), (9, 12288, 0), (9, 20000, 0), (9, 32768, 0), (9, 32784, 0)])
+def test_quantize_rows_of_every_width(torch_cuda, dtype, rows, K, pad):
+    torch = torch_cuda
+    print(f"quantize width {dtype} {rows}x{K}+{pad}", flush=True)
+    x = _dev(_hard_rows(np.random.default_rng(rows + K), rows, K + pad)).to(binding._torch_dtype(dtype))[:, :K]
+    # the largest element of one row and one that is not finite in another, both in the last unit
+    x[1] = 0.25
+    x[1, K - 1] = -3.0
+    x[rows - 1, K - 2] = float("nan")
+    x[rows - 2, K - 16] = float("-inf")
+    room = torch.full((rows + 2, K), 77, dtype=torch.int8, device=DEV)
+    scale_room = torch.full((rows + 2,), 77.0, device=DEV)
+    codes, scale = binding.quantize_i8(x, codes=room[1:rows + 1], scale=scale_room[1:rows + 1])
+    want_codes, want_scale = ref.quantize(x.float().cpu().numpy())
+    assert np.isnan(want_scale).sum() == 2 and want_codes[1, K - 1] == -127
+    assert np.array_equal(scale.cpu().numpy(), want_scale, equal_nan=True)
+    assert np.array_equal(codes.cpu().numpy(), want_codes)
+    assert bool((room[::rows + 1] == 77).all()) and bool((scale_room[::rows + 1] == 77.0).all())
