@@ -3,8 +3,10 @@
 import numpy as np
 import pytest
 
-from paper_2603_28768_amd import binding
+import oracle
+from paper_2603_28768_amd import binding, synth
 
+from cases import Case
 import product_reference as ref
 import product_shapes as shapes
 
@@ -572,3 +574,70 @@ def test_quantize_rows_of_every_width(torch_cuda, dtype, rows, K, pad):
     assert np.array_equal(scale.cpu().numpy(), want_scale, equal_nan=True)
     assert np.array_equal(codes.cpu().numpy(), want_codes)
     assert bool((room[::rows + 1] == 77).all()) and bool((scale_room[::rows + 1] == 77.0).all())
+
+
+# ------------------------------------------------------- behind the framework's own dispatch
+
+@pytest.mark.parametrize("T", [48, 1500])
+def test_layers_on_the_dispatch_of_the_forward(torch_cuda, T):
+    """src and slot_off as the rank forward leaves them: T k places, of which one rank's are somewhere in the middle.  In bf16 the
+    layer is the forward's own, held to the checker's as that is; in 8 bits it equals the one on the rank's rows alone.  Then both
+    recorded behind the forward, replayed on other scores."""
+    torch = torch_cuda
+    cfg = synth.scaled(synth.CONFIGS["qwen3"], T=T, H=512, I=384, E=32, k=4, D=4, replica_slots=3, zipf_s=1.2, profile_batches=2)
+    case = Case(cfg)
+    rank = max(range(1, 3), key=lambda r: case.rows[r])            # places in front of its own and behind
+    fwd, x, logits = case.gpu_rank(rank)
+    first_slot, end_slot = (int(v) for v in case.rank_slot_off[rank:rank + 2])
+    src, off = fwd.debug["src"], fwd.debug["slot_off"][first_slot:end_slot + 1]
+    wg, wu, wd = fwd._weights
+    q = [[binding.quantize_i8(w) for w in ws] for ws in (wg, wu, wd)]
+    codes, scales = [[c for c, _ in m] for m in q], [[s for _, s in m] for m in q]
+    first, second = binding.GroupedMatmul(wg, up=wu), binding.GroupedMatmul(wd)
+    first8 = binding.GroupedMatmul(codes[0], scales=scales[0], up=codes[1], up_scales=scales[1])
+    second8 = binding.GroupedMatmul(codes[2], scales=scales[2], dtype="f32")
+    places = T * cfg.k
+    make = lambda n, kind: torch.full((places, n), -7.0, dtype=kind, device=DEV)  # noqa: E731
+    h, y, h8, y8 = make(cfg.I, torch.bfloat16), make(cfg.H, torch.bfloat16), make(cfg.I, torch.bfloat16), make(cfg.H, torch.float32)
+
+    def step():
+        fwd(x, logits)
+        first(x, off, src=src, k=cfg.k, out=h)
+        second(h, off, out=y)
+        xq, xs = binding.quantize_i8(x)
+        first8(xq, off, x_scale=xs, src=src, k=cfg.k, out=h8)
+        hq, hs = binding.quantize_i8(h8)
+        second8(hq, off, x_scale=hs, out=y8)
+
+    def check():
+        torch.cuda.synchronize()
+        bounds = off.cpu().numpy()
+        lo, hi = int(bounds[0]), int(bounds[-1])
+        assert 0 < lo < hi < places
+        mine = np.zeros(places, bool)
+        mine[lo:hi] = True
+        for t in (h, y, h8, y8):
+            assert bool((t[_dev(~mine)] == -7.0).all()) and not bool((t[lo:hi] == -7.0).all(dim=1).any())
+        ref_out = oracle.rank_forward(case.x, logits.cpu().numpy(), cfg.k, case.slot_expert, case.rank_slot_off, rank, case.weights_of, True, None)["out"]
+        dest, weight = fwd.debug["dest"].cpu().numpy().reshape(T, cfg.k), fwd.debug["topk_w"].cpu().double().numpy()
+        here = (dest >= lo) & (dest < hi)
+        values = y.double().cpu().numpy()[np.where(here, dest, 0)]
+        out = (values * np.where(here, weight, 0.0)[:, :, None]).sum(axis=1)
+        assert np.abs(out - ref_out).max() <= 1e-2 * np.abs(ref_out).max()
+        xq, xs = binding.quantize_i8(x)
+        near = (off - lo).contiguous()
+        one = first8(xq, near, x_scale=xs, src=src[lo:hi].contiguous(), k=cfg.k)
+        hq, hs = binding.quantize_i8(one)
+        assert torch.equal(one, h8[lo:hi]) and torch.equal(second8(hq, near, x_scale=hs), y8[lo:hi])
+
+    step()
+    check()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for shift in (1, 5):
+        logits.copy_(logits.roll(shift, dims=1))
+        for t in (h, y, h8, y8):
+            t.fill_(-7.0)
+        graph.replay()
+        check()
