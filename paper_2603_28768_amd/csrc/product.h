@@ -6,6 +6,7 @@
 // instruction does not matter as long as both operands agree.
 #pragma once
 
+#include "ffn_common.h"
 #include "kernels.h"
 
 namespace craft {
@@ -16,8 +17,6 @@ typedef __bf16 pbf16x8_t __attribute__((ext_vector_type(8)));
 typedef unsigned int raw_t __attribute__((ext_vector_type(4)));        // 16 bytes of a row
 
 // Addresses read from a table in memory: said to be global, they are else read as flat ones, which wait for LDS as well.
-typedef const unsigned char __attribute__((address_space(1))) *bytes_t;
-typedef const raw_t __attribute__((address_space(1))) *pieces_t;
 typedef const float __attribute__((address_space(1))) *scales_t;
 
 template <int FMT> struct Numbers;
@@ -42,14 +41,6 @@ template <> struct Numbers<CRAFT_I8> {
     }
 };
 
-// Two fp32 values to a pair of bf16, to nearest even: one instruction.
-static __device__ __forceinline__ uint32_t product_bf16_pair(float lo, float hi) {
-    typedef __bf16 pair_t __attribute__((ext_vector_type(2)));
-    typedef float floats_t __attribute__((ext_vector_type(2)));
-    const floats_t v = {lo, hi};
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, pair_t));
-}
-
 // silu for fp32 results, and for those rounded to bf16 right after: the hardware's exponential and reciprocal (2^-21 off
 // where silu matters), with numerator and denominator scaled down alike, since a reciprocal below 2^-126 becomes zero
 // (g < -87.3, where silu times a large second factor still is a number).
@@ -61,7 +52,7 @@ static __device__ __forceinline__ float silu_bf16(float g) { return g * 0x1p-8f 
 static __device__ __forceinline__ void store_columns(const ProductArgs &a, int64_t row, int32_t col, const float (&v)[4], bool whole) {
     if (a.out_dtype == CRAFT_BF16) {
         uint16_t *p = static_cast<uint16_t *>(a.out) + row * a.out_stride + col;
-        const uint2 two = make_uint2(product_bf16_pair(v[0], v[1]), product_bf16_pair(v[2], v[3]));
+        const uint2 two = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
         if (whole && col + 4 <= a.N) {
             *reinterpret_cast<uint2 *>(p) = two;
         } else {

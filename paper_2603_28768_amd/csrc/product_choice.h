@@ -9,9 +9,9 @@
 namespace craft {
 
 // Which kernel, and the size of its tiles: what is expected to take the least time, from sizes that the host knows.  How rows are
-// spread over groups only the GPU knows.  Fitted to times of 70 drawn products of 6 to 3700 rows (1 to 68 groups, every type), of
-// which the choice takes 1.008 of the better kernel's time in the geometric mean; units up to 127 rows or 15 a group and tiles
-// beyond took 1.13.
+// spread over groups only the GPU knows.  Fitted to times of 70 drawn products of 6 to 3700 rows (1 to 68 groups, every type).  On 70
+// others of the same ranges the choice takes 1.01 of the better kernel's time in the geometric mean, units everywhere 1.06 and tiles
+// wherever they can be 1.16; on the 23 of them above 10 us 0.99 (at worst 1.08), 1.09 and 1.12.
 struct Sizes {
     double rows, groups, columns, slabs;           // groups: those that can have rows
     double matrix;                                 // cycles of a slab's matrix instructions, relative to 16 bits
@@ -39,7 +39,7 @@ inline double stream_time(const ProductArgs &a, const Sizes &z) {
     else time = std::ceil(units / a.num_cu) * (std::max(bytes / 60, matrix / 4) + 2000);
     return std::max(time, z.weights);
 }
-// ns of tiles.  A slab of a tile of FW x FX fragments a wave takes 88 FW + 26 FW FX cycles (0.39 us at 4 x 4, 0.87 at 8 x 4, 1.2 at
+// ns of tiles.  A slab of a tile of FW x FX fragments a wave takes 88 FW + 26 FW FX cycles (0.38 us at 4 x 4, 0.77 at 8 x 4, 1.2 at
 // 8 x 8), a tile 12000 and 150 for every product of fragments beside its slabs, at 2 GHz.  A third of a tile more for each group is
 // assumed, and that behind the first round tiles end at different times; groups of 64 rows in the mean: low tiles.
 inline double tile_time(const ProductArgs &a, const Sizes &z, int32_t *width, int32_t *height) {

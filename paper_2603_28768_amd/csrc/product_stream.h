@@ -8,7 +8,6 @@
 // lines for every 16 lanes) a CU gets 38 GB/s of its L1, which weights and rows have to share; this way 123.
 #pragma once
 
-#include "ffn_common.h"
 #include "product.h"
 
 namespace craft {

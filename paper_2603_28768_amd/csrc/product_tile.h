@@ -11,13 +11,12 @@
 //
 // A group's rows are shared evenly among as few tiles of at most `height` rows as hold them, in whole fragments of 32.  Groups of up
 // to 64 rows, which stream their weights through one CU at what that gets out of HBM, have tiles of 128 weight rows with up to six stages.
-// The list has the tallest tiles first.
+// The list has the tallest tiles first.  Groups that overlap can have more tiles than were launched for; those are cut otherwise.
 #pragma once
 
 #include <algorithm>
 #include <type_traits>
 
-#include "ffn_common.h"
 #include "product.h"
 
 namespace craft {
@@ -294,7 +293,7 @@ static __device__ __forceinline__ void product_tile(const ProductArgs &a, const 
                 if constexpr (GATED)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) y[0][e] = (bf16 ? silu_bf16(y[0][e]) : silu_f32(y[0][e])) * y[SIDES - 1][e];
-                if constexpr (bf16) *reinterpret_cast<uint2 *>(to + f / SIDES * 32) = make_uint2(product_bf16_pair(y[0][0], y[0][1]), product_bf16_pair(y[0][2], y[0][3]));
+                if constexpr (bf16) *reinterpret_cast<uint2 *>(to + f / SIDES * 32) = make_uint2(bf16_pair(y[0][0], y[0][1]), bf16_pair(y[0][2], y[0][3]));
                 else *reinterpret_cast<float4 *>(to + f / SIDES * 64) = make_float4(y[0][0], y[0][1], y[0][2], y[0][3]);
             }
             if (gather && !row_live[row])          // (seldom)
