@@ -581,7 +581,7 @@ def test_quantize_rows_of_every_width(torch_cuda, dtype, rows, K, pad):
 @pytest.mark.parametrize("T", [48, 1500])
 def test_layers_on_the_dispatch_of_the_forward(torch_cuda, T):
     """src and slot_off as the rank forward leaves them: T k places, of which one rank's are somewhere in the middle.  In bf16 the
-    layer is the forward's own, held to the checker's as that is; in 8 bits it equals the one on the rank's rows alone.  Then both
+    layer is the forward's own, held to the oracle's as that is; in 8 bits it equals the one on the rank's rows alone.  Then both
     recorded behind the forward, replayed on other scores."""
     torch = torch_cuda
     cfg = synth.scaled(synth.CONFIGS["qwen3"], T=T, H=512, I=384, E=32, k=4, D=4, replica_slots=3, zipf_s=1.2, profile_batches=2)
